@@ -165,8 +165,9 @@ def _rows8(x, group):
     x = _groups(x.float(), group)
     amax = x.abs().amax(2, keepdim=True)
     small = amax < 2.0 ** -116
-    q = torch.where(small, 0.0, torch.round(x * (127.0 / amax)))
-    s = torch.where(small, 0.0, amax / 127.0)
+    most = torch.full_like(amax, 127.0)         # (a quotient of tensors is one division; with a number it is a reciprocal and a product)
+    q = torch.where(small, 0.0, torch.round(x * (most / amax)))
+    s = torch.where(small, 0.0, amax / most)
     return q.to(torch.int8).reshape(rows, -1)[:, :cols], s[:, :, 0]
 
 
