@@ -17,6 +17,8 @@
  *   7. the time oracle estimate from measured runs         (Sec. 5)
  *   8. a search for better orders by proposed exchanges,
  *      measured by 4                                       (Sec. 3.1, 4.3)
+ *   9. operators of a worker's layers in 8 bits: what runs
+ *      between the transfers, to be timed by 7
  * 3 and 4 also take the timing samples as float32 arrays (tictac_simulate_f32,
  * tictac_tac_simulate_f32).
  *
@@ -45,6 +47,7 @@
 #ifndef TICTAC_H
 #define TICTAC_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -66,6 +69,9 @@ typedef enum tictac_status {
 
 /* TIC priority of a recv that no multi-dependency op consumes (M+ = +infinity). */
 #define TICTAC_PRIO_INF INT32_MAX
+
+/* Element types of the layers' operators (at the end of this file). */
+typedef enum tictac_dtype { TICTAC_F32 = 0, TICTAC_F16 = 1, TICTAC_BF16 = 2 } tictac_dtype;
 
 typedef struct tictac_dag tictac_dag; /* opaque; owns device copies of the graph, op.dep and derived tables */
 typedef void *tictac_stream;          /* a hipStream_t; NULL = the default stream */
@@ -309,6 +315,67 @@ int tictac_order_search(const tictac_dag *dag, int32_t B, const int32_t *order, 
                         int32_t n_moves, const int32_t *moves, const double *op_time, const double *recv_time,
                         int32_t *best_order, double *best_makespan, double *start_makespan, int32_t *n_accepted,
                         tictac_stream stream);
+
+/*
+ * ---- Layers: what a worker's iteration does between the transfers ----
+ * Operators of layers whose parameters are transferred in 8 bits (a recv of a quarter of the bytes of float32) and whose
+ * activations are kept in 8 bits for the backward pass.  They share one format, "8-bit rows": int8 [rows][ld], ld a multiple of
+ * 128, on a 16-byte boundary, every row readable up to the next multiple of 128 columns and zero from its last column to there; and
+ * float32 scales: [rows] (group 0: one per row, the operands of the products) or [rows][ceil(cols / 128)] (group 128: one
+ * per 128 columns, kept activations).  The value is q * scale.
+ * x, y, dy, dx and dw are device arrays of `dtype` (tictac_dtype), row-major, a stride (ld_...) in elements between rows; vectors
+ * are contiguous.  rows >= 0 and outs >= 0 may be zero, cols >= 1.  Sums and statistics are float32 (sums of 8-bit products int32).
+ * A workspace is the caller's device memory on a 256-byte boundary, of the size that the function beside it gives; nothing in it is
+ * kept between calls.  These calls only launch kernels (no allocation, no wait: they can be captured) and may overlap on
+ * different streams with workspaces of their own.
+ */
+
+/* scale = amax / 127 (amax: largest magnitude of the row, or of 128 columns of it), q = round(x * (127 / amax)) in float32, ties
+ * to even.  amax < 2^-116: zeros with a scale of zero.  A NaN or an infinity makes the scale NaN: the whole row (or group) reads as NaN.  The scale
+ * is at most 0x1.020406p121, so that finite values read back finite in float32. */
+int tictac_quantize_rows(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ld_x, int32_t group, int8_t *q, int64_t ld_q,
+                         float *scale, tictac_stream stream);
+
+/* x = q * scale, rounded to dtype. */
+int tictac_dequantize_rows(int32_t dtype, int64_t rows, int64_t cols, const int8_t *q, int64_t ld_q, const float *scale, int32_t group,
+                           void *x, int64_t ld_x, tictac_stream stream);
+
+/* y = (x - mean) rstd weight + bias with mean and rstd = 1 / sqrt(variance + eps) of each row of x.
+ *   weight, bias [cols] of param_dtype, may be NULL (ones, zeros)
+ *   y                   may be NULL
+ *   mean, rstd [rows]   float32, for the backward pass
+ *   yq, y_scale         may be NULL: y as 8-bit rows of group 0, formed from the float32 values
+ *   xq, x_scale         may be NULL: x as 8-bit rows of group 128, to be kept for the backward pass */
+int tictac_layer_norm(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ld_x, int32_t param_dtype, const void *weight,
+                      const void *bias, float eps, void *y, int64_t ld_y, float *mean, float *rstd, int8_t *yq, int64_t ld_yq,
+                      float *y_scale, int8_t *xq, int64_t ld_xq, float *x_scale, tictac_stream stream);
+
+/* With xh = (x - mean) rstd and g = dy weight: dx = rstd (g - mean(g) - xh mean(g xh)), dweight = sum of dy xh over the rows, dbias = sum
+ * of dy over the rows (both of param_dtype).  x, or xq and x_scale (8-bit rows of group 128).  dx, dweight and dbias may each be
+ * NULL; the workspace is needed for dweight and dbias.  Sums over rows have a fixed order. */
+int tictac_layer_norm_backward_workspace(int64_t rows, int64_t cols, size_t *bytes);
+int tictac_layer_norm_backward(int32_t dtype, int64_t rows, int64_t cols, const void *dy, int64_t ld_dy, const void *x, int64_t ld_x,
+                               const int8_t *xq, int64_t ld_xq, const float *x_scale, int32_t param_dtype, const void *weight,
+                               const float *mean, const float *rstd, void *dx, int64_t ld_dx, void *dweight, void *dbias,
+                               void *workspace, size_t workspace_bytes, tictac_stream stream);
+
+/* y[t][o] = x_scale[t] w_scale[o] sum_i xq[t][i] wq[o][i] + bias[o], sums exact.
+ *   x  [rows][cols] of dtype, rounded to 8 bits in the call, or NULL: xq, x_scale (8-bit rows of group 0)
+ *   wq [outs][ld_w], w_scale [outs]: 8-bit rows of group 0, one per output channel
+ *   bias [outs] of bias_dtype, may be NULL
+ * At most 2^21 rows and outputs, 2^17 columns, strides of 8-bit rows up to 2^24 (TICTAC_ERR_UNSUPPORTED). */
+int tictac_linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
+int tictac_linear_q8(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *x, int64_t ld_x, const int8_t *xq,
+                     int64_t ld_xq, const float *x_scale, const int8_t *wq, int64_t ld_w, const float *w_scale, int32_t bias_dtype,
+                     const void *bias, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, tictac_stream stream);
+
+/* Gradients of the above, the rounding of x taken for the identity: dx[t][i] = sum_o dy[t][o] w_scale[o] wq[o][i],
+ * dw[o][i] = sum_t dy[t][o] x_scale[t] xq[t][i], db[o] = sum_t dy[t][o]; all of dtype, each may be NULL. */
+int tictac_linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
+int tictac_linear_q8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *dy, int64_t ld_dy, const int8_t *xq,
+                              int64_t ld_xq, const float *x_scale, const int8_t *wq, int64_t ld_w, const float *w_scale, void *dx,
+                              int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,
+                              tictac_stream stream);
 
 /* Message of the last error on the calling thread; valid until its next call. */
 const char *tictac_last_error(void);

@@ -34,6 +34,9 @@ EXPORTS = (
     "tictac_tac_simulate_noalloc",
     "tictac_simulate_f32", "tictac_tac_simulate_f32",
     "tictac_simulate_channels", "tictac_simulate_sends", "tictac_straggler_effect", "tictac_time_oracle_min", "tictac_order_search",
+    "tictac_quantize_rows", "tictac_dequantize_rows", "tictac_layer_norm", "tictac_layer_norm_backward_workspace",
+    "tictac_layer_norm_backward", "tictac_linear_q8_workspace", "tictac_linear_q8", "tictac_linear_q8_backward_workspace",
+    "tictac_linear_q8_backward",
     "tictac_last_error", "tictac_version",
 )
 

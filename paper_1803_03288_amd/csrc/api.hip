@@ -30,8 +30,7 @@ void set_error(const char *fmt, ...)
     va_end(ap);
 }
 
-// No exception leaves an entry point: each is a function try block that ends in TT_CATCH.
-static int caught()
+int caught()
 {
     try {
         throw;
@@ -44,16 +43,6 @@ static int caught()
     }
     return TICTAC_ERR_NO_MEM;
 }
-#define TT_CATCH catch (...) { return caught(); }
-
-#define HIP_TRY(expr)                                                                        \
-    do {                                                                                     \
-        hipError_t e_ = (expr);                                                              \
-        if (e_ != hipSuccess) {                                                              \
-            set_error("%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, __LINE__); \
-            return TICTAC_ERR_HIP;                                                           \
-        }                                                                                    \
-    } while (0)
 
 // Device memory of the handles.  A program that takes in one graph after another allocates and frees blocks of the
 // same sizes all the time, and hipMalloc and hipFree cost tens of microseconds each, large blocks much more.  Freed

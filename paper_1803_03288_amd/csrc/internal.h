@@ -24,6 +24,19 @@ inline size_t k1_nodes_lds(int32_t ring, int32_t wc, int32_t per_pass)
 
 void set_error(const char *fmt, ...);
 
+// No exception leaves an entry point: each is a function try block that ends in TT_CATCH.
+int caught();
+#define TT_CATCH catch (...) { return caught(); }
+
+#define HIP_TRY(expr)                                                                        \
+    do {                                                                                     \
+        hipError_t e_ = (expr);                                                              \
+        if (e_ != hipSuccess) {                                                              \
+            set_error("%s failed: %s (%s:%d)", #expr, hipGetErrorString(e_), __FILE__, __LINE__); \
+            return TICTAC_ERR_HIP;                                                           \
+        }                                                                                    \
+    } while (0)
+
 // A device allocation of a handle (see Packer::commit and release() in api.hip).
 struct Block {
     void *p = nullptr;
@@ -368,5 +381,77 @@ struct SearchArgs {
 };
 // hipErrorNotSupported: the graph is outside what the kernel handles
 hipError_t launch_order_search(Dag &d, const SearchArgs &a, hipStream_t s);
+
+// ---- layers: activations and weights in 8 bits, layer norm, products (k7_*.hip, k8_*.hip; entry points in api_layers.hip) ----
+// 8-bit rows: int8 [rows][ld], ld a multiple of 128, zeros from the last column to the next multiple of 128; float32 scales, one per row or
+// (group = kRows8Group) one per so many columns.
+constexpr int32_t kRows8Group = 128;
+struct QuantizeArgs {
+    int32_t dtype;
+    int64_t rows, cols;
+    const void *x;              // to 8 bits
+    void *out;                  // and back
+    int64_t ld_x;               // of x or out, in elements
+    int32_t group;              // 0 or kRows8Group
+    int8_t *q;
+    int64_t ld_q;
+    float *scale;
+};
+hipError_t launch_quantize_rows(const QuantizeArgs &p, hipStream_t s);
+hipError_t launch_dequantize_rows(const QuantizeArgs &p, hipStream_t s);
+
+struct NormArgs {
+    int32_t dtype, param_dtype;
+    int64_t rows, cols;
+    const void *x;              // NULL (backward pass only): xq, xs
+    int64_t ld_x;
+    const void *weight, *bias;  // may be NULL: ones, zeros
+    float eps;
+    void *y;                    // may be NULL
+    int64_t ld_y;
+    float *mean, *rstd;
+    int8_t *yq;                 // may be NULL: y in 8 bits, a scale per row
+    int64_t ld_yq;
+    float *ys;
+    int8_t *xq;                 // may be NULL: x in 8 bits, a scale per kRows8Group columns
+    int64_t ld_xq;
+    float *xs;
+    // backward pass
+    const void *dy;
+    int64_t ld_dy;
+    void *dx;
+    int64_t ld_dx;
+    void *dweight, *dbias;
+    void *workspace;
+};
+hipError_t launch_layer_norm(const NormArgs &p, hipStream_t s);
+hipError_t launch_layer_norm_backward(const NormArgs &p, hipStream_t s);
+size_t layer_norm_backward_workspace(int64_t rows, int64_t cols);
+
+struct LinearArgs {
+    int32_t dtype, bias_dtype;
+    int64_t rows, cols, outs;
+    const void *x;              // float rows, or NULL: xq, xs
+    int64_t ld_x;
+    const int8_t *xq;
+    int64_t ld_xq;
+    const float *xs;
+    const int8_t *w;            // [outs][ld_w]
+    int64_t ld_w;
+    const float *ws;            // [outs]
+    const void *bias;           // may be NULL
+    void *y;
+    int64_t ld_y;
+    void *workspace;
+    // backward pass (dtype: of dy, dx, dw, db)
+    const void *dy;
+    int64_t ld_dy;
+    void *dx, *dw, *db;         // each may be NULL
+    int64_t ld_dx, ld_dw;
+};
+hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s);
+size_t linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs);
+hipError_t launch_linear_q8_backward(const LinearArgs &p, hipStream_t s);
+size_t linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs);
 
 }  // namespace tictac

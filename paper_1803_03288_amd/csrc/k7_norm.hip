@@ -1,0 +1,510 @@
+// Layer norm over the rows of x:
+//   mean = sum x / D,  var = sum (x - mean)^2 / D,  rstd = 1 / sqrt(var + eps),  y = (x - mean) rstd w + b
+// and its gradients, with xh = (x - mean) rstd and g = dy w:
+//   dx = rstd (g - mean(g) - xh mean(g xh)),  dw = sum over rows of dy xh,  db = sum over rows of dy
+// Statistics and sums in float32, from a row held in registers: the variance is that of the differences from the mean, not a
+// difference of large sums.  The output can be 8-bit rows with a scale per row (the operand of the product that follows), and the
+// input can be kept in 8 bits from the same pass; the backward pass takes the input itself or those 8-bit rows.
+// Bound by memory: a row is read once and stays in registers; the parameters stay there from row to row.
+#include "rows8.h"
+
+// Which products and sums are one operation is written out (fmaf): the kernels for rows on and off 16-byte boundaries, for a wave and for a
+// workgroup then give the same bits.
+#pragma clang fp contract(off)
+
+namespace tictac {
+
+// Sums and maxima over the threads of a row: a wave, or a workgroup through LDS.  Two sets of cells in turn, so that one barrier a
+// reduction is enough.
+template <int THREADS>
+struct RowReduce {
+    static constexpr int kWaves = THREADS / 64;
+    float (*cells)[2][kWaves];          // LDS, [2][2][kWaves]
+    int turn = 0;
+    __device__ __forceinline__ void sum2(float &a, float &b)
+    {
+        a = wave_sum_f32(a);
+        b = wave_sum_f32(b);
+        if (THREADS == 64) return;
+        if ((threadIdx.x & 63) == 0) { cells[turn][0][threadIdx.x >> 6] = a; cells[turn][1][threadIdx.x >> 6] = b; }
+        __syncthreads();
+        a = b = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) { a += cells[turn][0][i]; b += cells[turn][1][i]; }
+        turn ^= 1;
+    }
+    __device__ __forceinline__ float sum(float a)
+    {
+        a = wave_sum_f32(a);
+        if (THREADS == 64) return a;
+        if ((threadIdx.x & 63) == 0) cells[turn][0][threadIdx.x >> 6] = a;
+        __syncthreads();
+        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) a += cells[turn][0][i];
+        turn ^= 1;
+        return a;
+    }
+    __device__ __forceinline__ uint32_t max(uint32_t m)
+    {
+        m = wave_max_u32(m);
+        if (THREADS == 64) return m;
+        if ((threadIdx.x & 63) == 0) cells[turn][0][threadIdx.x >> 6] = __builtin_bit_cast(float, m);
+        __syncthreads();
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) m = ::max(m, __builtin_bit_cast(uint32_t, cells[turn][0][i]));
+        turn ^= 1;
+        return m;
+    }
+};
+
+// Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns, four waves 8 192, sixteen 16 384 (the
+// backward pass keeps four floats for each column of its thread: with more, registers would spill).  Longer rows are read
+// several times (norm_long_kernel).
+constexpr int64_t kLongest = 16384;
+
+template <int THREADS>
+struct RowShape {
+    static constexpr int kBlock = THREADS < 256 ? 256 : THREADS;        // threads of a workgroup
+    static constexpr int kRows = kBlock / THREADS;                      // rows it has under way
+};
+
+template <int DT, bool WIDE, int THREADS, int NC>
+__global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_kernel(NormArgs p)
+{
+    using E = Elem<DT>;
+    using T = typename E::type;
+    constexpr int kRows = RowShape<THREADS>::kRows;
+    __shared__ float cells[2][2][RowReduce<THREADS>::kWaves];
+    RowReduce<THREADS> r{cells};
+    const int t = threadIdx.x % THREADS;
+    const int64_t cols = p.cols, padded = (cols + 127) / 128 * 128, groups = padded / 128;
+    const float per = 1.0f / (float)cols;
+    float w[NC][8], b[NC][8];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int64_t col = (int64_t)(j * THREADS + t) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { w[j][i] = 1.0f; b[j][i] = 0.0f; }
+        if (p.weight) params8(p.weight, p.param_dtype, col, cols, w[j]);
+        if (p.bias) params8(p.bias, p.param_dtype, col, cols, b[j]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS; row < p.rows; row += (int64_t)gridDim.x * kRows) {
+        float v[NC][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            E::floats(load8<DT, WIDE>((const T *)p.x + row * p.ld_x, (int64_t)(j * THREADS + t) * 8, cols), v[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[j][i];
+        }
+        if (p.xq) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                const int64_t col = (int64_t)(j * THREADS + t) * 8;
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[j][i]));
+                const RowScale s = row_scale(row16_max(m));
+                if (col >= padded) continue;
+                *(uint2 *)(p.xq + row * p.ld_xq + col) = quantized8(v[j], s);
+                if ((t & 15) == 0) p.xs[row * groups + (col >> 7)] = s.scale;
+            }
+        }
+        const float mean = r.sum(sum) * per;
+        float sq = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int64_t col = (int64_t)(j * THREADS + t) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = col + i < cols ? v[j][i] - mean : 0.0f;
+                v[j][i] = d;
+                sq = fmaf(d, d, sq);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(r.sum(sq), per, p.eps));
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int64_t col = (int64_t)(j * THREADS + t) * 8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[j][i] = col + i < cols ? fmaf(v[j][i] * rstd, w[j][i], b[j][i]) : 0.0f;
+                m = max(m, magnitude(v[j][i]));
+            }
+            if (p.y) store8<DT, WIDE>((T *)p.y + row * p.ld_y, col, cols, v[j]);
+        }
+        if (p.yq) {
+            const RowScale s = row_scale(r.max(m));
+#pragma unroll
+            for (int j = 0; j < NC; ++j) {
+                const int64_t col = (int64_t)(j * THREADS + t) * 8;
+                if (col < padded) *(uint2 *)(p.yq + row * p.ld_yq + col) = quantized8(v[j], s);
+            }
+            if (t == 0) p.ys[row] = s.scale;
+        }
+        if (t == 0) { p.mean[row] = mean; p.rstd[row] = rstd; }
+    }
+}
+
+// ---- rows of any length: read again for every step ----
+template <int DT, bool WIDE>
+__device__ __forceinline__ void input8(const NormArgs &p, int64_t row, int64_t col, float *v)
+{
+    Elem<DT>::floats(load8<DT, WIDE>((const typename Elem<DT>::type *)p.x + row * p.ld_x, col, p.cols), v);
+}
+
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs p)
+{
+    using T = typename Elem<DT>::type;
+    __shared__ float cells[2][2][16];
+    RowReduce<1024> r{cells};
+    const int64_t cols = p.cols, padded = (cols + 127) / 128 * 128, groups = padded / 128;
+    const float per = 1.0f / (float)cols;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        float sum = 0.0f, sq = 0.0f;
+        for (int64_t col = threadIdx.x * 8; col < padded; col += 8192) {
+            float v[8];
+            uint32_t m = 0;
+            input8<DT, WIDE>(p, row, col, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { sum += v[i]; m = max(m, magnitude(v[i])); }
+            if (!p.xq) continue;
+            const RowScale s = row_scale(row16_max(m));         // (128 columns: all 16 lanes are in the loop, or none)
+            *(uint2 *)(p.xq + row * p.ld_xq + col) = quantized8(v, s);
+            if ((threadIdx.x & 15) == 0) p.xs[row * groups + (col >> 7)] = s.scale;
+        }
+        const float mean = r.sum(sum) * per;
+        for (int64_t col = threadIdx.x * 8; col < cols; col += 8192) {
+            float v[8];
+            input8<DT, WIDE>(p, row, col, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = col + i < cols ? v[i] - mean : 0.0f;
+                sq = fmaf(d, d, sq);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(r.sum(sq), per, p.eps));
+        uint32_t m = 0;
+        RowScale s{0.0f, 0.0f};
+        for (int turn = 0; turn < (p.yq ? 2 : 1); ++turn) {     // (the second time with the largest magnitude known)
+            for (int64_t col = threadIdx.x * 8; col < padded; col += 8192) {
+                float v[8], w[8], b[8];
+                input8<DT, WIDE>(p, row, col, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) { w[i] = 1.0f; b[i] = 0.0f; }
+                if (p.weight) params8(p.weight, p.param_dtype, col, cols, w);
+                if (p.bias) params8(p.bias, p.param_dtype, col, cols, b);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[i] = col + i < cols ? fmaf((v[i] - mean) * rstd, w[i], b[i]) : 0.0f;
+                    m = max(m, magnitude(v[i]));
+                }
+                if (turn == 0 && p.y) store8<DT, WIDE>((T *)p.y + row * p.ld_y, col, cols, v);
+                if (turn == 1) *(uint2 *)(p.yq + row * p.ld_yq + col) = quantized8(v, s);
+            }
+            if (turn == 0 && p.yq) s = row_scale(r.max(m));
+        }
+        if (threadIdx.x == 0) {
+            p.mean[row] = mean;
+            p.rstd[row] = rstd;
+            if (p.yq) p.ys[row] = s.scale;
+        }
+    }
+}
+
+// ---- backward ----
+// A workgroup takes every so many-th row and keeps the sums of its rows for dw and db in registers; they go to the workspace, [workgroup][2][cols],
+// and a second kernel adds them up in the order of the workgroups: the same sums at every run, without atomics.
+constexpr int kStrips = 512;
+
+template <int DT, bool WIDE, bool SAVED>
+struct NormRow {                                    // eight columns of dy and of x as they lie in memory
+    typename Elem<DT>::raw dy, x;
+    uint2 q;
+    float s;
+    __device__ __forceinline__ void load(const NormArgs &p, int64_t row, int64_t col, int64_t groups)
+    {
+        using T = typename Elem<DT>::type;
+        dy = load8<DT, WIDE>((const T *)p.dy + row * p.ld_dy, col, p.cols);
+        if (!SAVED) {
+            x = load8<DT, WIDE>((const T *)p.x + row * p.ld_x, col, p.cols);
+        } else if (col < p.cols) {
+            q = *(const uint2 *)(p.xq + row * p.ld_xq + col);
+            s = p.xs[row * groups + (col >> 7)];
+        } else {
+            q = uint2{0, 0};
+            s = 0.0f;
+        }
+    }
+    // dy, and x - mean with one rounding (where x lies near the mean, that of q * scale alone would be as large as what is left)
+    __device__ __forceinline__ void floats(float mean, float *g, float *d) const
+    {
+        Elem<DT>::floats(dy, g);
+        if (!SAVED) Elem<DT>::floats(x, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = SAVED ? fmaf(whole8(q, i), s, -mean) : d[i] - mean;
+    }
+};
+
+template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
+__global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward_kernel(NormArgs p)
+{
+    using T = typename Elem<DT>::type;
+    constexpr int kRows = RowShape<THREADS>::kRows;
+    __shared__ float cells[2][2][RowReduce<THREADS>::kWaves];
+    __shared__ float join[kRows > 1 ? kRows * 2 * NC * THREADS * 8 : 1];
+    RowReduce<THREADS> r{cells};
+    const int t = threadIdx.x % THREADS;
+    const int64_t cols = p.cols, groups = (cols + 127) / 128, step = (int64_t)gridDim.x * kRows;
+    const float per = 1.0f / (float)cols;
+    float w[NC][8], dw[NC][8], db[NC][8];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { w[j][i] = 1.0f; dw[j][i] = db[j][i] = 0.0f; }
+        if (p.weight) params8(p.weight, p.param_dtype, (int64_t)(j * THREADS + t) * 8, cols, w[j]);
+    }
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
+    NormRow<DT, WIDE, SAVED> next[NC];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (row < p.rows) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) next[j].load(p, row, (int64_t)(j * THREADS + t) * 8, groups);
+        next_mean = p.mean[row];
+        next_rstd = p.rstd[row];
+    }
+    for (; row < p.rows; row += step) {
+        float g[NC][8], xh[NC][8];
+        float sum_g = 0.0f, sum_gx = 0.0f;
+        const float mean = next_mean, rstd = next_rstd;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            const int64_t col = (int64_t)(j * THREADS + t) * 8;
+            next[j].floats(mean, g[j], xh[j]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                xh[j][i] = col + i < cols ? xh[j][i] * rstd : 0.0f;
+                dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
+                db[j][i] += g[j][i];
+                g[j][i] *= w[j][i];
+                sum_g += g[j][i];
+                sum_gx = fmaf(g[j][i], xh[j][i], sum_gx);
+            }
+        }
+        if (row + step < p.rows) {                              // the next row's loads are under way during the sums
+#pragma unroll
+            for (int j = 0; j < NC; ++j) next[j].load(p, row + step, (int64_t)(j * THREADS + t) * 8, groups);
+            next_mean = p.mean[row + step];
+            next_rstd = p.rstd[row + step];
+        }
+        r.sum2(sum_g, sum_gx);
+        sum_g *= per;
+        sum_gx *= per;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = rstd * fmaf(-xh[j][i], sum_gx, g[j][i] - sum_g);
+            if (p.dx) store8<DT, WIDE>((T *)p.dx + row * p.ld_dx, (int64_t)(j * THREADS + t) * 8, cols, d);
+        }
+    }
+    if (!p.workspace) return;
+    float *part = (float *)p.workspace + (int64_t)blockIdx.x * 2 * cols;
+    if (kRows > 1) {                                            // the rows of a workgroup first, in order
+        constexpr int kWidth = NC * THREADS * 8;
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                join[(threadIdx.x / THREADS * 2 + 0) * kWidth + (j * THREADS + t) * 8 + i] = dw[j][i];
+                join[(threadIdx.x / THREADS * 2 + 1) * kWidth + (j * THREADS + t) * 8 + i] = db[j][i];
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * kWidth; c += RowShape<THREADS>::kBlock) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kRows; ++k) sum += join[k * 2 * kWidth + c];
+            const int col = c % kWidth;
+            if (col < cols) part[c / kWidth * cols + col] = sum;
+        }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t col = (int64_t)(j * THREADS + t) * 8 + i;
+            if (col < cols) { part[col] = dw[j][i]; part[cols + col] = db[j][i]; }
+        }
+}
+
+// dy, and x - mean from x or from the 8-bit rows (NormRow), col < cols
+template <int DT, bool WIDE>
+__device__ __forceinline__ void inputs8(const NormArgs &p, int64_t row, int64_t col, float mean, float *g, float *d)
+{
+    const int64_t groups = (p.cols + 127) / 128;
+    if (p.x) {
+        NormRow<DT, WIDE, false> r;
+        r.load(p, row, col, groups);
+        r.floats(mean, g, d);
+    } else {
+        NormRow<DT, WIDE, true> r;
+        r.load(p, row, col, groups);
+        r.floats(mean, g, d);
+    }
+}
+
+// dx of rows of any length
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(1024) void norm_long_dx_kernel(NormArgs p)
+{
+    using E = Elem<DT>;
+    using T = typename E::type;
+    __shared__ float cells[2][2][16];
+    RowReduce<1024> r{cells};
+    const int64_t cols = p.cols;
+    const float per = 1.0f / (float)cols;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float sum_g = 0.0f, sum_gx = 0.0f;
+        for (int turn = 0; turn < 2; ++turn) {
+            for (int64_t col = threadIdx.x * 8; col < cols; col += 8192) {
+                float g[8], v[8], w[8];
+                inputs8<DT, WIDE>(p, row, col, mean, g, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = 1.0f;
+                if (p.weight) params8(p.weight, p.param_dtype, col, cols, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[i] = col + i < cols ? v[i] * rstd : 0.0f;
+                    g[i] *= w[i];
+                    if (turn == 0) { sum_g += g[i]; sum_gx = fmaf(g[i], v[i], sum_gx); }
+                    else v[i] = rstd * fmaf(-v[i], sum_gx, g[i] - sum_g);
+                }
+                if (turn == 1) store8<DT, WIDE>((T *)p.dx + row * p.ld_dx, col, cols, v);
+            }
+            if (turn == 0) { r.sum2(sum_g, sum_gx); sum_g *= per; sum_gx *= per; }
+        }
+    }
+}
+
+// Sums for dw and db where rows are too long for a workgroup's registers: eight columns per thread, every kStrips-th row.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void norm_long_params_kernel(NormArgs p)
+{
+    const int64_t cols = p.cols, col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (col >= cols) return;
+    float dw[8] = {}, db[8] = {};
+    for (int64_t row = blockIdx.y; row < p.rows; row += gridDim.y) {
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float g[8], v[8];
+        inputs8<DT, WIDE>(p, row, col, mean, g, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { dw[i] = fmaf(g[i], v[i] * rstd, dw[i]); db[i] += g[i]; }
+    }
+    float *part = (float *)p.workspace + (int64_t)blockIdx.y * 2 * cols;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (col + i < cols) { part[col + i] = dw[i]; part[cols + col + i] = db[i]; }
+}
+
+// Adds up the strips, [strips][2][cols]: 64 columns per workgroup, sixteen waves take a sixteenth of the strips each.
+__global__ __launch_bounds__(1024) void norm_params_kernel(int32_t strips, int64_t cols, const float *part, void *dweight, void *dbias, int32_t dt)
+{
+    __shared__ float sums[16][64];
+    const int64_t at = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    const int wave = threadIdx.x >> 6, per = (strips + 15) / 16;
+    float sum = 0.0f;
+    if (at < 2 * cols)
+        for (int k = wave * per; k < min(strips, (wave + 1) * per); ++k) sum += part[(int64_t)k * 2 * cols + at];
+    sums[wave][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (wave || at >= 2 * cols) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += sums[k][threadIdx.x & 63];
+    if (at < cols) {
+        if (dweight) put_param(dweight, dt, at, sum);
+    } else if (dbias) {
+        put_param(dbias, dt, at - cols, sum);
+    }
+}
+
+// ---- launches ----
+static unsigned few(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
+
+template <int DT, bool WIDE>
+static hipError_t forward(const NormArgs &p, hipStream_t s)
+{
+    const int64_t c = p.cols;
+    // four rows' worth of workgroups per compute unit (of 256) stay for all rows
+    if (c <= 512) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 1>), dim3(few((p.rows + 3) / 4, 2048)), dim3(256), 0, s, p);
+    else if (c <= 1024) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 2>), dim3(few((p.rows + 3) / 4, 2048)), dim3(256), 0, s, p);
+    else if (c <= 2048) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 1>), dim3(few(p.rows, 2048)), dim3(256), 0, s, p);
+    else if (c <= 4096) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 2>), dim3(few(p.rows, 2048)), dim3(256), 0, s, p);
+    else if (c <= 8192) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 4>), dim3(few(p.rows, 1024)), dim3(256), 0, s, p);
+    else if (c <= kLongest) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 1024, 2>), dim3(few(p.rows, 512)), dim3(1024), 0, s, p);
+    else hipLaunchKernelGGL((norm_long_kernel<DT, WIDE>), dim3(few(p.rows, 1 << 16)), dim3(1024), 0, s, p);
+    return hipGetLastError();
+}
+
+static int64_t strips_of(int64_t rows, int64_t cols)
+{
+    const int64_t blocks = cols <= 1024 ? (rows + 3) / 4 : rows;
+    return blocks < kStrips ? blocks : kStrips;
+}
+size_t layer_norm_backward_workspace(int64_t rows, int64_t cols) { return (size_t)strips_of(rows, cols) * 2 * cols * sizeof(float); }
+
+template <int DT, bool WIDE, bool SAVED>
+static void backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
+{
+    const int64_t c = p.cols;
+    if (c <= 512) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 64, 1>), dim3(strips), dim3(256), 0, s, p);
+    else if (c <= 1024) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 64, 2>), dim3(strips), dim3(256), 0, s, p);
+    else if (c <= 2048) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 256, 1>), dim3(strips), dim3(256), 0, s, p);
+    else if (c <= 4096) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 256, 2>), dim3(strips), dim3(256), 0, s, p);
+    else if (c <= 8192) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 256, 4>), dim3(strips), dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 1024, 2>), dim3(strips), dim3(1024), 0, s, p);
+}
+
+template <int DT, bool WIDE>
+static hipError_t backward(const NormArgs &p, hipStream_t s)
+{
+    const unsigned strips = (unsigned)strips_of(p.rows, p.cols);
+    if (!strips) {                                              // (no rows: the sums are zero)
+    } else if (p.cols > kLongest) {
+        if (p.dx) hipLaunchKernelGGL((norm_long_dx_kernel<DT, WIDE>), dim3(few(p.rows, 1 << 16)), dim3(1024), 0, s, p);
+        if (p.workspace) hipLaunchKernelGGL((norm_long_params_kernel<DT, WIDE>), dim3((unsigned)((p.cols + 2047) / 2048), strips), dim3(256), 0, s, p);
+    } else if (p.x) {
+        backward_rows<DT, WIDE, false>(p, strips, s);
+    } else {
+        backward_rows<DT, WIDE, true>(p, strips, s);
+    }
+    if (p.dweight || p.dbias)
+        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(1024), 0, s, (int32_t)strips, p.cols, (const float *)p.workspace, p.dweight, p.dbias, p.param_dtype);
+    return hipGetLastError();
+}
+
+#define BY_TYPE(dt, wide, f, ...)                                                                               \
+    ((dt) == TICTAC_F32    ? ((wide) ? f<TICTAC_F32, true>(__VA_ARGS__) : f<TICTAC_F32, false>(__VA_ARGS__))    \
+     : (dt) == TICTAC_F16  ? ((wide) ? f<TICTAC_F16, true>(__VA_ARGS__) : f<TICTAC_F16, false>(__VA_ARGS__))    \
+                           : ((wide) ? f<TICTAC_BF16, true>(__VA_ARGS__) : f<TICTAC_BF16, false>(__VA_ARGS__)))
+
+hipError_t launch_layer_norm(const NormArgs &p, hipStream_t s)
+{
+    const bool wide = wide_rows(p.x, p.dtype, p.ld_x, p.cols) && (!p.y || wide_rows(p.y, p.dtype, p.ld_y, p.cols));
+    return BY_TYPE(p.dtype, wide, forward, p, s);
+}
+
+hipError_t launch_layer_norm_backward(const NormArgs &p, hipStream_t s)
+{
+    const bool wide = (!p.x || wide_rows(p.x, p.dtype, p.ld_x, p.cols)) && wide_rows(p.dy, p.dtype, p.ld_dy, p.cols) &&
+                      (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols));
+    return BY_TYPE(p.dtype, wide, backward, p, s);
+}
+
+}  // namespace tictac

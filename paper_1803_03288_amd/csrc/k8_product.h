@@ -1,0 +1,34 @@
+// The tiled product behind the layers with 8-bit weights, forward and backward:
+//   out[c][r] = sum over k of P[r][k] Q[c][k]
+// P and Q have k contiguous and padded with zeros to whole steps of 128 bytes: 128 int8 or 64 bf16 values.  Both types take the same path
+// through LDS, sixteen bytes per lane, and differ in the matrix instruction alone.  r, along which the output is contiguous, is the row
+// index of the matrix instruction, so that a lane has four consecutive outputs.
+#pragma once
+
+#include "rows8.h"
+
+namespace tictac {
+
+struct ProductArgs {
+    const char *p, *q;
+    int64_t ld_p, ld_q;         // bytes
+    int32_t R, C;
+    int32_t steps;              // of 128 bytes, along q
+    int32_t p_steps;            // p starts again after so many: q holds `steps / p_steps` pieces side by side
+    int32_t splits;             // the steps are dealt to so many workgroups per tile, which leave sums in `parts`
+    void *out;
+    int64_t ld_out;
+    int32_t dtype;              // of out
+    // int8: out = sum * (q_scale[c] * p_scale[r]) + bias[r]; bf16: out = sum
+    const float *p_scale, *q_scale;
+    const void *bias;
+    int32_t bias_dtype;
+    void *parts;                // [splits][C][R], int32 or float32
+};
+
+int32_t product_splits(int32_t R, int32_t C, int32_t steps);
+inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
+hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_bf16(const ProductArgs &a, hipStream_t s);
+
+}  // namespace tictac
