@@ -1,5 +1,6 @@
 // See k8_product.h.  A workgroup has a tile of the output, its waves a part of that each; the operands come through LDS in steps of 128
 // bytes of k, two buffers in turn: while one is computed from, the next step is under way into the other, straight from memory to LDS.
+#include "device_utils.h"
 #include "k8_product.h"
 
 namespace tictac {
@@ -19,103 +20,170 @@ struct OpBf16 {
     }
 };
 
-__device__ __forceinline__ void put4(void *out, int dt, int64_t at, const float *v, int n)
-{
-    // (four outputs from `at` on; whole ones on an 8-byte boundary in one store)
-    if (dt == TICTAC_F32) {
-        float *o = (float *)out + at;
-        if (n == 4 && ((uintptr_t)o & 15) == 0) { *(f32x4 *)o = f32x4{v[0], v[1], v[2], v[3]}; return; }
-        for (int i = 0; i < n; ++i) o[i] = v[i];
-        return;
-    }
-    uint2 w;
-    if (dt == TICTAC_F16) {
-        const f16x2 a{(_Float16)v[0], (_Float16)v[1]}, b{(_Float16)v[2], (_Float16)v[3]};
-        w = uint2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)};
-    } else {
-        w = uint2{__builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2)),
-                  __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{v[2], v[3]}), bf16x2))};
-    }
-    uint16_t *o = (uint16_t *)out + at;
-    if (n == 4 && ((uintptr_t)o & 7) == 0) { *(uint2 *)o = w; return; }
-    for (int i = 0; i < n; ++i) o[i] = (uint16_t)((i < 2 ? w.x : w.y) >> (16 * (i & 1)));
-}
-
-// outputs r .. r + 3 of column c from their sums
-template <typename ACC>
-__device__ __forceinline__ void finish4(const ProductArgs &a, int32_t r, int32_t c, const ACC &sum)
-{
-    const int n = min(4, a.R - r);
-    float v[4];
+// ---- outputs ----
+// Eight outputs r .. r + 7 of a column from their sums.  The scales and the bias of r are the same for all columns of a thread.
+template <bool SCALED>
+struct Finish8 {
+    float scale[8], bias[8];
+    __device__ __forceinline__ void init(const ProductArgs &a, int32_t r)
+    {
+        if (!SCALED) return;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)sum[i];
-    if (a.p_scale) {
-        const float qs = a.q_scale[c];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i >= n) continue;
-            v[i] *= qs * a.p_scale[r + i];
-            if (a.bias) v[i] += param(a.bias, a.bias_dtype, r + i);
+        for (int i = 0; i < 8; ++i) {
+            scale[i] = r + i < a.R ? a.p_scale[r + i] : 0.0f;
+            bias[i] = a.bias && r + i < a.R ? param(a.bias, a.bias_dtype, r + i) : 0.0f;
         }
     }
-    put4(a.out, a.dtype, (int64_t)c * a.ld_out + r, v, n);
+    template <int DT>
+    __device__ __forceinline__ void store(const ProductArgs &a, int32_t r, int32_t c, const float *sum, bool wide) const
+    {
+        float v[8];
+        if (SCALED) {
+            const float qs = a.q_scale[c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = sum[i] * (qs * scale[i]) + bias[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = sum[i];
+        }
+        typename Elem<DT>::type *row = (typename Elem<DT>::type *)a.out + (int64_t)c * a.ld_out;
+        if (wide) store8<DT, true>(row, r, a.R, v);
+        else store8<DT, false>(row, r, a.R, v);
+    }
+};
+template <class OP>
+struct Scaled { static constexpr bool value = false; };
+template <>
+struct Scaled<OpI8> { static constexpr bool value = true; };
+
+constexpr int kParts = 3;           // in the place of an output type: sums of a split, as they are
+
+// What a wave holds, FR x FC blocks of 16 x 16 from (r, c) on, goes column by column through its own part of LDS, so that a thread has eight
+// consecutive outputs.  Lane l of a block holds rows 4 (l / 16) .. + 3 of column l % 16.
+template <class OP, int OUT, int FR, int FC>
+__device__ __forceinline__ void put_blocks(const ProductArgs &a, const typename OP::acc (&acc)[FR][FC], int32_t r, int32_t c, int32_t split, char *room)
+{
+    typedef typename OP::acc A;
+    constexpr int kStride = FR * 16 + 4, kThreads = FR * 2, kColumns = 64 / kThreads;       // words; threads per column; columns at a time
+    const int lane = threadIdx.x & 63, part = lane % kThreads, first = lane / kThreads;
+    A *to = (A *)room + ((lane & 15) * kStride + (lane >> 4) * 4) / 4;
+    const A *from = (const A *)room + (first * kStride + part * 8) / 4;
+    const int32_t mine = r + part * 8;
+    Finish8<Scaled<OP>::value && OUT != kParts> finish;
+    finish.init(a, mine);
+    const bool wide = OUT != kParts && (a.ld_out * (OUT == TICTAC_F32 ? 4 : 2)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
+#pragma unroll
+    for (int j = 0; j < FC; ++j) {
+#pragma unroll
+        for (int i = 0; i < FR; ++i) to[i * 4] = acc[i][j];
+        wave_sync();
+#pragma unroll
+        for (int k = 0; k < 16 / kColumns; ++k) {
+            const A lo = from[k * kColumns * kStride / 4], hi = from[k * kColumns * kStride / 4 + 1];
+            const int32_t column = c + j * 16 + k * kColumns + first;
+            if (column >= a.C || mine >= a.R) continue;
+            if constexpr (OUT == kParts) {
+                A *out = (A *)((uint32_t *)a.parts + ((int64_t)split * a.C + column) * a.R + mine);
+                if (a.R % 8 == 0) {
+                    out[0] = lo;
+                    out[1] = hi;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const auto sum = e < 4 ? lo[e & 3] : hi[e & 3];         // (a bit cast of a vector's element itself takes its first element)
+                        if (mine + e < a.R) ((uint32_t *)out)[e] = __builtin_bit_cast(uint32_t, sum);
+                    }
+                }
+            } else {
+                float sum[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { sum[e] = (float)lo[e]; sum[4 + e] = (float)hi[e]; }
+                finish.template store<OUT>(a, mine, column, sum, wide);
+            }
+        }
+        wave_sync();
+    }
 }
 
-// TR x TC outputs per workgroup, WR x WC waves, FR x FC blocks of 16 x 16 per wave.
-template <class OP, int WR, int WC, int FR, int FC>
-__global__ __launch_bounds__(WR *WC * 64) void product_kernel(ProductArgs a, int32_t tiles_r, int32_t tiles_c)
+// ---- tiles ----
+// Workgroups go to the eight XCDs in turn; each XCD gets a run of consecutive tiles, and a run goes down eight columns of tiles side by side,
+// so that what an XCD's L2 holds is used again.
+__device__ __forceinline__ void tile_of(int32_t tiles_r, int32_t tiles_c, int32_t &split, int32_t &tr, int32_t &tc)
 {
-    constexpr int TR = WR * FR * 16, TC = WC * FC * 16, kWaves = WR * WC;
-    constexpr int LP = TR / 8 / kWaves, LQ = TC / 8 / kWaves;           // loads of 8 rows x 128 bytes per wave and step
-    extern __shared__ char lds[];                                       // [2][TR + TC][128]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the eight XCDs in turn; each XCD gets a run of consecutive tiles, and a run goes down eight columns of tiles
-    // side by side, so that what an XCD's L2 holds is used again.
     const int32_t tiles = tiles_r * tiles_c;
     int32_t at = blockIdx.x % tiles;
-    const int32_t split = blockIdx.x / tiles;
-    {
-        const int32_t xcd = at & 7, whole = tiles >> 3, more = tiles & 7;
-        at = xcd * whole + min(xcd, more) + (at >> 3);
-    }
+    split = blockIdx.x / tiles;
+    const int32_t xcd = at & 7, whole = tiles >> 3, more = tiles & 7;
+    at = xcd * whole + min(xcd, more) + (at >> 3);
     const int32_t band = at / (8 * tiles_r), in_band = at - band * 8 * tiles_r, width = min(8, tiles_c - band * 8);
-    const int32_t r0 = in_band / width * TR, c0 = (band * 8 + in_band % width) * TC;
+    tr = in_band / width;
+    tc = band * 8 + in_band % width;
+}
 
-    const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
-    // A load brings 8 rows of 128 bytes, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i holds the
-    // bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.
-    const int lrow = lane >> 3, lcol = ((lane & 7) ^ lrow) * 16;
+// The loads of a tile.  A load brings 8 rows of 128 bytes to LDS, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i
+// holds the bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.  Rows behind the end are the last row again; nobody
+// stores what comes of them.
+template <int TR, int TC, int WAVES>
+struct TileLoads {
+    static constexpr int LP = TR / 8 / WAVES, LQ = TC / 8 / WAVES;      // per wave and step
     uint32_t off_p[LP], off_q[LQ];
+    const char *p, *q;
+    int32_t p_left;                     // steps until p starts again
+    __device__ __forceinline__ void init(const ProductArgs &a, int32_t r0, int32_t c0, int32_t first, int wave)
+    {
+        const int lane = threadIdx.x & 63, row = lane >> 3, col = ((lane & 7) ^ row) * 16;
 #pragma unroll
-    for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * kWaves + wave) * 8 + lrow) * (uint32_t)a.ld_p + lcol;
+        for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col;
 #pragma unroll
-    for (int i = 0; i < LQ; ++i) off_q[i] = (uint32_t)min(a.C - 1 - c0, (i * kWaves + wave) * 8 + lrow) * (uint32_t)a.ld_q + lcol;
-    const char *base_p = a.p + (int64_t)r0 * a.ld_p, *base_q = a.q + (int64_t)c0 * a.ld_q;
-
-    auto request = [&](int32_t step, int buffer) {
-        char *to = lds + buffer * (TR + TC) * 128;
-        const char *p = base_p + (int64_t)(step % a.p_steps) * 128, *q = base_q + (int64_t)step * 128;
+        for (int i = 0; i < LQ; ++i) off_q[i] = (uint32_t)min(a.C - 1 - c0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_q + col;
+        const int32_t at = a.p_steps ? first % a.p_steps : 0;
+        p = a.p + (int64_t)r0 * a.ld_p + (int64_t)at * 128;
+        q = a.q + (int64_t)c0 * a.ld_q + (int64_t)first * 128;
+        p_left = a.p_steps - at;
+    }
+    // the next step, to `to`: [TR + TC][128]
+    __device__ __forceinline__ void request(const ProductArgs &a, char *to, int wave)
+    {
 #pragma unroll
         for (int i = 0; i < LP; ++i)
-            __builtin_amdgcn_global_load_lds((global_void *)(p + off_p[i]), (lds_void *)(to + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_void *)(p + off_p[i]), (lds_void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
 #pragma unroll
         for (int i = 0; i < LQ; ++i)
-            __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[i]), (lds_void *)(to + TR * 128 + (i * kWaves + wave) * 1024), 16, 0, 0);
-    };
+            __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[i]), (lds_void *)(to + TR * 128 + (i * WAVES + wave) * 1024), 16, 0, 0);
+        q += 128;
+        p += 128;
+        if (--p_left == 0) {
+            p_left = a.p_steps;
+            p -= (int64_t)a.p_steps * 128;
+        }
+    }
+};
 
-    const int wr = wave % WR, wc = wave / WR;
+// A tile of 32 FR x 32 FC outputs by four waves, several workgroups per compute unit.
+template <class OP, int OUT, int FR, int FC>
+__global__ __launch_bounds__(256) void product_kernel(ProductArgs a, int32_t tiles_r, int32_t tiles_c)
+{
+    constexpr int TR = FR * 32, TC = FC * 32;
+    extern __shared__ char lds[];                                       // [2][TR + TC][128]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int32_t split, tr, tc;
+    tile_of(tiles_r, tiles_c, split, tr, tc);
+    const int32_t r0 = tr * TR, c0 = tc * TC;
+    const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
+    TileLoads<TR, TC, 4> loads;
+    loads.init(a, r0, c0, first, wave);
+    const int wr = wave & 1, wc = wave >> 1;
     typename OP::acc acc[FR][FC];
 #pragma unroll
     for (int i = 0; i < FR; ++i)
 #pragma unroll
         for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
-
     const int frow = lane & 15, fk = lane >> 4;
-    if (first < last) request(first, 0);
+    if (first < last) loads.request(a, lds, wave);
     for (int32_t step = first; step < last; ++step) {
         const int buffer = (step - first) & 1;
         __syncthreads();                    // this step has come, and nobody reads the other buffer any more
-        if (step + 1 < last) request(step + 1, buffer ^ 1);
+        if (step + 1 < last) loads.request(a, lds + (buffer ^ 1) * (TR + TC) * 128, wave);
         const char *tp = lds + buffer * (TR + TC) * 128 + (wr * FR * 16 + frow) * 128;
         const char *tq = lds + buffer * (TR + TC) * 128 + TR * 128 + (wc * FC * 16 + frow) * 128;
 #pragma unroll
@@ -132,44 +200,95 @@ __global__ __launch_bounds__(WR *WC * 64) void product_kernel(ProductArgs a, int
                 for (int j = 0; j < FC; ++j) acc[i][j] = OP::mma(fp[i], fq[j], acc[i][j]);
         }
     }
-    // lane l of a block of 16 x 16 holds rows 4 (l / 16) .. + 3 of column l % 16
+    __syncthreads();
+    put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, lds + wave * 16 * (FR * 16 + 4) * 4);
+}
+
+// A tile of 256 x 256 outputs by eight waves, two per SIMD: while one of the two computes, the other reads its next operands from LDS.  The waves of the
+// second half run one slot behind (a barrier ends a slot); a step has four slots of reading and four of sixteen matrix instructions each.
+// Slots of step t, for the first half: 8t read, 8t + 1 compute, ...; for the second: 8t + 1 read, 8t + 2 compute, ...
+//   - The other buffer is free from slot 8t on: the second half's last reads of step t - 1 are over at the barrier behind slot 8t - 1
+//     (they are waited for before it).  So each wave asks for step t + 1 in its first reading slot of step t.
+//   - Step t + 1 is read from slot 8t + 8 on: every wave has waited for its loads at the end of slot 8t + 7.
+template <class OP, int OUT>
+__global__ __launch_bounds__(512, 2) void product_kernel_256(ProductArgs a, int32_t tiles_r, int32_t tiles_c)
+{
+    constexpr int TR = 256, TC = 256, FR = 8, FC = 4;
+    extern __shared__ char lds[];                                       // [2][TR + TC][128]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2;
+    int32_t split, tr, tc;
+    tile_of(tiles_r, tiles_c, split, tr, tc);
+    const int32_t r0 = tr * TR, c0 = tc * TC;
+    TileLoads<TR, TC, 8> loads;
+    loads.init(a, r0, c0, 0, wave);
+    const int wr = wave & 1, wc = wave >> 1;
+    typename OP::acc acc[FR][FC];
 #pragma unroll
-    for (int j = 0; j < FC; ++j) {
-        const int32_t c = c0 + (wc * FC + j) * 16 + frow;
-        if (c >= a.C) continue;
+    for (int i = 0; i < FR; ++i)
 #pragma unroll
-        for (int i = 0; i < FR; ++i) {
-            const int32_t r = r0 + (wr * FR + i) * 16 + fk * 4;
-            if (r >= a.R) continue;
-            if (a.splits == 1) {
-                finish4(a, r, c, acc[i][j]);
-            } else {
-                uint32_t *part = (uint32_t *)a.parts + ((int64_t)split * a.C + c) * a.R + r;
+        for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
+    const int frow = lane & 15, fk = lane >> 4;
+    if (a.steps) loads.request(a, lds, wave);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    if (half) __builtin_amdgcn_s_barrier();
+    for (int32_t step = 0; step < a.steps; ++step) {
+        char *const here = lds + (step & 1) * (TR + TC) * 128;
+        const char *tp = here + (wr * FR * 16 + frow) * 128, *tq = here + TR * 128 + (wc * FC * 16 + frow) * 128;
+        i32x4 fp[FR / 2], fq[FC];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const auto sum = acc[i][j][e];          // (a bit cast of a vector's element itself takes its first element)
-                    if (r + e < a.R) part[e] = __builtin_bit_cast(uint32_t, sum);
-                }
+        for (int slot = 0; slot < 4; ++slot) {
+            const int k = slot >> 1, at = (slot & 1) * (FR / 2), place = ((k * 4 + fk) ^ (frow & 7)) * 16;
+            if (at == 0) {
+#pragma unroll
+                for (int j = 0; j < FC; ++j) fq[j] = *(const i32x4 *)(tq + j * 2048 + place);
             }
+#pragma unroll
+            for (int i = 0; i < FR / 2; ++i) fp[i] = *(const i32x4 *)(tp + (at + i) * 2048 + place);
+            if (slot == 0 && step + 1 < a.steps) loads.request(a, lds + ((step & 1) ^ 1) * (TR + TC) * 128, wave);
+            if (slot == 3 && half) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < FR / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < FC; ++j) acc[at + i][j] = OP::mma(fp[i], fq[j], acc[at + i][j]);
+            __builtin_amdgcn_s_setprio(0);
+            if (slot == 3 && !half) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
+    if (!half) __builtin_amdgcn_s_barrier();
+    __syncthreads();
+    put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, 0, lds + wave * 16 * (FR * 16 + 4) * 4);
 }
 
 // Adds up the splits in their order.
-template <class OP>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_t quads)
+template <class OP, int OUT>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_t eights)
 {
     const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)quads * a.C) return;
-    const int32_t c = (int32_t)(at / quads), r = (int32_t)(at % quads) * 4;
-    typename OP::acc sum{};
+    if (at >= (int64_t)eights * a.C) return;
+    const int32_t c = (int32_t)(at / eights), r = (int32_t)(at % eights) * 8;
+    typedef typename std::remove_reference<decltype(typename OP::acc{}[0] + typename OP::acc{}[0])>::type N;
+    N sum[8] = {};
     for (int32_t k = 0; k < a.splits; ++k) {
-        const uint32_t *part = (const uint32_t *)a.parts + ((int64_t)k * a.C + c) * a.R + r;
+        const N *part = (const N *)a.parts + ((int64_t)k * a.C + c) * a.R + r;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (r + e < a.R) sum[e] += __builtin_bit_cast(typename std::remove_reference<decltype(sum[0] + sum[0])>::type, part[e]);
+        for (int e = 0; e < 8; ++e)
+            if (r + e < a.R) sum[e] += part[e];
     }
-    finish4(a, r, c, sum);
+    Finish8<Scaled<OP>::value> finish;
+    finish.init(a, r);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)sum[e];
+    finish.template store<OUT>(a, r, c, v, (a.ld_out * (OUT == TICTAC_F32 ? 4 : 2)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0);
 }
 
 constexpr int32_t kSmallTile = 128;
@@ -183,28 +302,35 @@ int32_t product_splits(int32_t R, int32_t C, int32_t steps)
     return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
 }
 
-template <class OP>
-static hipError_t launch(const ProductArgs &a, hipStream_t s)
+template <class OP, int OUT>
+static hipError_t launch_as(const ProductArgs &a, hipStream_t s)
 {
-    if (a.R == 0 || a.C == 0) return hipSuccess;
     const int64_t big = (int64_t)((a.R + 255) / 256) * ((a.C + 255) / 256);
     if (a.splits == 1 && big >= 192) {
         constexpr int lds = 2 * 512 * 128;
-        const auto kernel = product_kernel<OP, 2, 4, 8, 4>;
+        const auto kernel = product_kernel_256<OP, OUT>;
         if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
         hipLaunchKernelGGL(kernel, dim3((unsigned)big), dim3(512), lds, s, a, (a.R + 255) / 256, (a.C + 255) / 256);
         return hipGetLastError();
     }
     constexpr int lds = 2 * 256 * 128;
     const int32_t tr = (a.R + kSmallTile - 1) / kSmallTile, tc = (a.C + kSmallTile - 1) / kSmallTile;
-    const auto kernel = product_kernel<OP, 2, 2, 4, 4>;
+    const auto kernel = a.splits > 1 ? product_kernel<OP, kParts, 4, 4> : product_kernel<OP, OUT, 4, 4>;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tr * tc * a.splits), dim3(256), lds, s, a, tr, tc);
     if (a.splits > 1) {
-        const int32_t quads = (a.R + 3) / 4;
-        hipLaunchKernelGGL((product_join_kernel<OP>), dim3((unsigned)(((int64_t)quads * a.C + 255) / 256)), dim3(256), 0, s, a, quads);
+        const int32_t eights = (a.R + 7) / 8;
+        hipLaunchKernelGGL((product_join_kernel<OP, OUT>), dim3((unsigned)(((int64_t)eights * a.C + 255) / 256)), dim3(256), 0, s, a, eights);
     }
     return hipGetLastError();
+}
+
+template <class OP>
+static hipError_t launch(const ProductArgs &a, hipStream_t s)
+{
+    if (a.R == 0 || a.C == 0) return hipSuccess;
+    if (a.dtype == TICTAC_F32) return launch_as<OP, TICTAC_F32>(a, s);
+    return a.dtype == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, s) : launch_as<OP, TICTAC_BF16>(a, s);
 }
 
 hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s) { return launch<OpI8>(a, s); }
