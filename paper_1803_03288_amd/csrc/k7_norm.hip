@@ -489,11 +489,6 @@ static hipError_t backward(const NormArgs &p, hipStream_t s)
     return hipGetLastError();
 }
 
-#define BY_TYPE(dt, wide, f, ...)                                                                               \
-    ((dt) == TICTAC_F32    ? ((wide) ? f<TICTAC_F32, true>(__VA_ARGS__) : f<TICTAC_F32, false>(__VA_ARGS__))    \
-     : (dt) == TICTAC_F16  ? ((wide) ? f<TICTAC_F16, true>(__VA_ARGS__) : f<TICTAC_F16, false>(__VA_ARGS__))    \
-                           : ((wide) ? f<TICTAC_BF16, true>(__VA_ARGS__) : f<TICTAC_BF16, false>(__VA_ARGS__)))
-
 hipError_t launch_layer_norm(const NormArgs &p, hipStream_t s)
 {
     const bool wide = wide_rows(p.x, p.dtype, p.ld_x, p.cols) && (!p.y || wide_rows(p.y, p.dtype, p.ld_y, p.cols));

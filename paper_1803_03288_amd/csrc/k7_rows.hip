@@ -44,16 +44,16 @@ __global__ __launch_bounds__(256) void quantize_groups_kernel(QuantizeArgs p, in
 }
 
 // A scale per row, a workgroup per row: the row is read twice, the second time from the caches.
-template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs p)
+template <int DT, bool WIDE, int THREADS>
+__global__ __launch_bounds__(THREADS) void quantize_rows_kernel(QuantizeArgs p)
 {
     using E = Elem<DT>;
-    __shared__ uint32_t part[4];
+    __shared__ uint32_t part[THREADS / 64];
     const int64_t padded = (p.cols + 127) / 128 * 128;
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const typename E::type *x = (const typename E::type *)p.x + row * p.ld_x;
         uint32_t m = 0;
-        for (int64_t col = threadIdx.x * 8; col < p.cols; col += 2048) {
+        for (int64_t col = threadIdx.x * 8; col < p.cols; col += THREADS * 8) {
             float v[8];
             E::floats(load8<DT, WIDE>(x, col, p.cols), v);
 #pragma unroll
@@ -62,9 +62,12 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs p)
         m = wave_max_u32(m);
         if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
         __syncthreads();
-        const RowScale s = row_scale(max(max(part[0], part[1]), max(part[2], part[3])));
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < THREADS / 64; ++i) m = max(m, part[i]);
+        const RowScale s = row_scale(m);
         __syncthreads();
-        for (int64_t col = threadIdx.x * 8; col < padded; col += 2048) {
+        for (int64_t col = threadIdx.x * 8; col < padded; col += THREADS * 8) {
             float v[8];
             E::floats(load8<DT, WIDE>(x, col, p.cols), v);
             *(uint2 *)(p.q + row * p.ld_q + col) = quantized8(v, s);
@@ -113,7 +116,10 @@ static hipError_t quantize(const QuantizeArgs &p, hipStream_t s)
         const int64_t groups = (p.cols + 127) / 128, total = groups * p.rows;
         hipLaunchKernelGGL((quantize_groups_kernel<DT, WIDE>), dim3(elementwise_blocks((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, groups, total);
     } else {
-        hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE>), dim3((unsigned)(p.rows < (1 << 20) ? p.rows : (1 << 20))), dim3(256), 0, s, p);
+        const dim3 grid((unsigned)(p.rows < (1 << 20) ? p.rows : (1 << 20)));
+        // few long rows leave most of the chip idle: as many loads under way as a workgroup can have
+        if (p.rows <= 512 && p.cols > 2048) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 1024>), grid, dim3(1024), 0, s, p);
+        else hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 256>), grid, dim3(256), 0, s, p);
     }
     return hipGetLastError();
 }
@@ -126,11 +132,6 @@ static hipError_t dequantize(const QuantizeArgs &p, hipStream_t s)
                        p.group ? (p.cols + 127) / 128 : (int64_t)1);
     return hipGetLastError();
 }
-
-#define BY_TYPE(dt, wide, f, ...)                                                                               \
-    ((dt) == TICTAC_F32    ? ((wide) ? f<TICTAC_F32, true>(__VA_ARGS__) : f<TICTAC_F32, false>(__VA_ARGS__))    \
-     : (dt) == TICTAC_F16  ? ((wide) ? f<TICTAC_F16, true>(__VA_ARGS__) : f<TICTAC_F16, false>(__VA_ARGS__))    \
-                           : ((wide) ? f<TICTAC_BF16, true>(__VA_ARGS__) : f<TICTAC_BF16, false>(__VA_ARGS__)))
 
 hipError_t launch_quantize_rows(const QuantizeArgs &p, hipStream_t s)
 {

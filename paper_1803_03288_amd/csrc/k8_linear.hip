@@ -8,72 +8,195 @@
 namespace tictac {
 
 // ---- few rows: bound by the bytes of the weights ----
-// A workgroup has 16 outputs, its eight waves an eighth of k each: weights go from memory to the matrix instruction without LDS, sixteen bytes per
-// lane, eight loads under way.  TB blocks of 16 rows of x.  The sums of the waves meet in LDS.
+// A workgroup has 16 FB outputs and a part of k, its eight waves an eighth of that each: weights go from memory to the matrix instruction without
+// LDS, sixteen bytes per lane, the next unit of 128 bytes under way while one is computed.  TB blocks of 16 rows of x come from the caches.  The
+// sums of the waves meet in LDS, those of several workgroups along k in the workspace.
+// Alone the weights of 4096 x 25088 stream at 5.1 TB/s (20 us).  Through the L2 go 7.4 TB/s in all, so x, read again for each 16 FB outputs, has to
+// stay well below the weights: rows / (16 FB) of their bytes.  32 rows with FB = 1: 41 us.
 constexpr int kFewWaves = 8;
 
-template <int TB>
-__global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs p, const int8_t *xq, int64_t ld_xq, const float *xs)
+template <int TB, int FB>
+__global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs p, const int8_t *xq, int64_t ld_xq, const float *xs, int32_t splits, int32_t *parts)
 {
     __shared__ i32x4 sums[kFewWaves][TB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, fk = (lane >> 4) * 16;
-    const int64_t o0 = (int64_t)blockIdx.x * 16;
-    const int32_t units = (int32_t)((p.cols + 127) / 128);
-    const int8_t *w = p.w + min(o0 + row, p.outs - 1) * p.ld_w + fk;
-    const int8_t *x[TB];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 16;
+    const int64_t blocks = gridDim.x / splits, o0 = blockIdx.x % blocks * (16 * FB);
+    const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.cols + 127) / 128);
+    const int32_t first = (int32_t)((int64_t)all * split / splits), units = (int32_t)((int64_t)all * (split + 1) / splits);
+    const int8_t *w[FB], *x[TB];
+#pragma unroll
+    for (int f = 0; f < FB; ++f) w[f] = p.w + min(o0 + f * 16 + row, p.outs - 1) * p.ld_w + fk;
 #pragma unroll
     for (int b = 0; b < TB; ++b) x[b] = xq + min((int64_t)b * 16 + row, p.rows - 1) * ld_xq + fk;
-    i32x4 acc[TB];
+    i32x4 acc[FB][TB] = {}, now[FB][2], next[FB][2];
+    const auto request = [&](int32_t u) {
 #pragma unroll
-    for (int b = 0; b < TB; ++b) acc[b] = i32x4{};
-    int32_t u = wave;
-    for (; u + 3 * kFewWaves < units; u += 4 * kFewWaves) {
-        i32x4 fw[8];
+        for (int f = 0; f < FB; ++f)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) fw[k] = __builtin_nontemporal_load((const i32x4 *)(w + (int64_t)(u + (k >> 1) * kFewWaves) * 128 + (k & 1) * 64));
+            for (int k = 0; k < 2; ++k) next[f][k] = *(const i32x4 *)(w[f] + (int64_t)u * 128 + k * 64);
+    };
+    if (first + wave < units) request(first + wave);
+    for (int32_t u = first + wave; u < units; u += kFewWaves) {
+        i32x4 fx[2][TB];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int b = 0; b < TB; ++b)
-                acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw[k], *(const i32x4 *)(x[b] + (int64_t)(u + (k >> 1) * kFewWaves) * 128 + (k & 1) * 64), acc[b], 0, 0, 0);
+            for (int b = 0; b < TB; ++b) fx[k][b] = *(const i32x4 *)(x[b] + (int64_t)u * 128 + k * 64);
+#pragma unroll
+        for (int f = 0; f < FB; ++f)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) now[f][k] = next[f][k];
+        if (u + kFewWaves < units) request(u + kFewWaves);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int f = 0; f < FB; ++f)
+#pragma unroll
+                for (int b = 0; b < TB; ++b) acc[f][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[f][k], fx[k][b], acc[f][b], 0, 0, 0);
     }
-    for (; u < units; u += kFewWaves)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const i32x4 fw = *(const i32x4 *)(w + (int64_t)u * 128 + k * 64);
+    for (int f = 0; f < FB; ++f) {
+        if (f) __syncthreads();
 #pragma unroll
-            for (int b = 0; b < TB; ++b)
-                acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fw, *(const i32x4 *)(x[b] + (int64_t)u * 128 + k * 64), acc[b], 0, 0, 0);
+        for (int b = 0; b < TB; ++b) sums[wave][b][lane] = acc[f][b];
+        __syncthreads();
+        // lane l of a block holds outputs 4 (l / 16) .. + 3 of row l % 16; a thread finishes one output
+        for (int i = threadIdx.x; i < TB * 256; i += kFewWaves * 64) {
+            const int b = i >> 8, o = i & 15, t = (i >> 4) & 15;
+            int32_t sum = 0;
+#pragma unroll
+            for (int k = 0; k < kFewWaves; ++k) sum += sums[k][b][(o >> 2) * 16 + t][o & 3];
+            const int64_t at = (int64_t)b * 16 + t, out = o0 + f * 16 + o;
+            if (at >= p.rows || out >= p.outs) continue;
+            if (splits > 1) {
+                parts[((int64_t)split * p.rows + at) * p.outs + out] = sum;
+                continue;
+            }
+            float v = (float)sum * (xs[at] * p.ws[out]);
+            if (p.bias) v += param(p.bias, p.bias_dtype, out);
+            put_param(p.y, p.dtype, at * p.ld_y + out, v);
         }
-#pragma unroll
-    for (int b = 0; b < TB; ++b) sums[wave][b][lane] = acc[b];
-    __syncthreads();
-    // lane l of a block holds outputs 4 (l / 16) .. + 3 of row l % 16; a thread finishes one output
-    for (int i = threadIdx.x; i < TB * 256; i += kFewWaves * 64) {
-        const int b = i >> 8, o = i & 15, t = (i >> 4) & 15;
-        int32_t sum = 0;
-#pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) sum += sums[k][b][(o >> 2) * 16 + t][o & 3];
-        const int64_t at = (int64_t)b * 16 + t;
-        if (at >= p.rows || o0 + o >= p.outs) continue;
-        float v = (float)sum * (xs[at] * p.ws[o0 + o]);
-        if (p.bias) v += param(p.bias, p.bias_dtype, o0 + o);
-        put_param(p.y, p.dtype, at * p.ld_y + o0 + o, v);
     }
 }
 
-constexpr int64_t kFewRows = 64;
+// Up to eight rows of floats, rounded to 8 bits here: every workgroup takes the largest magnitudes of the rows again (they come from the caches, under the
+// first loads of the weights), which costs less than a launch before it while all rows are at most 64 KB (kOnceBytes).  1 x 4096 x 4096: 6 us; two launches
+// take 2.6 and 5.5 us and what lies between them.  The 8-bit values are those of quantize_rows_kernel.
+constexpr int kOnceWaves = 16, kOnceRows = 8;
+constexpr int64_t kOnceBytes = 64 << 10;
 
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(kOnceWaves * 64) void linear_once_kernel(LinearArgs p)
+{
+    using E = Elem<DT>;
+    using T = typename E::type;
+    constexpr int kUnits = 2;                               // of weights under way
+    __shared__ uint32_t part[kOnceRows][kOnceWaves];
+    __shared__ i32x4 sums[kOnceWaves][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 16;
+    const int64_t o0 = (int64_t)blockIdx.x * 16;
+    const int32_t units = (int32_t)((p.cols + 127) / 128), rows = (int32_t)p.rows;
+    const int8_t *w = p.w + min(o0 + row, p.outs - 1) * p.ld_w + fk;
+    i32x4 next[kUnits][2];
+    const auto request = [&](int32_t u) {
+#pragma unroll
+        for (int n = 0; n < kUnits; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                next[n][k] = u + n * kOnceWaves < units ? *(const i32x4 *)(w + (int64_t)(u + n * kOnceWaves) * 128 + k * 64) : i32x4{};
+    };
+    request(wave);
+    for (int t = 0; t < rows; ++t) {
+        uint32_t m = 0;
+        for (int64_t col = threadIdx.x * 8; col < p.cols; col += kOnceWaves * 512) {
+            float v[8];
+            E::floats(load8<DT, WIDE>((const T *)p.x + t * p.ld_x, col, p.cols), v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+        }
+        m = wave_max_u32(m);
+        if (lane == 0) part[t][wave] = m;
+    }
+    __syncthreads();
+    const int mine = min(row, rows - 1);
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kOnceWaves; ++i) m = max(m, part[mine][i]);
+    const RowScale scale = row_scale(m);
+    const T *x = (const T *)p.x + mine * p.ld_x;
+    i32x4 acc{};
+    for (int32_t u = wave; u < units; u += kUnits * kOnceWaves) {
+        i32x4 now[kUnits][2], fx[kUnits][2];
+#pragma unroll
+        for (int n = 0; n < kUnits; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                now[n][k] = next[n][k];
+                const int64_t col = (int64_t)(u + n * kOnceWaves) * 128 + k * 64 + fk;
+                float v[16];
+                E::floats(load8<DT, WIDE>(x, col, p.cols), v);
+                E::floats(load8<DT, WIDE>(x, col + 8, p.cols), v + 8);
+                const uint2 lo = quantized8(v, scale), hi = quantized8(v + 8, scale);
+                fx[n][k] = i32x4{(int32_t)lo.x, (int32_t)lo.y, (int32_t)hi.x, (int32_t)hi.y};
+            }
+        request(u + kUnits * kOnceWaves);
+#pragma unroll
+        for (int n = 0; n < kUnits; ++n)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[n][k], fx[n][k], acc, 0, 0, 0);
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    const int o = threadIdx.x & 15, t = threadIdx.x >> 4;
+    if (t >= rows || o0 + o >= p.outs) return;
+    int32_t sum = 0;
+#pragma unroll
+    for (int k = 0; k < kOnceWaves; ++k) sum += sums[k][(o >> 2) * 16 + t][o & 3];
+    m = 0;
+#pragma unroll
+    for (int i = 0; i < kOnceWaves; ++i) m = max(m, part[t][i]);
+    float v = (float)sum * (row_scale(m).scale * p.ws[o0 + o]);
+    if (p.bias) v += param(p.bias, p.bias_dtype, o0 + o);
+    put_param(p.y, p.dtype, t * p.ld_y + o0 + o, v);
+}
+
+static bool once(const LinearArgs &p)
+{
+    return p.x && p.rows <= kOnceRows && p.rows * p.cols * (int64_t)elem_size(p.dtype) <= kOnceBytes;
+}
+
+template <int DT, bool WIDE>
+static hipError_t launch_once(const LinearArgs &p, hipStream_t s)
+{
+    hipLaunchKernelGGL((linear_once_kernel<DT, WIDE>), dim3((unsigned)((p.outs + 15) / 16)), dim3(kOnceWaves * 64), 0, s, p);
+    return hipGetLastError();
+}
+
+constexpr int64_t kFewRows = 64;
+static int32_t few_blocks_of(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }       // FB: x at most half of the weights' bytes, up to 32 rows
+static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
+{
+    const int64_t blocks = (outs + 16 * few_blocks_of(rows) - 1) / (16 * few_blocks_of(rows)), units = (cols + 127) / 128;
+    if (blocks == 0) return 1;
+    int64_t n = 256 / blocks;                           // a workgroup per compute unit
+    if (n > units / (2 * kFewWaves)) n = units / (2 * kFewWaves);       // two units for each wave at least
+    return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
+}
+
+static size_t forward_parts(int64_t rows, int64_t cols, int64_t outs, int32_t *splits)
+{
+    *splits = rows <= kFewRows ? few_splits(rows, cols, outs) : product_splits((int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128));
+    return product_parts_bytes(*splits, (int32_t)outs, (int32_t)rows);
+}
 size_t linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
-    size_t bytes = 0;
-    if (from_floats) bytes += (size_t)rows * rows8_stride(cols) + ((size_t)rows * 4 + 255) / 256 * 256;
-    if (rows > kFewRows) bytes += product_parts_bytes(product_splits((int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128)), (int32_t)outs, (int32_t)rows);
-    return bytes;
+    int32_t splits;
+    return (from_floats ? (size_t)rows * rows8_stride(cols) + ((size_t)rows * 4 + 255) / 256 * 256 : 0) + forward_parts(rows, cols, outs, &splits);
 }
 
 hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
 {
+    if (once(p)) return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), launch_once, p, s);
     const int8_t *xq = p.xq;
     const float *xs = p.xs;
     int64_t ld_xq = p.ld_xq;
@@ -89,23 +212,221 @@ hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
         xs = scale;
         room += (size_t)p.rows * ld_xq;
     }
-    if (p.rows <= kFewRows) {
-        const dim3 grid((unsigned)((p.outs + 15) / 16)), block(kFewWaves * 64);
-        if (p.rows <= 16) hipLaunchKernelGGL(linear_few_kernel<1>, grid, block, 0, s, p, xq, ld_xq, xs);
-        else if (p.rows <= 32) hipLaunchKernelGGL(linear_few_kernel<2>, grid, block, 0, s, p, xq, ld_xq, xs);
-        else hipLaunchKernelGGL(linear_few_kernel<4>, grid, block, 0, s, p, xq, ld_xq, xs);
-        return hipGetLastError();
-    }
     ProductArgs a{};
     a.p = (const char *)p.w; a.ld_p = p.ld_w;
     a.q = (const char *)xq; a.ld_q = ld_xq;
     a.R = (int32_t)p.outs; a.C = (int32_t)p.rows;
     a.steps = a.p_steps = (int32_t)(rows8_stride(p.cols) / 128);
-    a.splits = product_splits(a.R, a.C, a.steps);
     a.out = p.y; a.ld_out = p.ld_y; a.dtype = p.dtype;
     a.p_scale = p.ws; a.q_scale = xs; a.bias = p.bias; a.bias_dtype = p.bias_dtype;
     a.parts = room;
-    return launch_product_i8(a, s);
+    forward_parts(p.rows, p.cols, p.outs, &a.splits);
+    if (p.rows > kFewRows) return launch_product_i8(a, s);
+    const int32_t outs = 16 * few_blocks_of(p.rows);
+    const dim3 grid((unsigned)((p.outs + outs - 1) / outs * a.splits)), block(kFewWaves * 64);
+    const auto kernel = p.rows <= 8 ? linear_few_kernel<1, 1> : p.rows <= 16 ? linear_few_kernel<1, 2> : p.rows <= 32 ? linear_few_kernel<2, 4> : linear_few_kernel<4, 4>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, p, xq, ld_xq, xs, a.splits, (int32_t *)room);
+    return a.splits > 1 ? launch_product_join_i8(a, s) : hipGetLastError();
+}
+
+// dy times a scale in PIECES bf16 values that add up to it: all but the last cut off, which leaves the rest exact, the last rounded.  (An infinity
+// stays one, with nothing left.)
+template <int PIECES>
+__device__ __forceinline__ void cut(float v, uint16_t *piece)
+{
+#pragma unroll
+    for (int k = 0; k < PIECES - 1; ++k) {
+        const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+        piece[k] = (uint16_t)(high >> 16);
+        v = (high & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __builtin_bit_cast(float, high);
+    }
+    const __bf16 last = (__bf16)v;
+    piece[PIECES - 1] = __builtin_bit_cast(uint16_t, last);
+}
+__device__ __forceinline__ int32_t pair(uint16_t lo, uint16_t hi) { return lo | (int32_t)((uint32_t)hi << 16); }
+
+// Byte `b` of eight words as eight bf16 values (exact: eight bits).
+__device__ __forceinline__ i32x4 bytes_bf16(const int32_t *w, int b)
+{
+    uint32_t f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __builtin_bit_cast(uint32_t, (float)((w[e] << (24 - 8 * b)) >> 24));
+    i32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (int32_t)__builtin_amdgcn_perm(f[2 * e + 1], f[2 * e], 0x07060302);
+    return r;
+}
+__device__ __forceinline__ f32x4 mma_bf16(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+static int pieces_of(int32_t dtype) { return dtype == TICTAC_F32 ? 3 : dtype == TICTAC_F16 ? 2 : 1; }
+template <int DT>
+struct Pieces { static constexpr int value = DT == TICTAC_F32 ? 3 : DT == TICTAC_F16 ? 2 : 1; };
+
+// ---- backward with few rows: bound by the weights read for dx, and by dw written ----
+// dx: the weights have k (the outputs o) as rows, and the matrix instruction wants eight of k per lane.  A lane reads 4 ND bytes of each of eight
+// rows and turns this block of 8 x 4 ND round in registers: byte j of the eight words is an operand whose row r is the column
+// i = 4 ND r + j of the block, so 4 ND instructions take what one round of loads brought.  The result has, per lane, 4 ND columns next to each
+// other.  A workgroup has 64 ND columns and a part of k, its eight waves blocks of 32 of k in turn; their sums meet in LDS, in fixed order.
+constexpr int kBackWaves = 8;
+
+template <int DT, bool WIDE, int TB, int ND>
+__global__ __launch_bounds__(kBackWaves * 64) void linear_dx_few_kernel(LinearArgs p, int32_t splits, float *parts)
+{
+    using E = Elem<DT>;
+    using T = typename E::type;
+    constexpr int PIECES = Pieces<DT>::value, NJ = 4 * ND;
+    __shared__ f32x4 room[kBackWaves / 2][NJ][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int64_t blocks = gridDim.x / splits, i0 = blockIdx.x % blocks * (16 * NJ), padded = (p.cols + 127) / 128 * 128;
+    const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.outs + 31) / 32);
+    const int32_t first = (int32_t)((int64_t)all * split / splits), last = (int32_t)((int64_t)all * (split + 1) / splits);
+    const int8_t *w = p.w + (i0 + c * NJ < padded ? i0 + c * NJ : 0);           // (columns behind the end: any will do)
+    typedef int32_t Words __attribute__((ext_vector_type(ND)));
+    Words now[8], next[8];
+    const auto request = [&](int32_t kb) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) next[e] = *(const Words *)(w + min((int64_t)kb * 32 + g * 8 + e, p.outs - 1) * p.ld_w);
+    };
+    f32x4 acc[NJ][TB] = {};
+    if (first + wave < last) request(first + wave);
+    for (int32_t kb = first + wave; kb < last; kb += kBackWaves) {
+        const int64_t o = (int64_t)kb * 32 + g * 8;
+        float scale[8];
+        params8(p.ws, TICTAC_F32, o, p.outs, scale);
+        i32x4 q[TB][PIECES];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+            float v[8];
+            uint16_t cuts[8][PIECES];
+            E::floats(load8<DT, WIDE>((const T *)p.dy + min((int64_t)b * 16 + c, p.rows - 1) * p.ld_dy, o, p.outs), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cut<PIECES>(v[e] * scale[e], cuts[e]);
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) q[b][k][e] = pair(cuts[2 * e][k], cuts[2 * e + 1][k]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) now[e] = next[e];
+        if (kb + kBackWaves < last) request(kb + kBackWaves);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            int32_t words[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) words[e] = now[e][j >> 2];
+            const i32x4 f = bytes_bf16(words, j & 3);
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k) acc[j][b] = mma_bf16(f, q[b][k], acc[j][b]);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < TB; ++b)
+        for (int half = kBackWaves / 2; half; half >>= 1) {
+            if (wave >= half && wave < 2 * half)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) room[wave - half][j][lane] = acc[j][b];
+            __syncthreads();
+            if (wave < half)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[j][b] += room[wave][j][lane];
+            __syncthreads();
+        }
+    if (wave) return;
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+        const int64_t t = b * 16 + c;
+        if (t >= p.rows) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t i = i0 + NJ * (4 * g + e);
+#pragma unroll
+            for (int h = 0; h < NJ / 8; ++h) {
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = acc[h * 8 + j][b][e];
+                if (splits > 1) {
+                    float *part = parts + ((int64_t)split * p.rows + t) * p.cols;
+                    if (p.cols % 8 == 0) store8<TICTAC_F32, true>(part, i + h * 8, p.cols, v);
+                    else store8<TICTAC_F32, false>(part, i + h * 8, p.cols, v);
+                } else if (WIDE) {
+                    store8<DT, true>((T *)p.dx + t * p.ld_dx, i + h * 8, p.cols, v);
+                } else {
+                    store8<DT, false>((T *)p.dx + t * p.ld_dx, i + h * 8, p.cols, v);
+                }
+            }
+        }
+    }
+}
+
+// dw: all of k (the rows t, up to 32 KB) is at hand.  The activations are turned round in registers as the weights above, four bytes per lane, and stay
+// there; the pieces of dy times scale lie in LDS.  A workgroup has 64 outputs and 512 columns, a wave 64 columns; a lane stores sixteen values
+// next to each other.  db rides along with the first columns.
+template <int DT, bool WIDE, int KB>
+__global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
+{
+    using E = Elem<DT>;
+    using T = typename E::type;
+    constexpr int PIECES = Pieces<DT>::value, kOuts = 64, kStride = KB * 32 * PIECES + 8;       // (sixteen bytes more: rows start in other banks)
+    __shared__ __align__(16) uint16_t q[kOuts * kStride];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int64_t o0 = (int64_t)blockIdx.y * kOuts, i0 = (int64_t)blockIdx.x * 512 + wave * 64;
+    const int o = threadIdx.x & 63;
+    for (int t = threadIdx.x >> 6; t < KB * 32; t += 8) {
+        uint16_t cuts[PIECES];
+        cut<PIECES>(t < p.rows && o0 + o < p.outs ? E::to_float(((const T *)p.dy)[t * p.ld_dy + o0 + o]) * p.xs[t] : 0.0f, cuts);
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) q[o * kStride + k * KB * 32 + t] = cuts[k];
+    }
+    if (p.db && blockIdx.x == 0 && threadIdx.x < kOuts && o0 + o < p.outs) {
+        float sum = 0.0f;
+        for (int64_t t = 0; t < p.rows; ++t) sum += E::to_float(((const T *)p.dy)[t * p.ld_dy + o0 + o]);
+        ((T *)p.db)[o0 + o] = E::from_float(sum);
+    }
+    __syncthreads();
+    if (!p.dw || i0 >= p.cols) return;
+    i32x4 f[KB][4];
+#pragma unroll
+    for (int b = 0; b < KB; ++b) {
+        int32_t words[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) words[e] = *(const int32_t *)(p.xq + min((int64_t)b * 32 + g * 8 + e, p.rows - 1) * p.ld_xq + i0 + c * 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[b][j] = bytes_bf16(words, j);
+    }
+#pragma unroll
+    for (int block = 0; block < kOuts / 16; ++block) {
+        f32x4 acc[4] = {};
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                const i32x4 fq = *(const i32x4 *)(q + (block * 16 + c) * kStride + k * KB * 32 + b * 32 + g * 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = mma_bf16(f[b][j], fq, acc[j]);
+            }
+        const int64_t out = o0 + block * 16 + c, i = i0 + 16 * g;
+        if (out >= p.outs) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) v[n] = acc[n & 3][h * 2 + (n >> 2)];
+            store8<DT, WIDE>((T *)p.dw + out * p.ld_dw, i + h * 8, p.cols, v);
+        }
+    }
+}
+
+static int32_t dx_few_words(int64_t rows) { return rows <= 32 ? 4 : 2; }
+static int32_t dx_few_splits(int64_t rows, int64_t cols, int64_t outs)
+{
+    const int64_t wide = 64 * dx_few_words(rows), blocks = (cols + wide - 1) / wide, units = (outs + 31) / 32;
+    int64_t n = 256 / blocks;                                           // a workgroup per compute unit
+    if (n > units / (2 * kBackWaves)) n = units / (2 * kBackWaves);     // two blocks of k for each wave at least
+    return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
 }
 
 // ---- backward: operands with k contiguous ----
@@ -137,20 +458,6 @@ __global__ __launch_bounds__(256) void transpose_rows8_kernel(int64_t rows, int6
             w[i] = tile[r + h * 8 + 2 * i][threadIdx.x >> 2] | (uint32_t)tile[r + h * 8 + 2 * i + 1][threadIdx.x >> 2] << 16;
         *(i32x4 *)(out + c * padded + r0 + r + h * 8) = w;
     }
-}
-
-// dy times a scale in PIECES bf16 values that add up to it: all but the last cut off, which leaves the rest exact, the last rounded.
-template <int PIECES>
-__device__ __forceinline__ void cut(float v, uint16_t *piece)
-{
-#pragma unroll
-    for (int k = 0; k < PIECES - 1; ++k) {
-        const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
-        piece[k] = (uint16_t)(high >> 16);
-        v -= __builtin_bit_cast(float, high);
-    }
-    const __bf16 last = (__bf16)v;
-    piece[PIECES - 1] = __builtin_bit_cast(uint16_t, last);
 }
 
 // out[t][piece][o] = pieces of dy[t][o] ws[o], zeros for o from `outs` to `padded`
@@ -238,8 +545,6 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(int64_t parts, int64_
     put_param(db, dt, o, sum);
 }
 
-static int pieces_of(int32_t dtype) { return dtype == TICTAC_F32 ? 3 : dtype == TICTAC_F16 ? 2 : 1; }
-
 // The workspace of one backward call; the two products come one after the other and use the same room.
 struct BackwardRoom {
     int64_t padded_o, padded_t;
@@ -250,6 +555,10 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const int pieces = pieces_of(dtype);
     BackwardRoom r{};
+    if (rows <= kFewRows) {
+        r.bytes = up(product_parts_bytes(dx_few_splits(rows, cols, outs), (int32_t)cols, (int32_t)rows));
+        return r;
+    }
     r.padded_o = (outs + 63) / 64 * 64;
     r.padded_t = (rows + 63) / 64 * 64;
     r.sums = 0;
@@ -264,6 +573,27 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     return r;
 }
 size_t linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs) { return backward_room(dtype, rows, cols, outs).bytes; }
+
+template <int DT, bool WIDE>
+static hipError_t backward_few(const LinearArgs &p, hipStream_t s)
+{
+    if (p.dx && p.rows) {
+        const int32_t splits = dx_few_splits(p.rows, p.cols, p.outs), wide = 64 * dx_few_words(p.rows);
+        const auto kernel = p.rows <= 16 ? linear_dx_few_kernel<DT, WIDE, 1, 4> : p.rows <= 32 ? linear_dx_few_kernel<DT, WIDE, 2, 4> : linear_dx_few_kernel<DT, WIDE, 4, 2>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.cols + wide - 1) / wide * splits)), dim3(kBackWaves * 64), 0, s, p, splits, (float *)p.workspace);
+        if (splits > 1) {
+            ProductArgs a{};
+            a.R = (int32_t)p.cols; a.C = (int32_t)p.rows; a.splits = splits; a.out = p.dx; a.ld_out = p.ld_dx; a.dtype = DT; a.parts = p.workspace;
+            if (const hipError_t e = launch_product_join_bf16(a, s); e != hipSuccess) return e;
+        }
+    }
+    if ((p.dw || p.db) && p.outs) {
+        const dim3 grid((unsigned)(p.dw ? (p.cols + 511) / 512 : 1), (unsigned)((p.outs + 63) / 64));
+        const auto kernel = p.rows <= 32 ? linear_dw_few_kernel<DT, WIDE, 1> : linear_dw_few_kernel<DT, WIDE, 2>;
+        hipLaunchKernelGGL(kernel, grid, dim3(512), 0, s, p);
+    }
+    return hipGetLastError();
+}
 
 template <int DT, int PIECES>
 static hipError_t backward(const LinearArgs &p, hipStream_t s)
@@ -320,6 +650,10 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
 
 hipError_t launch_linear_q8_backward(const LinearArgs &p, hipStream_t s)
 {
+    if (p.rows > 0 && p.outs > 0 && p.rows <= kFewRows) {
+        const bool wide = wide_rows(p.dy, p.dtype, p.ld_dy, p.outs) && (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols)) && (!p.dw || wide_rows(p.dw, p.dtype, p.ld_dw, p.cols));
+        return BY_TYPE(p.dtype, wide, backward_few, p, s);
+    }
     if (p.dtype == TICTAC_F32) return backward<TICTAC_F32, 3>(p, s);
     return p.dtype == TICTAC_F16 ? backward<TICTAC_F16, 2>(p, s) : backward<TICTAC_BF16, 1>(p, s);
 }

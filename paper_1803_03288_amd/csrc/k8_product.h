@@ -29,6 +29,8 @@ struct ProductArgs {
 int32_t product_splits(int32_t R, int32_t C, int32_t steps);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
 hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s);        // the sums in `parts` to the output
+hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s);
 hipError_t launch_product_bf16(const ProductArgs &a, hipStream_t s);
 
 }  // namespace tictac

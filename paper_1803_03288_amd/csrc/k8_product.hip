@@ -268,27 +268,47 @@ __global__ __launch_bounds__(512, 2) void product_kernel_256(ProductArgs a, int3
     put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, 0, lds + wave * 16 * (FR * 16 + 4) * 4);
 }
 
-// Adds up the splits in their order.
-template <class OP, int OUT>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_t eights)
+// Adds up the splits in their order, four outputs per thread (one where rows of the sums do not start on 16-byte boundaries), the loads of
+// four splits under way.
+template <class OP, int OUT, int VEC>
+__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_t pieces)
 {
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= (int64_t)eights * a.C) return;
-    const int32_t c = (int32_t)(at / eights), r = (int32_t)(at % eights) * 8;
     typedef typename std::remove_reference<decltype(typename OP::acc{}[0] + typename OP::acc{}[0])>::type N;
-    N sum[8] = {};
-    for (int32_t k = 0; k < a.splits; ++k) {
-        const N *part = (const N *)a.parts + ((int64_t)k * a.C + c) * a.R + r;
+    typedef N NV __attribute__((ext_vector_type(VEC)));
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= (int64_t)pieces * a.C) return;
+    const int32_t c = (int32_t)(at / pieces), r = (int32_t)(at % pieces) * VEC;
+    const NV *part = (const NV *)((const N *)a.parts + (int64_t)c * a.R + r);
+    const int64_t step = (int64_t)a.C * a.R / VEC;
+    NV sum = {};
+    int32_t k = 0;
+    for (; k + 4 <= a.splits; k += 4) {
+        NV v[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (r + e < a.R) sum[e] += part[e];
+        for (int i = 0; i < 4; ++i) v[i] = part[(k + i) * step];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += v[i];
     }
-    Finish8<Scaled<OP>::value> finish;
-    finish.init(a, r);
-    float v[8];
+    for (; k < a.splits; ++k) sum += part[k * step];
+    typename Elem<OUT>::type *out = (typename Elem<OUT>::type *)a.out + (int64_t)c * a.ld_out + r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)sum[e];
-    finish.template store<OUT>(a, r, c, v, (a.ld_out * (OUT == TICTAC_F32 ? 4 : 2)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0);
+    for (int i = 0; i < VEC; ++i) {
+        float v = (float)sum[i];
+        if (Scaled<OP>::value) {
+            v *= a.q_scale[c] * a.p_scale[r + i];
+            if (a.bias) v += param(a.bias, a.bias_dtype, r + i);
+        }
+        out[i] = Elem<OUT>::from_float(v);
+    }
+}
+
+template <class OP, int OUT>
+static hipError_t join_as(const ProductArgs &a, hipStream_t s)
+{
+    const int32_t vec = a.R % 4 ? 1 : 4, pieces = a.R / vec;
+    const auto kernel = vec == 4 ? product_join_kernel<OP, OUT, 4> : product_join_kernel<OP, OUT, 1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(((int64_t)pieces * a.C + 255) / 256)), dim3(256), 0, s, a, pieces);
+    return hipGetLastError();
 }
 
 constexpr int32_t kSmallTile = 128;
@@ -318,11 +338,7 @@ static hipError_t launch_as(const ProductArgs &a, hipStream_t s)
     const auto kernel = a.splits > 1 ? product_kernel<OP, kParts, 4, 4> : product_kernel<OP, OUT, 4, 4>;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tr * tc * a.splits), dim3(256), lds, s, a, tr, tc);
-    if (a.splits > 1) {
-        const int32_t eights = (a.R + 7) / 8;
-        hipLaunchKernelGGL((product_join_kernel<OP, OUT>), dim3((unsigned)(((int64_t)eights * a.C + 255) / 256)), dim3(256), 0, s, a, eights);
-    }
-    return hipGetLastError();
+    return a.splits > 1 ? join_as<OP, OUT>(a, s) : hipGetLastError();
 }
 
 template <class OP>
@@ -333,6 +349,15 @@ static hipError_t launch(const ProductArgs &a, hipStream_t s)
     return a.dtype == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, s) : launch_as<OP, TICTAC_BF16>(a, s);
 }
 
+template <class OP>
+static hipError_t join(const ProductArgs &a, hipStream_t s)
+{
+    if (a.dtype == TICTAC_F32) return join_as<OP, TICTAC_F32>(a, s);
+    return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(a, s) : join_as<OP, TICTAC_BF16>(a, s);
+}
+
+hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8>(a, s); }
+hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s) { return join<OpBf16>(a, s); }
 hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s) { return launch<OpI8>(a, s); }
 hipError_t launch_product_bf16(const ProductArgs &a, hipStream_t s) { return launch<OpBf16>(a, s); }
 

@@ -241,4 +241,10 @@ inline bool wide_rows(const void *p, int dt, int64_t ld, int64_t cols)
     return ((uintptr_t)p & 15) == 0 && (ld * elem_size(dt)) % 16 == 0 && cols % 8 == 0;
 }
 
+// f<type, wide>(...)
+#define BY_TYPE(dt, wide, f, ...)                                                                               \
+    ((dt) == TICTAC_F32    ? ((wide) ? f<TICTAC_F32, true>(__VA_ARGS__) : f<TICTAC_F32, false>(__VA_ARGS__))    \
+     : (dt) == TICTAC_F16  ? ((wide) ? f<TICTAC_F16, true>(__VA_ARGS__) : f<TICTAC_F16, false>(__VA_ARGS__))    \
+                           : ((wide) ? f<TICTAC_BF16, true>(__VA_ARGS__) : f<TICTAC_BF16, false>(__VA_ARGS__)))
+
 }  // namespace tictac
