@@ -172,15 +172,25 @@ static hipError_t launch_once(const LinearArgs &p, hipStream_t s)
     return hipGetLastError();
 }
 
+// Into how many parts along k the work of `blocks` workgroups is cut, at most `most`, where `room` workgroups run at a time: rounds times the length of a
+// part, an eighth of the whole added for what each part costs by itself.
+static int32_t parts_along_k(int64_t blocks, int64_t most, int64_t room)
+{
+    int32_t best = 1;
+    float least = 1e30f;
+    for (int32_t n = 1; n <= 16 && n <= most; ++n) {
+        const float cost = (float)((blocks * n + room - 1) / room) * (1.0f / (float)n + 0.125f);
+        if (cost < least) { least = cost; best = n; }
+    }
+    return best;
+}
+
 constexpr int64_t kFewRows = 64;
 static int32_t few_blocks_of(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }       // FB: x at most half of the weights' bytes, up to 32 rows
 static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
 {
     const int64_t blocks = (outs + 16 * few_blocks_of(rows) - 1) / (16 * few_blocks_of(rows)), units = (cols + 127) / 128;
-    if (blocks == 0) return 1;
-    int64_t n = 256 / blocks;                           // a workgroup per compute unit
-    if (n > units / (2 * kFewWaves)) n = units / (2 * kFewWaves);       // two units for each wave at least
-    return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
+    return parts_along_k(blocks, units / (2 * kFewWaves), 256);              // two units for each wave at least
 }
 
 static size_t forward_parts(int64_t rows, int64_t cols, int64_t outs, int32_t *splits)
@@ -229,8 +239,8 @@ hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
     return a.splits > 1 ? launch_product_join_i8(a, s) : hipGetLastError();
 }
 
-// dy times a scale in PIECES bf16 values that add up to it: all but the last cut off, which leaves the rest exact, the last rounded.  (An infinity
-// stays one, with nothing left.)
+// dy times a scale in PIECES bf16 values that add up to it: all but the last cut off, which leaves the rest exact, the last rounded.  An infinity
+// leaves NaN, for which the median of three takes the smallest: the pieces still add up to the infinity.
 template <int PIECES>
 __device__ __forceinline__ void cut(float v, uint16_t *piece)
 {
@@ -238,7 +248,7 @@ __device__ __forceinline__ void cut(float v, uint16_t *piece)
     for (int k = 0; k < PIECES - 1; ++k) {
         const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
         piece[k] = (uint16_t)(high >> 16);
-        v = (high & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __builtin_bit_cast(float, high);
+        v = __builtin_amdgcn_fmed3f(v - __builtin_bit_cast(float, high), -0x1p126f, 0x1p126f);
     }
     const __bf16 last = (__bf16)v;
     piece[PIECES - 1] = __builtin_bit_cast(uint16_t, last);
@@ -271,46 +281,82 @@ struct Pieces { static constexpr int value = DT == TICTAC_F32 ? 3 : DT == TICTAC
 // other.  A workgroup has 64 ND columns and a part of k, its eight waves blocks of 32 of k in turn; their sums meet in LDS, in fixed order.
 constexpr int kBackWaves = 8;
 
-template <int DT, bool WIDE, int TB, int ND>
-__global__ __launch_bounds__(kBackWaves * 64) void linear_dx_few_kernel(LinearArgs p, int32_t splits, float *parts)
-{
+// what eight of k bring for dx besides the weights: dy of TB blocks of 16 rows, and the weights' scales
+template <int DT, bool WIDE, int TB>
+struct GradientRows {
     using E = Elem<DT>;
-    using T = typename E::type;
-    constexpr int PIECES = Pieces<DT>::value, NJ = 4 * ND;
-    __shared__ f32x4 room[kBackWaves / 2][NJ][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-    const int64_t blocks = gridDim.x / splits, i0 = blockIdx.x % blocks * (16 * NJ), padded = (p.cols + 127) / 128 * 128;
-    const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.outs + 31) / 32);
-    const int32_t first = (int32_t)((int64_t)all * split / splits), last = (int32_t)((int64_t)all * (split + 1) / splits);
-    const int8_t *w = p.w + (i0 + c * NJ < padded ? i0 + c * NJ : 0);           // (columns behind the end: any will do)
-    typedef int32_t Words __attribute__((ext_vector_type(ND)));
-    Words now[8], next[8];
-    const auto request = [&](int32_t kb) {
+    typename E::raw dy[TB];
+    Elem<TICTAC_F32>::raw scale;
+    __device__ __forceinline__ void load(const LinearArgs &p, int64_t row, int64_t o)
+    {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) next[e] = *(const Words *)(w + min((int64_t)kb * 32 + g * 8 + e, p.outs - 1) * p.ld_w);
-    };
-    f32x4 acc[NJ][TB] = {};
-    if (first + wave < last) request(first + wave);
-    for (int32_t kb = first + wave; kb < last; kb += kBackWaves) {
-        const int64_t o = (int64_t)kb * 32 + g * 8;
-        float scale[8];
-        params8(p.ws, TICTAC_F32, o, p.outs, scale);
-        i32x4 q[TB][PIECES];
+        for (int b = 0; b < TB; ++b)
+            dy[b] = load8_or_last<DT, WIDE>((const typename E::type *)p.dy + min(b * 16 + row, p.rows - 1) * p.ld_dy, o, p.outs);
+        scale = load8_or_last<TICTAC_F32, WIDE>(p.ws, o, p.outs);
+    }
+    template <int PIECES>
+    __device__ __forceinline__ void operands(int64_t o, int64_t outs, i32x4 (&q)[TB][PIECES]) const
+    {
+        float s[8];
+        Elem<TICTAC_F32>::floats(scale, s);
 #pragma unroll
         for (int b = 0; b < TB; ++b) {
             float v[8];
             uint16_t cuts[8][PIECES];
-            E::floats(load8<DT, WIDE>((const T *)p.dy + min((int64_t)b * 16 + c, p.rows - 1) * p.ld_dy, o, p.outs), v);
+            E::floats(dy[b], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cut<PIECES>(v[e] * scale[e], cuts[e]);
+            for (int e = 0; e < 8; ++e) v[e] *= s[e];
+            if (o + 8 > outs)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = o + e < outs ? v[e] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cut<PIECES>(v[e], cuts[e]);
 #pragma unroll
             for (int k = 0; k < PIECES; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) q[b][k][e] = pair(cuts[2 * e][k], cuts[2 * e + 1][k]);
         }
+    }
+};
+
+template <int DT, bool WIDE, int TB, int ND>
+__global__ __launch_bounds__(kBackWaves * 64) void linear_dx_few_kernel(LinearArgs p, int32_t splits, float *parts)
+{
+    using T = typename Elem<DT>::type;
+    constexpr int PIECES = Pieces<DT>::value, NJ = 4 * ND;
+    extern __shared__ float room[];                             // [waves][NJ][64 lanes][4]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int64_t blocks = gridDim.x / splits, i0 = blockIdx.x % blocks * (16 * NJ), padded = (p.cols + 127) / 128 * 128;
+    const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.outs + 31) / 32);
+    const int32_t first = (int32_t)((int64_t)all * split / splits), last = (int32_t)((int64_t)all * (split + 1) / splits);
+    // rows g * 8 .. + 7 of a block of 32 of the weights, the same for all blocks (columns behind the end: any will do)
+    const uint32_t at = (uint32_t)(g * 8) * (uint32_t)p.ld_w + (uint32_t)(i0 + c * NJ < padded ? i0 + c * NJ : 0);
+    typedef int32_t Words __attribute__((ext_vector_type(ND)));
+    Words now[8], next[8];
+    GradientRows<DT, WIDE, TB> dy;
+    const auto request = [&](int32_t kb) {
+        const int8_t *block = p.w + (int64_t)kb * 32 * p.ld_w;
+        if ((int64_t)kb * 32 + 32 <= p.outs) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) next[e] = *(const Words *)(block + e * p.ld_w + at);
+        } else {                                                // the last block: its last row again
+            const int32_t rows = (int32_t)(p.outs - (int64_t)kb * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) next[e] = *(const Words *)(block + (at - (uint32_t)(g * 8) * (uint32_t)p.ld_w) + min(g * 8 + e, rows - 1) * p.ld_w);
+        }
+        dy.load(p, c, (int64_t)kb * 32 + g * 8);
+    };
+    f32x4 acc[NJ][TB] = {};
+    // Each workgroup starts at another block: rows of dy often lie a power of two apart, and what all ask for at a time would be in few channels.
+    const int32_t count = last - first, turn = count ? blockIdx.x * 5 % count : 0;
+    const auto block_of = [&](int32_t n) { return first + (n + turn < count ? n + turn : n + turn - count); };
+    if (wave < count) request(block_of(wave));
+    for (int32_t n = wave; n < count; n += kBackWaves) {
+        i32x4 q[TB][PIECES];
+        dy.template operands<PIECES>((int64_t)block_of(n) * 32 + g * 8, p.outs, q);
 #pragma unroll
         for (int e = 0; e < 8; ++e) now[e] = next[e];
-        if (kb + kBackWaves < last) request(kb + kBackWaves);
+        if (n + kBackWaves < count) request(block_of(n + kBackWaves));
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             int32_t words[8];
@@ -323,48 +369,36 @@ __global__ __launch_bounds__(kBackWaves * 64) void linear_dx_few_kernel(LinearAr
                 for (int k = 0; k < PIECES; ++k) acc[j][b] = mma_bf16(f, q[b][k], acc[j][b]);
         }
     }
-#pragma unroll
-    for (int b = 0; b < TB; ++b)
-        for (int half = kBackWaves / 2; half; half >>= 1) {
-            if (wave >= half && wave < 2 * half)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) room[wave - half][j][lane] = acc[j][b];
-            __syncthreads();
-            if (wave < half)
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[j][b] += room[wave][j][lane];
-            __syncthreads();
-        }
-    if (wave) return;
+    // A thread adds up eight columns of one row over the waves, in their order: element e of lane l, halves of the NJ operands by threads.
+    constexpr int kParts = NJ / 8, kThreads = 256 * kParts;
+    const int le = threadIdx.x & 255, part = threadIdx.x >> 8, from = le >> 2;
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
-        const int64_t t = b * 16 + c;
-        if (t >= p.rows) continue;
+        if (b) __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t i = i0 + NJ * (4 * g + e);
+        for (int j = 0; j < NJ; ++j) *(f32x4 *)(room + ((wave * NJ + j) * 64 + lane) * 4) = acc[j][b];
+        __syncthreads();
+        const int64_t t = b * 16 + (from & 15), i = i0 + NJ * (4 * (from >> 4) + (le & 3)) + part * 8;
+        if ((int)threadIdx.x >= kThreads || t >= p.rows) continue;
+        float v[8];
 #pragma unroll
-            for (int h = 0; h < NJ / 8; ++h) {
-                float v[8];
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = acc[h * 8 + j][b][e];
-                if (splits > 1) {
-                    float *part = parts + ((int64_t)split * p.rows + t) * p.cols;
-                    if (p.cols % 8 == 0) store8<TICTAC_F32, true>(part, i + h * 8, p.cols, v);
-                    else store8<TICTAC_F32, false>(part, i + h * 8, p.cols, v);
-                } else if (WIDE) {
-                    store8<DT, true>((T *)p.dx + t * p.ld_dx, i + h * 8, p.cols, v);
-                } else {
-                    store8<DT, false>((T *)p.dx + t * p.ld_dx, i + h * 8, p.cols, v);
-                }
-            }
+            for (int k = 0; k < kBackWaves; ++k) v[j] += room[(k * NJ + part * 8 + j) * 256 + le];
+        }
+        if (splits > 1) {
+            float *to = parts + ((int64_t)split * p.rows + t) * p.cols;
+            if (p.cols % 8 == 0) store8<TICTAC_F32, true>(to, i, p.cols, v);
+            else store8<TICTAC_F32, false>(to, i, p.cols, v);
+        } else {
+            store8<DT, WIDE>((T *)p.dx + t * p.ld_dx, i, p.cols, v);
         }
     }
 }
 
 // dw: all of k (the rows t, up to 32 KB) is at hand.  The activations are turned round in registers as the weights above, four bytes per lane, and stay
-// there; the pieces of dy times scale lie in LDS.  A workgroup has 64 outputs and 512 columns, a wave 64 columns; a lane stores sixteen values
-// next to each other.  db rides along with the first columns.
+// there; the pieces of dy times scale lie in LDS.  A workgroup has 64 outputs and 512 columns, a wave 64 columns.  db rides along with the first columns.
 template <int DT, bool WIDE, int KB>
 __global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
 {
@@ -388,12 +422,15 @@ __global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
     }
     __syncthreads();
     if (!p.dw || i0 >= p.cols) return;
+    // row r of an operand is the column at(r) + j: a lane's results (rows 4 g + e) then are eight next to each other at 8 g, and eight at 32 + 8 g, and
+    // four lanes store 64 bytes in a row
+    const int64_t column = i0 + ((c & 2) << 4) + ((c >> 2) << 3) + ((c & 1) << 2);
     i32x4 f[KB][4];
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
         int32_t words[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) words[e] = *(const int32_t *)(p.xq + min((int64_t)b * 32 + g * 8 + e, p.rows - 1) * p.ld_xq + i0 + c * 4);
+        for (int e = 0; e < 8; ++e) words[e] = *(const int32_t *)(p.xq + min((int64_t)b * 32 + g * 8 + e, p.rows - 1) * p.ld_xq + column);
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[b][j] = bytes_bf16(words, j);
     }
@@ -408,14 +445,14 @@ __global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[j] = mma_bf16(f[b][j], fq, acc[j]);
             }
-        const int64_t out = o0 + block * 16 + c, i = i0 + 16 * g;
+        const int64_t out = o0 + block * 16 + c;
         if (out >= p.outs) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float v[8];
 #pragma unroll
             for (int n = 0; n < 8; ++n) v[n] = acc[n & 3][h * 2 + (n >> 2)];
-            store8<DT, WIDE>((T *)p.dw + out * p.ld_dw, i + h * 8, p.cols, v);
+            store8<DT, WIDE>((T *)p.dw + out * p.ld_dw, i0 + h * 32 + g * 8, p.cols, v);
         }
     }
 }
@@ -424,9 +461,7 @@ static int32_t dx_few_words(int64_t rows) { return rows <= 32 ? 4 : 2; }
 static int32_t dx_few_splits(int64_t rows, int64_t cols, int64_t outs)
 {
     const int64_t wide = 64 * dx_few_words(rows), blocks = (cols + wide - 1) / wide, units = (outs + 31) / 32;
-    int64_t n = 256 / blocks;                                           // a workgroup per compute unit
-    if (n > units / (2 * kBackWaves)) n = units / (2 * kBackWaves);     // two blocks of k for each wave at least
-    return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
+    return parts_along_k(blocks, units / (2 * kBackWaves), 256);             // two blocks of k for each wave at least
 }
 
 // ---- backward: operands with k contiguous ----
@@ -580,7 +615,9 @@ static hipError_t backward_few(const LinearArgs &p, hipStream_t s)
     if (p.dx && p.rows) {
         const int32_t splits = dx_few_splits(p.rows, p.cols, p.outs), wide = 64 * dx_few_words(p.rows);
         const auto kernel = p.rows <= 16 ? linear_dx_few_kernel<DT, WIDE, 1, 4> : p.rows <= 32 ? linear_dx_few_kernel<DT, WIDE, 2, 4> : linear_dx_few_kernel<DT, WIDE, 4, 2>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.cols + wide - 1) / wide * splits)), dim3(kBackWaves * 64), 0, s, p, splits, (float *)p.workspace);
+        const size_t lds = (size_t)kBackWaves * wide * 64;
+        if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.cols + wide - 1) / wide * splits)), dim3(kBackWaves * 64), lds, s, p, splits, (float *)p.workspace);
         if (splits > 1) {
             ProductArgs a{};
             a.R = (int32_t)p.cols; a.C = (int32_t)p.rows; a.splits = splits; a.out = p.dx; a.ld_out = p.ld_dx; a.dtype = DT; a.parts = p.workspace;
@@ -651,7 +688,7 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
 hipError_t launch_linear_q8_backward(const LinearArgs &p, hipStream_t s)
 {
     if (p.rows > 0 && p.outs > 0 && p.rows <= kFewRows) {
-        const bool wide = wide_rows(p.dy, p.dtype, p.ld_dy, p.outs) && (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols)) && (!p.dw || wide_rows(p.dw, p.dtype, p.ld_dw, p.cols));
+        const bool wide = wide_rows(p.dy, p.dtype, p.ld_dy, p.outs) && ((uintptr_t)p.ws & 15) == 0 && (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols)) && (!p.dw || wide_rows(p.dw, p.dtype, p.ld_dw, p.cols));
         return BY_TYPE(p.dtype, wide, backward_few, p, s);
     }
     if (p.dtype == TICTAC_F32) return backward<TICTAC_F32, 3>(p, s);

@@ -107,8 +107,19 @@ __device__ __forceinline__ typename Elem<DT>::raw load8(const typename Elem<DT>:
     }
     float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? E::to_float(row[col + i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) {
+        const float x = E::to_float(row[min(col + i, cols - 1)]);          // (eight loads without a branch)
+        v[i] = col + i < cols ? x : 0.0f;
+    }
     return E::pack(v);              // (the values of the type: nothing is rounded)
+}
+
+// The same where a caller makes zeros of what lies behind the end: the row's last elements come again, without a branch.
+template <int DT, bool WIDE>
+__device__ __forceinline__ typename Elem<DT>::raw load8_or_last(const typename Elem<DT>::type *row, int64_t col, int64_t cols)
+{
+    if (WIDE) return Elem<DT>::load(row + min(col, cols - 8));
+    return load8<DT, false>(row, col, cols);
 }
 
 template <int DT, bool WIDE>
