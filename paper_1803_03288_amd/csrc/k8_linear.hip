@@ -2,7 +2,8 @@
 //   dx[t][i] = sum_o (dy[t][o] ws[o]) w[o][i],   dw[o][i] = sum_t (dy[t][o] xs[t]) xq[t][i],   db[o] = sum_t dy[t][o]
 // Forward: sums exact in int32.  Backward: int8 values are exact in bf16; dy times a scale, a float32 value, is cut into as many bf16
 // pieces as dy's type has bits to give (bf16 one, rounded once as dy itself was; float16 two; float32 three, exact), and the pieces go side by
-// side along k through the one product of k8_product.hip; sums in float32.
+// side along k through the one product of k8_product.hip (with many rows of bf16 the scale goes to the 8-bit value instead, also rounded once);
+// sums in float32.
 #include "k8_product.h"
 
 namespace tictac {
@@ -464,126 +465,130 @@ static int32_t dx_few_splits(int64_t rows, int64_t cols, int64_t outs)
     return parts_along_k(blocks, units / (2 * kBackWaves), 256);             // two blocks of k for each wave at least
 }
 
-// ---- backward: operands with k contiguous ----
-// Columns of int8 rows as bf16 rows: out[c][r] = q[r][c], zeros for r from `rows` to `padded`.  64 x 64 through LDS.
-__global__ __launch_bounds__(256) void transpose_rows8_kernel(int64_t rows, int64_t cols, const int8_t *q, int64_t ld, __bf16 *out, int64_t padded)
+// ---- backward with more rows: operands with k contiguous, for the tiles of k8_product.hip ----
+// A wave turns 64 rows of 128 bytes round in registers: lane l has eight rows, 8 (l % 8) .. + 7, and sixteen bytes of each, 16 (l / 8) ..; it stores for
+// each column eight values next to each other, and eight lanes store 128 bytes.  Reads and writes are whole lines, and nothing goes through LDS.
+//   weights, activations: int8 -> bf16, out[c][r] = q[r][c], times the scale of row r where dy is bf16 (SCALED: rounded once; dy then is an
+//   operand as it is)
+//   dy: out[o][piece][t] = pieces of dy[t][o] xs[t] and out[t][piece][o] = pieces of dy[t][o] ws[o]; where dy is bf16, dy[t][o] itself (and the second only
+//   if its rows are no operands as they are); sums of dy over each 64 rows
+template <bool SCALED>
+__device__ __forceinline__ void turn_rows8(int64_t rows, int64_t cols, const int8_t *q, int64_t ld, const float *scale, uint16_t *out, int64_t padded, int64_t r0, int64_t c0)
 {
-    __shared__ uint16_t tile[64][66];                           // (33 words a row: a column lies in all banks)
-    const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-    {
-        const int64_t r = r0 + (threadIdx.x >> 2);
-        const int c = (threadIdx.x & 3) * 16;
-        i32x4 v{};
-        if (r < rows) v = *(const i32x4 *)(q + r * ld + c0 + c);         // (c0 + 64 <= ld: rows are padded to 128)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float f = (float)((v[i >> 2] << (24 - 8 * (i & 3))) >> 24);
-            tile[threadIdx.x >> 2][c + i] = (uint16_t)(__builtin_bit_cast(uint32_t, f) >> 16);      // (exact: eight bits)
-        }
-    }
-    __syncthreads();
-    const int64_t c = c0 + (threadIdx.x >> 2);
-    const int r = (threadIdx.x & 3) * 16;
-    if (c >= cols) return;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        i32x4 w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = tile[r + h * 8 + 2 * i][threadIdx.x >> 2] | (uint32_t)tile[r + h * 8 + 2 * i + 1][threadIdx.x >> 2] << 16;
-        *(i32x4 *)(out + c * padded + r0 + r + h * 8) = w;
-    }
-}
-
-// out[t][piece][o] = pieces of dy[t][o] ws[o], zeros for o from `outs` to `padded`
-template <int DT, int PIECES>
-__global__ __launch_bounds__(256) void scaled_rows_kernel(int64_t rows, int64_t outs, const void *dy, int64_t ld_dy, const float *ws, uint16_t *out, int64_t padded)
-{
-    using E = Elem<DT>;
-    const int64_t o = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (o >= padded) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t r = r0 + (lane & 7) * 8, c = c0 + (lane >> 3) * 16;
+    i32x4 w[8];
     float s[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i] = o + i < outs ? ws[o + i] : 0.0f;
-    for (int64_t t = blockIdx.y; t < rows; t += gridDim.y) {
-        const typename E::type *row = (const typename E::type *)dy + t * ld_dy;
-        float v[8];
-        if (o + 8 <= outs && ((uintptr_t)(row + o) & 15) == 0) {
-            E::floats(E::load(row + o), v);
+    for (int e = 0; e < 8; ++e) {
+        w[e] = *(const i32x4 *)(q + min(r + e, rows - 1) * ld + c);          // (c + 16 <= ld: rows are padded to 128)
+        s[e] = r + e < rows ? (SCALED ? scale[min(r + e, rows - 1)] : 1.0f) : 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+        int32_t words[8];
+        i32x4 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) words[e] = w[e][j >> 2];
+        if (SCALED) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = r + e < rows ? (float)((words[e] << (24 - 8 * (j & 3))) >> 24) * s[e] : 0.0f;
+            v = __builtin_bit_cast(i32x4, Elem<TICTAC_BF16>::pack(f));
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = o + i < outs ? E::to_float(row[o + i]) : 0.0f;
+            for (int e = 0; e < 8; ++e) words[e] = r + e < rows ? words[e] : 0;
+            v = bytes_bf16(words, j & 3);
         }
-        uint16_t c[8][PIECES];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) cut<PIECES>(v[i] * s[i], c[i]);
-#pragma unroll
-        for (int k = 0; k < PIECES; ++k) {
-            i32x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = c[2 * i][k] | (uint32_t)c[2 * i + 1][k] << 16;
-            *(i32x4 *)(out + (t * PIECES + k) * padded + o) = w;
-        }
+        if (c + j < cols) *(i32x4 *)(out + (c + j) * padded + r) = v;
     }
 }
 
-// out[o][piece][t] = pieces of dy[t][o] xs[t], zeros for t from `rows` to `padded`; sums of dy over each 64 rows.
-template <int DT, int PIECES>
-__global__ __launch_bounds__(256) void scaled_columns_kernel(int64_t rows, int64_t outs, const void *dy, int64_t ld_dy, const float *xs, uint16_t *out, int64_t padded, float *sums)
+struct Operands {
+    int64_t units[3];                   // waves: up to here weights, activations, dy
+    uint16_t *p_x, *p_w, *q_x, *q_w;    // NULL: not needed
+    float *sums;                        // [rows / 64][outs], may be NULL
+    int64_t padded_o, padded_t;
+};
+
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Operands to)
 {
     using E = Elem<DT>;
     using T = typename E::type;
-    __shared__ float tile[64][65];
-    const int64_t t0 = (int64_t)blockIdx.y * 64, o0 = (int64_t)blockIdx.x * 64;
-    const int o = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-    for (int i = quarter; i < 64; i += 4)
-        tile[i][o] = t0 + i < rows && o0 + o < outs ? E::to_float(((const T *)dy)[(t0 + i) * ld_dy + o0 + o]) : 0.0f;
-    __syncthreads();
-    if (sums && quarter == 0 && o0 + o < outs) {
-        float sum = 0.0f;
-        for (int i = 0; i < 64; ++i) sum += tile[i][o];
-        sums[(int64_t)blockIdx.y * outs + o0 + o] = sum;
+    constexpr int PIECES = Pieces<DT>::value;
+    const int lane = threadIdx.x & 63;
+    int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t wide = (p.cols + 127) / 128;
+    if (unit < to.units[0]) {
+        turn_rows8<PIECES == 1>(p.outs, p.cols, p.w, p.ld_w, p.ws, to.p_x, to.padded_o, unit / wide * 64, unit % wide * 128);
+        return;
     }
-    if (!out) return;
-    const int row = threadIdx.x >> 2, t = (threadIdx.x & 3) * 16;
-    if (o0 + row >= outs) return;
-    uint16_t c[16][PIECES];
+    if (unit < to.units[1]) {
+        unit -= to.units[0];
+        turn_rows8<PIECES == 1>(p.rows, p.cols, p.xq, p.ld_xq, p.xs, to.p_w, to.padded_t, unit / wide * 64, unit % wide * 128);
+        return;
+    }
+    if (unit >= to.units[2]) return;
+    unit -= to.units[1];
+    const int64_t tiles = (p.outs + 63) / 64, t0 = unit / tiles * 64, t = t0 + (lane & 7) * 8, o = unit % tiles * 64 + (lane >> 3) * 8;
+    float v[8][8];                                              // [row][column]
 #pragma unroll
-    for (int i = 0; i < 16; ++i) cut<PIECES>(t0 + t + i < rows ? tile[t + i][row] * xs[t0 + t + i] : 0.0f, c[i]);
+    for (int e = 0; e < 8; ++e) {
+        const int64_t row = min(t + e, p.rows - 1);
+        E::floats(load8<DT, WIDE>((const T *)p.dy + row * p.ld_dy, o, p.outs), v[e]);
+        if (t + e >= p.rows)
 #pragma unroll
-    for (int k = 0; k < PIECES; ++k)
+            for (int i = 0; i < 8; ++i) v[e][i] = 0.0f;
+    }
+    if (to.sums) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            i32x4 w;
+        for (int i = 0; i < 8; ++i) {
+            float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = c[h * 8 + 2 * i][k] | (uint32_t)c[h * 8 + 2 * i + 1][k] << 16;
-            *(i32x4 *)(out + ((o0 + row) * PIECES + k) * padded + t0 + t + h * 8) = w;
+            for (int e = 0; e < 8; ++e) sum += v[e][i];
+#pragma unroll
+            for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
+            if ((lane & 7) == 0 && o + i < p.outs) to.sums[t0 / 64 * p.outs + o + i] = sum;
         }
-}
-
-// Adds up the sums of 64 rows each in their order.
-__global__ __launch_bounds__(1024) void column_sums_kernel(int64_t parts, int64_t outs, const float *sums, void *db, int32_t dt)
-{
-    __shared__ float shared[16][64];
-    const int64_t o = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-    const int wave = threadIdx.x >> 6;
-    const int64_t per = (parts + 15) / 16;
-    float sum = 0.0f;
-    if (o < outs)
-        for (int64_t k = wave * per; k < min(parts, (wave + 1) * per); ++k) sum += sums[k * outs + o];
-    shared[wave][threadIdx.x & 63] = sum;
-    __syncthreads();
-    if (wave || o >= outs) return;
-    sum = 0.0f;
+    }
+    if (to.q_x) {
+        float s[8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) sum += shared[k][threadIdx.x & 63];
-    put_param(db, dt, o, sum);
+        for (int i = 0; i < 8; ++i) s[i] = PIECES > 1 && o + i < p.outs ? p.ws[o + i] : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint16_t cuts[8][PIECES];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) cut<PIECES>(PIECES > 1 ? v[e][i] * s[i] : v[e][i], cuts[i]);
+            if (t + e >= p.rows) continue;
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                *(i32x4 *)(to.q_x + ((t + e) * PIECES + k) * to.padded_o + o) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
+        }
+    }
+    if (to.q_w) {
+        float s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = PIECES > 1 ? p.xs[min(t + e, p.rows - 1)] : 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint16_t cuts[8][PIECES];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) cut<PIECES>(PIECES > 1 ? (t + e < p.rows ? v[e][i] * s[e] : 0.0f) : v[e][i], cuts[e]);
+            if (o + i >= p.outs) continue;
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+                *(i32x4 *)(to.q_w + ((o + i) * PIECES + k) * to.padded_t + t) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
+        }
+    }
 }
 
-// The workspace of one backward call; the two products come one after the other and use the same room.
+// The workspace of one backward call.
 struct BackwardRoom {
     int64_t padded_o, padded_t;
-    size_t sums, p, q, parts, bytes;            // offsets
+    int32_t splits_x, splits_w;
+    size_t sums, p_x, p_w, q_x, q_w, parts_x, parts_w, bytes;           // offsets
 };
 static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int64_t outs)
 {
@@ -596,15 +601,15 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     }
     r.padded_o = (outs + 63) / 64 * 64;
     r.padded_t = (rows + 63) / 64 * 64;
-    r.sums = 0;
-    r.p = up((size_t)(r.padded_t / 64) * outs * 4);
-    const size_t p = (size_t)cols * (r.padded_o > r.padded_t ? r.padded_o : r.padded_t) * 2;
-    const size_t qx = (size_t)rows * r.padded_o * pieces * 2, qw = (size_t)outs * r.padded_t * pieces * 2;
-    r.q = r.p + up(p);
-    r.parts = r.q + up(qx > qw ? qx : qw);
-    const size_t px = product_parts_bytes(product_splits((int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces)), (int32_t)cols, (int32_t)rows);
-    const size_t pw = product_parts_bytes(product_splits((int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces)), (int32_t)cols, (int32_t)outs);
-    r.bytes = r.parts + up(px > pw ? px : pw);
+    r.splits_x = product_splits((int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces));
+    r.splits_w = product_splits((int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces));
+    r.p_x = r.sums + up((size_t)(r.padded_t / 64) * outs * 4);
+    r.p_w = r.p_x + up((size_t)cols * r.padded_o * 2);
+    r.q_x = r.p_w + up((size_t)cols * r.padded_t * 2);
+    r.q_w = r.q_x + up((size_t)rows * r.padded_o * pieces * 2);
+    r.parts_x = r.q_w + up((size_t)outs * r.padded_t * pieces * 2);
+    r.parts_w = r.parts_x + up(product_parts_bytes(r.splits_x, (int32_t)cols, (int32_t)rows));
+    r.bytes = r.parts_w + up(product_parts_bytes(r.splits_w, (int32_t)cols, (int32_t)outs));
     return r;
 }
 size_t linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs) { return backward_room(dtype, rows, cols, outs).bytes; }
@@ -632,67 +637,86 @@ static hipError_t backward_few(const LinearArgs &p, hipStream_t s)
     return hipGetLastError();
 }
 
-template <int DT, int PIECES>
+template <int DT, bool WIDE>
 static hipError_t backward(const LinearArgs &p, hipStream_t s)
 {
+    constexpr int PIECES = Pieces<DT>::value;
     const BackwardRoom room = backward_room(DT, p.rows, p.cols, p.outs);
     char *at = (char *)p.workspace;
+    // rows of bf16 that are whole steps of 128 bytes are operands as they are
+    const bool as_is = PIECES == 1 && WIDE && p.outs % 64 == 0 && p.ld_dy * 2 <= 1 << 24;         // (offsets inside a tile are 32 bits)
+    Operands to{};
+    to.padded_o = room.padded_o;
+    to.padded_t = room.padded_t;
+    if (p.dx) to.p_x = (uint16_t *)(at + room.p_x);
+    if (p.dw) to.p_w = (uint16_t *)(at + room.p_w);
+    if (p.dx && !as_is) to.q_x = (uint16_t *)(at + room.q_x);
+    if (p.dw) to.q_w = (uint16_t *)(at + room.q_w);
+    if (p.db) to.sums = (float *)(at + room.sums);
+    to.units[0] = p.dx ? (p.cols + 127) / 128 * (room.padded_o / 64) : 0;
+    to.units[1] = to.units[0] + (p.dw ? (p.cols + 127) / 128 * (room.padded_t / 64) : 0);
+    to.units[2] = to.units[1] + (to.q_x || to.q_w || to.sums ? (p.outs + 63) / 64 * (room.padded_t / 64) : 0);
+    hipLaunchKernelGGL((linear_operands_kernel<DT, WIDE>), dim3((unsigned)((to.units[2] + 3) / 4)), dim3(256), 0, s, p, to);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    ProductArgs a[2] = {};
+    int n = 0;
+    if (p.dx) {
+        ProductArgs &x = a[n++];
+        x.p = at + room.p_x;
+        x.ld_p = room.padded_o * 2;
+        x.q = as_is ? (const char *)p.dy : at + room.q_x;
+        x.ld_q = as_is ? p.ld_dy * 2 : room.padded_o * 2 * PIECES;
+        x.R = (int32_t)p.cols;
+        x.C = (int32_t)p.rows;
+        x.p_steps = (int32_t)(room.padded_o / 64);
+        x.splits = room.splits_x;
+        x.out = p.dx;
+        x.ld_out = p.ld_dx;
+        x.parts = at + room.parts_x;
+    }
+    if (p.dw) {
+        ProductArgs &w = a[n++];
+        w.p = at + room.p_w;
+        w.ld_p = room.padded_t * 2;
+        w.q = at + room.q_w;
+        w.ld_q = room.padded_t * 2 * PIECES;
+        w.R = (int32_t)p.cols;
+        w.C = (int32_t)p.outs;
+        w.p_steps = (int32_t)(room.padded_t / 64);
+        w.splits = room.splits_w;
+        w.out = p.dw;
+        w.ld_out = p.ld_dw;
+        w.parts = at + room.parts_w;
+    }
+    for (int i = 0; i < n; ++i) {
+        a[i].steps = a[i].p_steps * PIECES;
+        a[i].dtype = DT;
+    }
+    const ColumnSums c{(const float *)(at + room.sums), room.padded_t / 64, p.outs, p.db, DT};
+    return launch_products_bf16(a, n, c, s);
+}
+
+// No rows, or no outputs: what there is of the gradients is zero.
+static hipError_t backward_nothing(const LinearArgs &p, hipStream_t s)
+{
     ProductArgs a{};
-    a.p = at + room.p;
-    a.q = at + room.q;
+    a.splits = 1;
     a.R = (int32_t)p.cols;
-    a.dtype = DT;
-    a.parts = at + room.parts;
-    if (p.dx && p.rows) {
-        if (p.outs) {
-            hipLaunchKernelGGL(transpose_rows8_kernel, dim3((unsigned)((p.cols + 63) / 64), (unsigned)(room.padded_o / 64)), dim3(256), 0, s, p.outs, p.cols, p.w, p.ld_w,
-                               (__bf16 *)a.p, room.padded_o);
-            hipLaunchKernelGGL((scaled_rows_kernel<DT, PIECES>), dim3((unsigned)((room.padded_o + 2047) / 2048), (unsigned)(p.rows < 4096 ? p.rows : 4096)), dim3(256), 0, s, p.rows, p.outs,
-                               p.dy, p.ld_dy, p.ws, (uint16_t *)a.q, room.padded_o);
-        }
-        a.ld_p = room.padded_o * 2;
-        a.ld_q = room.padded_o * 2 * PIECES;
-        a.C = (int32_t)p.rows;
-        a.p_steps = (int32_t)(room.padded_o / 64);
-        a.steps = a.p_steps * PIECES;
-        a.splits = product_splits(a.R, a.C, a.steps);
-        a.out = p.dx;
-        a.ld_out = p.ld_dx;
-        if (const hipError_t e = launch_product_bf16(a, s); e != hipSuccess) return e;
-    }
-    if (p.outs && (p.dw || p.db)) {
-        float *sums = (float *)(at + room.sums);
-        if (p.rows)
-            hipLaunchKernelGGL((scaled_columns_kernel<DT, PIECES>), dim3((unsigned)((p.outs + 63) / 64), (unsigned)(room.padded_t / 64)), dim3(256), 0, s, p.rows, p.outs, p.dy, p.ld_dy,
-                               p.xs, p.dw ? (uint16_t *)a.q : nullptr, room.padded_t, p.db ? sums : nullptr);
-        if (p.db)
-            hipLaunchKernelGGL(column_sums_kernel, dim3((unsigned)((p.outs + 63) / 64)), dim3(1024), 0, s, room.padded_t / 64, p.outs, sums, p.db, p.dtype);
-    }
-    if (p.dw && p.outs) {
-        if (p.rows)
-            hipLaunchKernelGGL(transpose_rows8_kernel, dim3((unsigned)((p.cols + 63) / 64), (unsigned)(room.padded_t / 64)), dim3(256), 0, s, p.rows, p.cols, p.xq, p.ld_xq,
-                               (__bf16 *)a.p, room.padded_t);
-        a.ld_p = room.padded_t * 2;
-        a.ld_q = room.padded_t * 2 * PIECES;
-        a.C = (int32_t)p.outs;
-        a.p_steps = (int32_t)(room.padded_t / 64);
-        a.steps = a.p_steps * PIECES;
-        a.splits = product_splits(a.R, a.C, a.steps);
-        a.out = p.dw;
-        a.ld_out = p.ld_dw;
-        if (const hipError_t e = launch_product_bf16(a, s); e != hipSuccess) return e;
-    }
-    return hipGetLastError();
+    a.dtype = p.dtype;
+    a.C = (int32_t)(p.rows ? p.rows : p.outs);
+    a.out = p.rows ? p.dx : p.dw;
+    a.ld_out = p.rows ? p.ld_dx : p.ld_dw;
+    const ColumnSums c{nullptr, 0, p.outs, p.outs ? p.db : nullptr, p.dtype};
+    return launch_products_bf16(&a, a.out && a.C ? 1 : 0, c, s);
 }
 
 hipError_t launch_linear_q8_backward(const LinearArgs &p, hipStream_t s)
 {
-    if (p.rows > 0 && p.outs > 0 && p.rows <= kFewRows) {
-        const bool wide = wide_rows(p.dy, p.dtype, p.ld_dy, p.outs) && ((uintptr_t)p.ws & 15) == 0 && (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols)) && (!p.dw || wide_rows(p.dw, p.dtype, p.ld_dw, p.cols));
-        return BY_TYPE(p.dtype, wide, backward_few, p, s);
-    }
-    if (p.dtype == TICTAC_F32) return backward<TICTAC_F32, 3>(p, s);
-    return p.dtype == TICTAC_F16 ? backward<TICTAC_F16, 2>(p, s) : backward<TICTAC_BF16, 1>(p, s);
+    if (p.rows == 0 || p.outs == 0) return backward_nothing(p, s);
+    const bool few = p.rows <= kFewRows, wide = wide_rows(p.dy, p.dtype, p.ld_dy, p.outs);
+    if (!few) return BY_TYPE(p.dtype, wide, backward, p, s);
+    const bool all = wide && ((uintptr_t)p.ws & 15) == 0 && (!p.dx || wide_rows(p.dx, p.dtype, p.ld_dx, p.cols)) && (!p.dw || wide_rows(p.dw, p.dtype, p.ld_dw, p.cols));
+    return BY_TYPE(p.dtype, all, backward_few, p, s);
 }
 
 }  // namespace tictac

@@ -26,11 +26,19 @@ struct ProductArgs {
     void *parts;                // [splits][C][R], int32 or float32
 };
 
+// Sums of `parts` rows of floats, [parts][n], in their order, as a vector of `dtype`: rides along with the products of a backward pass.
+struct ColumnSums {
+    const float *sums;
+    int64_t parts, n;
+    void *out;                  // NULL: none
+    int32_t dtype;
+};
+
 int32_t product_splits(int32_t R, int32_t C, int32_t steps);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
 hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s);
+hipError_t launch_products_bf16(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s);     // one or two products, of one output type, in one launch
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s);        // the sums in `parts` to the output
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s);
-hipError_t launch_product_bf16(const ProductArgs &a, hipStream_t s);
 
 }  // namespace tictac

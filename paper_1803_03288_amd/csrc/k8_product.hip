@@ -106,13 +106,36 @@ __device__ __forceinline__ void put_blocks(const ProductArgs &a, const typename 
 }
 
 // ---- tiles ----
+// What one launch does: up to two products, a run of workgroups each, and the sums of columns.
+struct Products {
+    ProductArgs a[2];
+    int32_t tiles_r[2], tiles_c[2];
+    int32_t first[3];                   // workgroups from first[i] on: product 0, product 1, sums
+    ColumnSums sums;
+};
+
+__device__ __forceinline__ void column_sums(const ColumnSums &c, int32_t block, float *room)        // 64 columns per workgroup
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    const int64_t at = (int64_t)block * 64 + lane, per = (c.parts + waves - 1) / waves;
+    float sum = 0.0f;
+    if (at < c.n)
+        for (int64_t k = wave * per; k < min(c.parts, (wave + 1) * per); ++k) sum += c.sums[k * c.n + at];
+    room[wave * 64 + lane] = sum;
+    __syncthreads();
+    if (wave || at >= c.n) return;
+    sum = 0.0f;
+    for (int k = 0; k < waves; ++k) sum += room[k * 64 + lane];
+    put_param(c.out, c.dtype, at, sum);
+}
+
 // Workgroups go to the eight XCDs in turn; each XCD gets a run of consecutive tiles, and a run goes down eight columns of tiles side by side,
 // so that what an XCD's L2 holds is used again.
-__device__ __forceinline__ void tile_of(int32_t tiles_r, int32_t tiles_c, int32_t &split, int32_t &tr, int32_t &tc)
+__device__ __forceinline__ void tile_of(int32_t block, int32_t tiles_r, int32_t tiles_c, int32_t &split, int32_t &tr, int32_t &tc)
 {
     const int32_t tiles = tiles_r * tiles_c;
-    int32_t at = blockIdx.x % tiles;
-    split = blockIdx.x / tiles;
+    int32_t at = block % tiles;
+    split = block / tiles;
     const int32_t xcd = at & 7, whole = tiles >> 3, more = tiles & 7;
     at = xcd * whole + min(xcd, more) + (at >> 3);
     const int32_t band = at / (8 * tiles_r), in_band = at - band * 8 * tiles_r, width = min(8, tiles_c - band * 8);
@@ -161,13 +184,19 @@ struct TileLoads {
 
 // A tile of 32 FR x 32 FC outputs by four waves, several workgroups per compute unit.
 template <class OP, int OUT, int FR, int FC>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs a, int32_t tiles_r, int32_t tiles_c)
+__global__ __launch_bounds__(256) void product_kernel(Products all)
 {
     constexpr int TR = FR * 32, TC = FC * 32;
     extern __shared__ char lds[];                                       // [2][TR + TC][128]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if ((int32_t)blockIdx.x >= all.first[2]) {
+        column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
+        return;
+    }
+    const int which = (int32_t)blockIdx.x >= all.first[1];
+    const ProductArgs &a = all.a[which];
     int32_t split, tr, tc;
-    tile_of(tiles_r, tiles_c, split, tr, tc);
+    tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
     const int32_t r0 = tr * TR, c0 = tc * TC;
     const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
     TileLoads<TR, TC, 4> loads;
@@ -201,7 +230,9 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a, int32_t til
         }
     }
     __syncthreads();
-    put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, lds + wave * 16 * (FR * 16 + 4) * 4);
+    char *room = lds + wave * 16 * (FR * 16 + 4) * 4;
+    if (a.splits > 1) put_blocks<OP, kParts, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
+    else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
 }
 
 // A tile of 256 x 256 outputs by eight waves, two per SIMD: while one of the two computes, the other reads its next operands from LDS.  The waves of the
@@ -211,13 +242,19 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs a, int32_t til
 //     (they are waited for before it).  So each wave asks for step t + 1 in its first reading slot of step t.
 //   - Step t + 1 is read from slot 8t + 8 on: every wave has waited for its loads at the end of slot 8t + 7.
 template <class OP, int OUT>
-__global__ __launch_bounds__(512, 2) void product_kernel_256(ProductArgs a, int32_t tiles_r, int32_t tiles_c)
+__global__ __launch_bounds__(512, 2) void product_kernel_256(Products all)
 {
     constexpr int TR = 256, TC = 256, FR = 8, FC = 4;
     extern __shared__ char lds[];                                       // [2][TR + TC][128]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2;
+    if ((int32_t)blockIdx.x >= all.first[2]) {
+        column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
+        return;
+    }
+    const int which = (int32_t)blockIdx.x >= all.first[1];
+    const ProductArgs &a = all.a[which];
     int32_t split, tr, tc;
-    tile_of(tiles_r, tiles_c, split, tr, tc);
+    tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
     const int32_t r0 = tr * TR, c0 = tc * TC;
     TileLoads<TR, TC, 8> loads;
     loads.init(a, r0, c0, 0, wave);
@@ -270,12 +307,17 @@ __global__ __launch_bounds__(512, 2) void product_kernel_256(ProductArgs a, int3
 
 // Adds up the splits in their order, four outputs per thread (one where rows of the sums do not start on 16-byte boundaries), the loads of
 // four splits under way.
+struct Joins {
+    ProductArgs a[2];
+    uint32_t first1;                    // workgroups from here on: product 1
+};
+
 template <class OP, int OUT, int VEC>
-__global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_t pieces)
+__device__ __forceinline__ void join_part(const ProductArgs &a, int64_t at)
 {
     typedef typename std::remove_reference<decltype(typename OP::acc{}[0] + typename OP::acc{}[0])>::type N;
     typedef N NV __attribute__((ext_vector_type(VEC)));
-    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int32_t pieces = a.R / VEC;
     if (at >= (int64_t)pieces * a.C) return;
     const int32_t c = (int32_t)(at / pieces), r = (int32_t)(at % pieces) * VEC;
     const NV *part = (const NV *)((const N *)a.parts + (int64_t)c * a.R + r);
@@ -303,11 +345,31 @@ __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs a, int32_
 }
 
 template <class OP, int OUT>
-static hipError_t join_as(const ProductArgs &a, hipStream_t s)
+__global__ __launch_bounds__(256) void product_join_kernel(Joins all)
 {
-    const int32_t vec = a.R % 4 ? 1 : 4, pieces = a.R / vec;
-    const auto kernel = vec == 4 ? product_join_kernel<OP, OUT, 4> : product_join_kernel<OP, OUT, 1>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(((int64_t)pieces * a.C + 255) / 256)), dim3(256), 0, s, a, pieces);
+    const int which = blockIdx.x >= all.first1;
+    const ProductArgs &a = all.a[which];
+    const int64_t at = (int64_t)(blockIdx.x - (which ? all.first1 : 0)) * 256 + threadIdx.x;
+    if (a.R % 4 == 0) join_part<OP, OUT, 4>(a, at);
+    else join_part<OP, OUT, 1>(a, at);
+}
+
+template <class OP, int OUT>
+static hipError_t join_as(const ProductArgs *a, int n, hipStream_t s)
+{
+    Joins all{};
+    uint32_t blocks = 0;
+    int m = 0;
+    for (int i = 0; i < n; ++i) {
+        if (a[i].splits <= 1) continue;
+        all.a[m] = a[i];
+        if (m == 1) all.first1 = blocks;
+        blocks += (uint32_t)(((int64_t)(a[i].R % 4 ? a[i].R : a[i].R / 4) * a[i].C + 255) / 256);
+        ++m;
+    }
+    if (m == 0) return hipSuccess;
+    if (m == 1) all.first1 = UINT32_MAX;
+    hipLaunchKernelGGL((product_join_kernel<OP, OUT>), dim3(blocks), dim3(256), 0, s, all);
     return hipGetLastError();
 }
 
@@ -323,42 +385,57 @@ int32_t product_splits(int32_t R, int32_t C, int32_t steps)
 }
 
 template <class OP, int OUT>
-static hipError_t launch_as(const ProductArgs &a, hipStream_t s)
+static hipError_t launch_as(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s)
 {
-    const int64_t big = (int64_t)((a.R + 255) / 256) * ((a.C + 255) / 256);
-    if (a.splits == 1 && big >= 192) {
-        constexpr int lds = 2 * 512 * 128;
-        const auto kernel = product_kernel_256<OP, OUT>;
-        if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)big), dim3(512), lds, s, a, (a.R + 255) / 256, (a.C + 255) / 256);
-        return hipGetLastError();
+    Products all{};
+    int64_t big = 0;
+    bool whole = true;
+    for (int i = 0; i < n; ++i) {
+        big += (int64_t)((a[i].R + 255) / 256) * ((a[i].C + 255) / 256);
+        whole &= a[i].splits <= 1;
     }
-    constexpr int lds = 2 * 256 * 128;
-    const int32_t tr = (a.R + kSmallTile - 1) / kSmallTile, tc = (a.C + kSmallTile - 1) / kSmallTile;
-    const auto kernel = a.splits > 1 ? product_kernel<OP, kParts, 4, 4> : product_kernel<OP, OUT, 4, 4>;
+    whole &= big >= 192;
+    const int32_t tile = whole ? 256 : kSmallTile;
+    int32_t blocks = 0;
+    for (int i = 0; i < 2; ++i) {
+        all.first[i] = blocks;
+        if (i >= n) continue;
+        all.a[i] = a[i];
+        all.tiles_r[i] = (a[i].R + tile - 1) / tile;
+        all.tiles_c[i] = (a[i].C + tile - 1) / tile;
+        blocks += all.tiles_r[i] * all.tiles_c[i] * a[i].splits;
+    }
+    all.first[2] = blocks;
+    all.sums = c;
+    if (c.out) blocks += (int32_t)((c.n + 63) / 64);
+    if (n == 1) all.first[1] = all.first[2];
+    if (blocks == 0) return hipSuccess;
+    const auto kernel = whole ? product_kernel_256<OP, OUT> : product_kernel<OP, OUT, 4, 4>;
+    const int lds = 2 * 2 * tile * 128;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tr * tc * a.splits), dim3(256), lds, s, a, tr, tc);
-    return a.splits > 1 ? join_as<OP, OUT>(a, s) : hipGetLastError();
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(whole ? 512 : 256), lds, s, all);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    return join_as<OP, OUT>(a, n, s);
 }
 
 template <class OP>
-static hipError_t launch(const ProductArgs &a, hipStream_t s)
+static hipError_t launch(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s)
 {
-    if (a.R == 0 || a.C == 0) return hipSuccess;
-    if (a.dtype == TICTAC_F32) return launch_as<OP, TICTAC_F32>(a, s);
-    return a.dtype == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, s) : launch_as<OP, TICTAC_BF16>(a, s);
+    const int32_t dt = n ? a[0].dtype : c.dtype;
+    if (dt == TICTAC_F32) return launch_as<OP, TICTAC_F32>(a, n, c, s);
+    return dt == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, n, c, s) : launch_as<OP, TICTAC_BF16>(a, n, c, s);
 }
 
 template <class OP>
 static hipError_t join(const ProductArgs &a, hipStream_t s)
 {
-    if (a.dtype == TICTAC_F32) return join_as<OP, TICTAC_F32>(a, s);
-    return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(a, s) : join_as<OP, TICTAC_BF16>(a, s);
+    if (a.dtype == TICTAC_F32) return join_as<OP, TICTAC_F32>(&a, 1, s);
+    return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(&a, 1, s) : join_as<OP, TICTAC_BF16>(&a, 1, s);
 }
 
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8>(a, s); }
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s) { return join<OpBf16>(a, s); }
-hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s) { return launch<OpI8>(a, s); }
-hipError_t launch_product_bf16(const ProductArgs &a, hipStream_t s) { return launch<OpBf16>(a, s); }
+hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s) { return launch<OpI8>(&a, 1, ColumnSums{}, s); }
+hipError_t launch_products_bf16(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s) { return launch<OpBf16>(a, n, c, s); }
 
 }  // namespace tictac
