@@ -1,5 +1,7 @@
 // See k8_product.h.  A workgroup has a tile of the output, its waves a part of that each; the operands come through LDS in steps of 128
 // bytes of k, two buffers in turn: while one is computed from, the next step is under way into the other, straight from memory to LDS.
+#include <algorithm>
+
 #include "device_utils.h"
 #include "k8_product.h"
 
@@ -11,6 +13,7 @@ typedef const __attribute__((address_space(1))) void global_void;
 struct OpI8 {
     typedef i32x4 acc;
     static __device__ __forceinline__ acc mma(i32x4 a, i32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void mma_in_place(i32x4 a, i32x4 b, acc &c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 struct OpBf16 {
     typedef f32x4 acc;
@@ -18,6 +21,7 @@ struct OpBf16 {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     }
+    static __device__ __forceinline__ void mma_in_place(i32x4 a, i32x4 b, acc &c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 
 // ---- outputs ----
@@ -110,7 +114,8 @@ __device__ __forceinline__ void put_blocks(const ProductArgs &a, const typename 
 struct Products {
     ProductArgs a[2];
     int32_t tiles_r[2], tiles_c[2];
-    int32_t first[3];                   // workgroups from first[i] on: product 0, product 1, sums
+    int32_t first[3];                   // tiles (times splits) from first[i] on: product 0, product 1, none
+    int32_t sum_blocks;                 // the last workgroups: sums
     ColumnSums sums;
 };
 
@@ -146,7 +151,8 @@ __device__ __forceinline__ void tile_of(int32_t block, int32_t tiles_r, int32_t 
 // The loads of a tile.  A load brings 8 rows of 128 bytes to LDS, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i
 // holds the bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.  Rows behind the end are the last row again; nobody
 // stores what comes of them.
-template <int TR, int TC, int WAVES>
+// PAIRED: rows of p go to the places that suit the reads of product_kernel_256, j ^ (i % 4 + 4 (i / 8 % 2)).
+template <int TR, int TC, int WAVES, bool PAIRED>
 struct TileLoads {
     static constexpr int LP = TR / 8 / WAVES, LQ = TC / 8 / WAVES;      // per wave and step
     uint32_t off_p[LP], off_q[LQ];
@@ -154,9 +160,11 @@ struct TileLoads {
     int32_t p_left;                     // steps until p starts again
     __device__ __forceinline__ void init(const ProductArgs &a, int32_t r0, int32_t c0, int32_t first, int wave)
     {
+        static_assert(WAVES % 2 == 0, "rows 8 (i WAVES + wave) .. + 7: bit 3 is that of the wave");
         const int lane = threadIdx.x & 63, row = lane >> 3, col = ((lane & 7) ^ row) * 16;
+        const int col_p = PAIRED ? ((lane & 7) ^ ((row & 3) | (wave & 1) << 2)) * 16 : col;
 #pragma unroll
-        for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col;
+        for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col_p;
 #pragma unroll
         for (int i = 0; i < LQ; ++i) off_q[i] = (uint32_t)min(a.C - 1 - c0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_q + col;
         const int32_t at = a.p_steps ? first % a.p_steps : 0;
@@ -173,6 +181,16 @@ struct TileLoads {
 #pragma unroll
         for (int i = 0; i < LQ; ++i)
             __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[i]), (lds_void *)(to + TR * 128 + (i * WAVES + wave) * 1024), 16, 0, 0);
+        next(a);
+    }
+    // one of its LP + LQ loads; next() when all have been asked for
+    __device__ __forceinline__ void request_one(const ProductArgs &a, char *to, int wave, int i)
+    {
+        if (i < LP) __builtin_amdgcn_global_load_lds((global_void *)(p + off_p[i % LP]), (lds_void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
+        else __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[(i - LP) % LQ]), (lds_void *)(to + TR * 128 + ((i - LP) * WAVES + wave) * 1024), 16, 0, 0);
+    }
+    __device__ __forceinline__ void next(const ProductArgs &a)
+    {
         q += 128;
         p += 128;
         if (--p_left == 0) {
@@ -189,7 +207,7 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
     constexpr int TR = FR * 32, TC = FC * 32;
     extern __shared__ char lds[];                                       // [2][TR + TC][128]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int32_t)blockIdx.x >= all.first[2]) {
+    if ((int32_t)blockIdx.x >= all.first[2]) {                          // (a workgroup per tile)
         column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
         return;
     }
@@ -199,7 +217,7 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
     tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
     const int32_t r0 = tr * TR, c0 = tc * TC;
     const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
-    TileLoads<TR, TC, 4> loads;
+    TileLoads<TR, TC, 4, false> loads;
     loads.init(a, r0, c0, first, wave);
     const int wr = wave & 1, wc = wave >> 1;
     typename OP::acc acc[FR][FC];
@@ -235,74 +253,154 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
     else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
 }
 
-// A tile of 256 x 256 outputs by eight waves, two per SIMD: while one of the two computes, the other reads its next operands from LDS.  The waves of the
-// second half run one slot behind (a barrier ends a slot); a step has four slots of reading and four of sixteen matrix instructions each.
-// Slots of step t, for the first half: 8t read, 8t + 1 compute, ...; for the second: 8t + 1 read, 8t + 2 compute, ...
-//   - The other buffer is free from slot 8t on: the second half's last reads of step t - 1 are over at the barrier behind slot 8t - 1
-//     (they are waited for before it).  So each wave asks for step t + 1 in its first reading slot of step t.
-//   - Step t + 1 is read from slot 8t + 8 on: every wave has waited for its loads at the end of slot 8t + 7.
+// Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each.  A step of 128 bytes has two halves of 64 matrix instructions; under
+// each half the operands of the next are read:
+//   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1:
+//     all of step t + 1 is there, and nobody reads the buffer of step t any more;
+//   - half 1 of step t reads the first half of step t + 1 and asks for step t + 2, into the buffer of step t.
+// The accumulators fill the 256 accumulation registers, hence the matrix instructions in assembly.  One workgroup per compute unit goes from tile to tile:
+// behind the last barrier of a tile LDS is free, and the first two steps of the next tile are asked for before this one's outputs are formed.
+// Two blocks of 16 rows share 32 rows of p in turns of four (row 4 n + e of block 2 m + h is row 32 m + 8 n + 4 h + e of the tile), so that a lane has
+// eight outputs next to each other and stores sixteen bytes of bf16 straight from its registers.
+// 8192 x 4096 x 16384 int8: a step takes 1.47 us of a workgroup (2.9 POP/s), what lies between two tiles used to take 14 us.
 template <class OP, int OUT>
-__global__ __launch_bounds__(512, 2) void product_kernel_256(Products all)
+__global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 {
-    constexpr int TR = 256, TC = 256, FR = 8, FC = 4;
-    extern __shared__ char lds[];                                       // [2][TR + TC][128]
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = wave >> 2;
-    if ((int32_t)blockIdx.x >= all.first[2]) {
-        column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
+    constexpr int TR = 256, TC = 256, FR = 8, FC = 8, kBuffer = (TR + TC) * 128;
+    extern __shared__ char lds[];                                       // [2][TR + TC][128], scales of rows, bias, scales of columns
+    float *const scales = (float *)(lds + 2 * kBuffer);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int32_t workers = gridDim.x - all.sum_blocks;
+    if ((int32_t)blockIdx.x >= workers) {
+        column_sums(all.sums, blockIdx.x - workers, (float *)lds);
         return;
     }
-    const int which = (int32_t)blockIdx.x >= all.first[1];
-    const ProductArgs &a = all.a[which];
-    int32_t split, tr, tc;
-    tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
-    const int32_t r0 = tr * TR, c0 = tc * TC;
-    TileLoads<TR, TC, 8> loads;
-    loads.init(a, r0, c0, 0, wave);
-    const int wr = wave & 1, wc = wave >> 1;
+    const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
+    const char *const tp = lds + (wr * FR * 16 + (frow >> 2) * 8 + (frow & 3)) * 128, *const tq = lds + TR * 128 + (wc * FC * 16 + frow) * 128;
+    constexpr bool kScaled = Scaled<OP>::value;
+    TileLoads<TR, TC, 4, true> loads;
     typename OP::acc acc[FR][FC];
+    i32x4 fp[2][FR], fq[2][FC];
+    int32_t r0, c0, which;
+    const auto begin = [&](int32_t tile) {
+        which = tile >= all.first[1];
+        const ProductArgs &a = all.a[which];
+        int32_t split, tr, tc;
+        tile_of(tile - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
+        r0 = tr * TR;
+        c0 = tc * TC;
+        loads.init(a, r0, c0, 0, wave);
+        if (a.steps) loads.request(a, lds, wave);
+        if (a.steps > 1) loads.request(a, lds + kBuffer, wave);
+    };
+    const auto read_one = [&](int half, int n, int place) {
+        if (n < FC) fq[half][n] = *(const i32x4 *)(tq + n * 2048 + place);
+        else fp[half][n - FC] = *(const i32x4 *)(tp + ((n - FC) >> 1) * 4096 + ((n - FC) & 1) * 512 + place);
+    };
+    // One half of a step: its 64 matrix instructions, after every fourth a read of the operands of the next half and a load of a later step
+    const auto run = [&](const ProductArgs &a, int half, int32_t step, bool read, bool ask) {
+        const int buffer = (step + half) & 1;                           // (half 1 reads the next step)
+        const int place = buffer * kBuffer + (((half ^ 1) * 4 + fk) ^ swizzle) * 16;
 #pragma unroll
-    for (int i = 0; i < FR; ++i)
+        for (int n = 0; n < 16; ++n) {
+            if (read) read_one(half ^ 1, n, place);
+            if (ask) loads.request_one(a, lds + (step & 1) * kBuffer, wave, n);
+            const int i = n >> 1, j0 = (n & 1) * 4;
 #pragma unroll
-        for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
-    const int frow = lane & 15, fk = lane >> 4;
-    if (a.steps) loads.request(a, lds, wave);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    if (half) __builtin_amdgcn_s_barrier();
-    for (int32_t step = 0; step < a.steps; ++step) {
-        char *const here = lds + (step & 1) * (TR + TC) * 128;
-        const char *tp = here + (wr * FR * 16 + frow) * 128, *tq = here + TR * 128 + (wc * FC * 16 + frow) * 128;
-        i32x4 fp[FR / 2], fq[FC];
-#pragma unroll
-        for (int slot = 0; slot < 4; ++slot) {
-            const int k = slot >> 1, at = (slot & 1) * (FR / 2), place = ((k * 4 + fk) ^ (frow & 7)) * 16;
-            if (at == 0) {
-#pragma unroll
-                for (int j = 0; j < FC; ++j) fq[j] = *(const i32x4 *)(tq + j * 2048 + place);
-            }
-#pragma unroll
-            for (int i = 0; i < FR / 2; ++i) fp[i] = *(const i32x4 *)(tp + (at + i) * 2048 + place);
-            if (slot == 0 && step + 1 < a.steps) loads.request(a, lds + ((step & 1) ^ 1) * (TR + TC) * 128, wave);
-            if (slot == 3 && half) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int i = 0; i < FR / 2; ++i)
-#pragma unroll
-                for (int j = 0; j < FC; ++j) acc[at + i][j] = OP::mma(fp[i], fq[j], acc[at + i][j]);
-            __builtin_amdgcn_s_setprio(0);
-            if (slot == 3 && !half) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
+            for (int j = j0; j < j0 + 4; ++j) OP::mma_in_place(fp[half][i], fq[half][j], acc[i][j]);
         }
+        if (ask) loads.next(a);
+    };
+    const auto barrier = [] {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");                                  // (nothing is read before the barrier)
+    };
+    int32_t tile = blockIdx.x, after = 0;                               // after: stores that surely were issued behind the loads under way
+    begin(tile);
+    while (true) {
+        const ProductArgs &a = all.a[which];
+        const int32_t steps = a.steps, row0 = r0, col0 = c0, t = threadIdx.x;
+        float row_scale = 0.0f, row_bias = 0.0f, col_scale = 0.0f;
+        if (kScaled) {
+            if (row0 + t < a.R) row_scale = a.p_scale[row0 + t];
+            if (a.bias && row0 + t < a.R) row_bias = param(a.bias, a.bias_dtype, row0 + t);
+            if (col0 + t < a.C) col_scale = a.q_scale[col0 + t];
+        }
+#pragma unroll
+        for (int i = 0; i < FR; ++i)
+#pragma unroll
+            for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
+        // (of what was issued behind the loads, the stores of the tile before may go on)
+        if (after >= 32) asm volatile("s_waitcnt vmcnt(32)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        barrier();
+        if (steps) {
+#pragma unroll
+            for (int n = 0; n < 16; ++n) read_one(0, n, (fk ^ swizzle) * 16);
+        }
+        const auto meet = [&] {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            barrier();
+        };
+        int32_t step = 0;
+        for (; step + 2 < steps; ++step) {
+            run(a, 0, step, true, false);
+            meet();
+            run(a, 1, step, true, true);
+        }
+        for (; step < steps; ++step) {
+            run(a, 0, step, true, false);
+            meet();
+            run(a, 1, step, step + 1 < steps, false);
+        }
+        if (kScaled) {
+            scales[t] = row_scale;
+            scales[256 + t] = row_bias;
+            scales[512 + t] = col_scale;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            barrier();
+        }
+        tile += workers;
+        const bool more = tile < all.first[2];
+        if (more) begin(tile);
+        // the compiler does not know that matrix instructions wrote these, and their results take a while
+#pragma unroll
+        for (int i = 0; i < FR; ++i)
+            asm volatile("s_nop 15" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]), "+a"(acc[i][4]), "+a"(acc[i][5]), "+a"(acc[i][6]), "+a"(acc[i][7]));
+        typedef typename Elem<OUT>::type T;
+        const bool wide = (a.ld_out * sizeof(T)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
+        const bool whole = wide && row0 + TR <= a.R && col0 + TC <= a.C;
+        const int32_t r = wr * FR * 16 + fk * 8, c = wc * FC * 16 + frow;
+#pragma unroll
+        for (int i = 0; i < FR / 2; ++i) {
+            float s[8], b[8];
+            if (kScaled)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 u = *(const f32x4 *)(scales + r + i * 32 + h * 4), v = *(const f32x4 *)(scales + 256 + r + i * 32 + h * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { s[h * 4 + e] = u[e]; b[h * 4 + e] = v[e]; }
+                }
+#pragma unroll
+            for (int j = 0; j < FC; ++j) {
+                const float qs = kScaled ? scales[512 + c + j * 16] : 0.0f;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = (float)acc[2 * i + (e >> 2)][j][e & 3];
+                    if (kScaled) v[e] = v[e] * (qs * s[e]) + b[e];
+                }
+                const int32_t row = row0 + r + i * 32, column = col0 + c + j * 16;
+                T *out = (T *)a.out + (int64_t)column * a.ld_out;
+                if (whole) Elem<OUT>::store(out + row, Elem<OUT>::pack(v));
+                else if (column < a.C && wide) store8<OUT, true>(out, row, a.R, v);
+                else if (column < a.C) store8<OUT, false>(out, row, a.R, v);
+            }
+        }
+        if (!more) return;
+        after = whole ? 32 : 0;
+        if (kScaled) barrier();                                         // (the scales are read before the next tile's are written)
     }
-    if (!half) __builtin_amdgcn_s_barrier();
-    __syncthreads();
-    put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, 0, lds + wave * 16 * (FR * 16 + 4) * 4);
 }
 
 // Adds up the splits in their order, four outputs per thread (one where rows of the sums do not start on 16-byte boundaries), the loads of
@@ -407,13 +505,19 @@ static hipError_t launch_as(const ProductArgs *a, int n, const ColumnSums &c, hi
     }
     all.first[2] = blocks;
     all.sums = c;
-    if (c.out) blocks += (int32_t)((c.n + 63) / 64);
+    all.sum_blocks = c.out ? (int32_t)((c.n + 63) / 64) : 0;
     if (n == 1) all.first[1] = all.first[2];
-    if (blocks == 0) return hipSuccess;
+    if (blocks + all.sum_blocks == 0) return hipSuccess;
+    if (whole) {
+        int device = 0;
+        if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+        blocks = std::min(blocks, (int32_t)device_cu_count(device));
+    }
+    blocks += all.sum_blocks;
     const auto kernel = whole ? product_kernel_256<OP, OUT> : product_kernel<OP, OUT, 4, 4>;
-    const int lds = 2 * 2 * tile * 128;
+    const int lds = 2 * 2 * tile * 128 + (whole ? 768 * 4 : 0);
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(whole ? 512 : 256), lds, s, all);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, s, all);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     return join_as<OP, OUT>(a, n, s);
 }
