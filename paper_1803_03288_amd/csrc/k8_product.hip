@@ -253,6 +253,28 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
     else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
 }
 
+// Lanes 16 g + n hold, of column `column` (n on from a multiple of 16), sixteen bytes `lo` at row `row` and sixteen `hi` STEP rows behind, the four g making
+// up 64 bytes, or every other sixteen of 128.  Columns n and n + 8 exchange a half, so that each store brings eight lanes' 128 bytes of a column: whole
+// lines, which stores past the caches need.  Through the caches the outputs (25 MB at least, where tiles of this size are taken) would drive out what
+// they hold of the operands: 8192 x 4096 x 16384 int8 to bf16, all values alike: 435 us through the caches, 400 past them in parts, 374 in lines;
+// with random values 494 and 465.
+__device__ __forceinline__ i32x4 i32x4_of(const float *v) { return __builtin_bit_cast(i32x4, (f32x4{v[0], v[1], v[2], v[3]})); }
+template <int STEP, typename T>
+__device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, int64_t ld, i32x4 lo, i32x4 hi)
+{
+    const bool first = (threadIdx.x & 8) == 0;
+    i32x4 a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t mine = first ? hi[e] : lo[e], other = __builtin_amdgcn_update_dpp(0, mine, 0x128, 0xf, 0xf, true);     // row_ror:8
+        a[e] = first ? lo[e] : other;
+        b[e] = first ? other : hi[e];
+    }
+    i32x4 *const to = (i32x4 *)(out + (int64_t)(first ? column : column - 8) * ld + row + (first ? 0 : STEP)), *const next = (i32x4 *)((T *)to + 8 * ld);
+    __builtin_nontemporal_store(a, to);
+    __builtin_nontemporal_store(b, next);
+}
+
 // Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each.  A step of 128 bytes has two halves of 64 matrix instructions; under
 // each half the operands of the next are read:
 //   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1:
@@ -371,6 +393,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
         const bool wide = (a.ld_out * sizeof(T)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
         const bool whole = wide && row0 + TR <= a.R && col0 + TC <= a.C;
         const int32_t r = wr * FR * 16 + fk * 8, c = wc * FC * 16 + frow;
+        T *const out = (T *)a.out;
+        i32x4 held[FC];                                                 // 16-bit outputs of the block before
 #pragma unroll
         for (int i = 0; i < FR / 2; ++i) {
             float s[8], b[8];
@@ -391,10 +415,17 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
                     if (kScaled) v[e] = v[e] * (qs * s[e]) + b[e];
                 }
                 const int32_t row = row0 + r + i * 32, column = col0 + c + j * 16;
-                T *out = (T *)a.out + (int64_t)column * a.ld_out;
-                if (whole) Elem<OUT>::store(out + row, Elem<OUT>::pack(v));
-                else if (column < a.C && wide) store8<OUT, true>(out, row, a.R, v);
-                else if (column < a.C) store8<OUT, false>(out, row, a.R, v);
+                if (!whole) {
+                    if (column >= a.C) continue;
+                    if (wide) store8<OUT, true>(out + (int64_t)column * a.ld_out, row, a.R, v);
+                    else store8<OUT, false>(out + (int64_t)column * a.ld_out, row, a.R, v);
+                } else if constexpr (OUT == TICTAC_F32) {
+                    put_lines<4>(out, row, column, a.ld_out, i32x4_of(v), i32x4_of(v + 4));
+                } else {
+                    const auto packed = Elem<OUT>::pack(v);
+                    if (i & 1) put_lines<32>(out, row - 32, column, a.ld_out, held[j], __builtin_bit_cast(i32x4, packed));
+                    else held[j] = __builtin_bit_cast(i32x4, packed);
+                }
             }
         }
         if (!more) return;
