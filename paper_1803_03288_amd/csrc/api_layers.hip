@@ -175,7 +175,8 @@ try {
     a.dtype = dtype; a.param_dtype = param_dtype; a.rows = rows; a.cols = cols; a.x = x; a.ld_x = ld_x; a.weight = weight;
     a.mean = const_cast<float *>(mean); a.rstd = const_cast<float *>(rstd);
     a.xq = const_cast<int8_t *>(xq); a.ld_xq = ld_xq; a.xs = const_cast<float *>(x_scale);
-    a.dy = dy; a.ld_dy = ld_dy; a.dx = dx; a.ld_dx = ld_dx; a.dweight = dweight; a.dbias = dbias; a.workspace = params ? workspace : nullptr;
+    a.dy = dy; a.ld_dy = ld_dy; a.dx = dx; a.ld_dx = ld_dx; a.dweight = dweight; a.dbias = dbias;
+    a.workspace = params && layer_norm_backward_workspace(rows, cols) ? workspace : nullptr;
     HIP_TRY(launch_layer_norm_backward(a, (hipStream_t)stream));
     return TICTAC_OK;
 } TT_CATCH

@@ -251,7 +251,7 @@ struct NormRow {                                    // eight columns of dy and o
 };
 
 template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
-__global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward_kernel(NormArgs p)
+__device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)          // the workgroups 0 .. blocks - 1
 {
     using T = typename Elem<DT>::type;
     constexpr int kRows = RowShape<THREADS>::kRows;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward
     __shared__ float join[kRows > 1 ? kRows * 2 * NC * THREADS * 8 : 1];
     RowReduce<THREADS> r{cells};
     const int t = threadIdx.x % THREADS;
-    const int64_t cols = p.cols, groups = (cols + 127) / 128, step = (int64_t)gridDim.x * kRows;
+    const int64_t cols = p.cols, groups = (cols + 127) / 128, step = (int64_t)blocks * kRows;
     const float per = 1.0f / (float)cols;
     float w[NC][8], dw[NC][8], db[NC][8];
 #pragma unroll
@@ -356,6 +356,46 @@ __device__ __forceinline__ void inputs8(const NormArgs &p, int64_t row, int64_t 
         r.load(p, row, col, groups);
         r.floats(mean, g, d);
     }
+}
+
+template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
+__global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward_kernel(NormArgs p)
+{
+    backward_rows<DT, WIDE, SAVED, THREADS, NC>(p, gridDim.x);
+}
+
+// Small inputs, which the caches hold: dx by a workgroup per row, and beside them workgroups of 16 columns that go over all rows again for dw and db.
+// One launch and no workspace, where the other form's second launch would cost as much again (77 x 1023: 8 us, 11.7 in two).
+constexpr int64_t kSmall = 1 << 19;                 // elements
+static bool is_small(int64_t rows, int64_t cols) { return rows * cols <= kSmall && rows <= 1024 && cols <= 8192; }
+
+template <int DT, bool WIDE, bool SAVED, int NC>
+__global__ __launch_bounds__(256) void layer_norm_backward_small_kernel(NormArgs p)
+{
+    if ((int64_t)blockIdx.x < p.rows) {
+        backward_rows<DT, WIDE, SAVED, 256, NC>(p, (int32_t)p.rows);
+        return;
+    }
+    using T = typename Elem<DT>::type;
+    __shared__ float sums[2][16][17];
+    const int c = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const int64_t col = ((int64_t)blockIdx.x - p.rows) * 16 + c, at = min(col, p.cols - 1), groups = (p.cols + 127) / 128;
+    float dw = 0.0f, db = 0.0f;
+#pragma unroll 4
+    for (int64_t row = slice; row < p.rows; row += 16) {
+        const float g = Elem<DT>::to_float(((const T *)p.dy)[row * p.ld_dy + at]), mean = p.mean[row];
+        const float d = SAVED ? fmaf((float)p.xq[row * p.ld_xq + at], p.xs[row * groups + (at >> 7)], -mean) : Elem<DT>::to_float(((const T *)p.x)[row * p.ld_x + at]) - mean;
+        dw = fmaf(g, d * p.rstd[row], dw);
+        db += g;
+    }
+    sums[0][slice][c] = dw;
+    sums[1][slice][c] = db;
+    __syncthreads();
+    if (slice || col >= p.cols) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) { dw += sums[0][k][c]; db += sums[1][k][c]; }
+    if (p.dweight) put_param(p.dweight, p.param_dtype, col, dw);
+    if (p.dbias) put_param(p.dbias, p.param_dtype, col, db);
 }
 
 // dx of rows of any length
@@ -457,10 +497,10 @@ static int64_t strips_of(int64_t rows, int64_t cols)
     const int64_t blocks = cols <= 1024 ? (rows + 3) / 4 : rows;
     return blocks < kStrips ? blocks : kStrips;
 }
-size_t layer_norm_backward_workspace(int64_t rows, int64_t cols) { return (size_t)strips_of(rows, cols) * 2 * cols * sizeof(float); }
+size_t layer_norm_backward_workspace(int64_t rows, int64_t cols) { return is_small(rows, cols) ? 0 : (size_t)strips_of(rows, cols) * 2 * cols * sizeof(float); }
 
 template <int DT, bool WIDE, bool SAVED>
-static void backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
+static void launch_backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
 {
     const int64_t c = p.cols;
     if (c <= 512) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 64, 1>), dim3(strips), dim3(256), 0, s, p);
@@ -471,18 +511,30 @@ static void backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
     else hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 1024, 2>), dim3(strips), dim3(1024), 0, s, p);
 }
 
+template <int DT, bool WIDE, bool SAVED>
+static hipError_t backward_small(const NormArgs &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.rows + (p.dweight || p.dbias ? (p.cols + 15) / 16 : 0)));
+    const auto kernel = p.cols <= 2048   ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 1>
+                        : p.cols <= 4096 ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 2>
+                                         : layer_norm_backward_small_kernel<DT, WIDE, SAVED, 4>;
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
 template <int DT, bool WIDE>
 static hipError_t backward(const NormArgs &p, hipStream_t s)
 {
+    if (p.rows && is_small(p.rows, p.cols)) return p.x ? backward_small<DT, WIDE, false>(p, s) : backward_small<DT, WIDE, true>(p, s);
     const unsigned strips = (unsigned)strips_of(p.rows, p.cols);
     if (!strips) {                                              // (no rows: the sums are zero)
     } else if (p.cols > kLongest) {
         if (p.dx) hipLaunchKernelGGL((norm_long_dx_kernel<DT, WIDE>), dim3(few(p.rows, 1 << 16)), dim3(1024), 0, s, p);
         if (p.workspace) hipLaunchKernelGGL((norm_long_params_kernel<DT, WIDE>), dim3((unsigned)((p.cols + 2047) / 2048), strips), dim3(256), 0, s, p);
     } else if (p.x) {
-        backward_rows<DT, WIDE, false>(p, strips, s);
+        launch_backward_rows<DT, WIDE, false>(p, strips, s);
     } else {
-        backward_rows<DT, WIDE, true>(p, strips, s);
+        launch_backward_rows<DT, WIDE, true>(p, strips, s);
     }
     if (p.dweight || p.dbias)
         hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(1024), 0, s, (int32_t)strips, p.cols, (const float *)p.workspace, p.dweight, p.dbias, p.param_dtype);

@@ -80,10 +80,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs p
     }
 }
 
-// Up to eight rows of floats, rounded to 8 bits here: every workgroup takes the largest magnitudes of the rows again (they come from the caches, under the
+// Up to sixteen rows of floats, rounded to 8 bits here: every workgroup takes the largest magnitudes of the rows again (they come from the caches, under the
 // first loads of the weights), which costs less than a launch before it while all rows are at most 64 KB (kOnceBytes).  1 x 4096 x 4096: 6 us; two launches
 // take 2.6 and 5.5 us and what lies between them.  The 8-bit values are those of quantize_rows_kernel.
-constexpr int kOnceWaves = 16, kOnceRows = 8;
+constexpr int kOnceWaves = 16, kOnceRows = 16;
 constexpr int64_t kOnceBytes = 64 << 10;
 
 template <int DT, bool WIDE>

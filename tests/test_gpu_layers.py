@@ -14,6 +14,8 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+from layer_calls import call
+
 F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
 TYPES = [F32, F16, BF16]
 U = 2.0 ** -24
@@ -466,9 +468,9 @@ def test_outputs_at_a_stride_leave_the_rest_alone(L):
         room = [torch.full((r, c + 9), 5.0, dtype=BF16, device="cuda") for r, c in ((rows, outs), (rows, cols), (outs, cols))]
         space = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
         s = binding._stream()
-        L._call("tictac_linear_q8", 2, rows, cols, outs, x.data_ptr(), cols, None, 0, None, w.q.data_ptr(), w.q.stride(0), w.scale.data_ptr(), 0, None,
+        call("tictac_linear_q8", 2, rows, cols, outs, x.data_ptr(), cols, None, 0, None, w.q.data_ptr(), w.q.stride(0), w.scale.data_ptr(), 0, None,
                 room[0].data_ptr() + 6, outs + 9, space.data_ptr(), space.numel(), s)
-        L._call("tictac_linear_q8_backward", 2, rows, cols, outs, dy.data_ptr(), outs, x8.q.data_ptr(), x8.q.stride(0), x8.scale.data_ptr(), w.q.data_ptr(),
+        call("tictac_linear_q8_backward", 2, rows, cols, outs, dy.data_ptr(), outs, x8.q.data_ptr(), x8.q.stride(0), x8.scale.data_ptr(), w.q.data_ptr(),
                 w.q.stride(0), w.scale.data_ptr(), room[1].data_ptr() + 6, cols + 9, room[2].data_ptr() + 6, cols + 9, None, space.data_ptr(), space.numel(), s)
         for t, want in zip(room, (y, dx, dw)):
             n = want.shape[1]
