@@ -194,15 +194,16 @@ static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
     return parts_along_k(blocks, units / (2 * kFewWaves), 256);              // two units for each wave at least
 }
 
-static size_t forward_parts(int64_t rows, int64_t cols, int64_t outs, int32_t *splits)
+static ProductPlan forward_plan(int64_t rows, int64_t cols, int64_t outs)
 {
-    *splits = rows <= kFewRows ? few_splits(rows, cols, outs) : product_splits((int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128));
-    return product_parts_bytes(*splits, (int32_t)outs, (int32_t)rows);
+    if (rows <= kFewRows) return {0, {few_splits(rows, cols, outs), 1}};
+    const ProductShape shape{(int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128)};
+    return plan_products(&shape, 1);
 }
 size_t linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
-    int32_t splits;
-    return (from_floats ? (size_t)rows * rows8_stride(cols) + ((size_t)rows * 4 + 255) / 256 * 256 : 0) + forward_parts(rows, cols, outs, &splits);
+    return (from_floats ? (size_t)rows * rows8_stride(cols) + ((size_t)rows * 4 + 255) / 256 * 256 : 0) +
+           product_parts_bytes(forward_plan(rows, cols, outs).splits[0], (int32_t)outs, (int32_t)rows);
 }
 
 hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
@@ -231,8 +232,9 @@ hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
     a.out = p.y; a.ld_out = p.ld_y; a.dtype = p.dtype;
     a.p_scale = p.ws; a.q_scale = xs; a.bias = p.bias; a.bias_dtype = p.bias_dtype;
     a.parts = room;
-    forward_parts(p.rows, p.cols, p.outs, &a.splits);
-    if (p.rows > kFewRows) return launch_product_i8(a, s);
+    const ProductPlan plan = forward_plan(p.rows, p.cols, p.outs);
+    a.splits = plan.splits[0];
+    if (p.rows > kFewRows) return launch_product_i8(a, plan.tile, s);
     const int32_t outs = 16 * few_blocks_of(p.rows);
     const dim3 grid((unsigned)((p.outs + outs - 1) / outs * a.splits)), block(kFewWaves * 64);
     const auto kernel = p.rows <= 8 ? linear_few_kernel<1, 1> : p.rows <= 16 ? linear_few_kernel<1, 2> : p.rows <= 32 ? linear_few_kernel<2, 4> : linear_few_kernel<4, 4>;
@@ -505,7 +507,7 @@ __device__ __forceinline__ void turn_rows8(int64_t rows, int64_t cols, const int
 }
 
 struct Operands {
-    int64_t units[3];                   // waves: up to here weights, activations, dy
+    int64_t units[4];                   // waves: up to here weights, activations, rows of dy, columns of dy
     uint16_t *p_x, *p_w, *q_x, *q_w;    // NULL: not needed
     float *sums;                        // [rows / 64][outs], may be NULL
     int64_t padded_o, padded_t;
@@ -529,8 +531,10 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
         turn_rows8<PIECES == 1>(p.rows, p.cols, p.xq, p.ld_xq, p.xs, to.p_w, to.padded_t, unit / wide * 64, unit % wide * 128);
         return;
     }
-    if (unit >= to.units[2]) return;
-    unit -= to.units[1];
+    if (unit >= to.units[3]) return;
+    // (rows and columns of dy by waves of their own: each is a chain of a thousand instructions where dy has several pieces)
+    const bool rows_only = unit < to.units[2];
+    unit -= rows_only ? to.units[1] : to.units[2];
     const int64_t tiles = (p.outs + 63) / 64, t0 = unit / tiles * 64, t = t0 + (lane & 7) * 8, o = unit % tiles * 64 + (lane >> 3) * 8;
     float v[8][8];                                              // [row][column]
 #pragma unroll
@@ -541,7 +545,7 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[e][i] = 0.0f;
     }
-    if (to.sums) {
+    if (to.sums && !rows_only) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float sum = 0.0f;
@@ -552,7 +556,7 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
             if ((lane & 7) == 0 && o + i < p.outs) to.sums[t0 / 64 * p.outs + o + i] = sum;
         }
     }
-    if (to.q_x) {
+    if (rows_only) {
         float s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = PIECES > 1 && o + i < p.outs ? p.ws[o + i] : 1.0f;
@@ -567,7 +571,7 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
                 *(i32x4 *)(to.q_x + ((t + e) * PIECES + k) * to.padded_o + o) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
         }
     }
-    if (to.q_w) {
+    if (to.q_w && !rows_only) {
         float s[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e] = PIECES > 1 ? p.xs[min(t + e, p.rows - 1)] : 1.0f;
@@ -587,7 +591,7 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
 // The workspace of one backward call.
 struct BackwardRoom {
     int64_t padded_o, padded_t;
-    int32_t splits_x, splits_w;
+    ProductPlan plan;                                       // dx, dw
     size_t sums, p_x, p_w, q_x, q_w, parts_x, parts_w, bytes;           // offsets
 };
 static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int64_t outs)
@@ -601,15 +605,15 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     }
     r.padded_o = (outs + 63) / 64 * 64;
     r.padded_t = (rows + 63) / 64 * 64;
-    r.splits_x = product_splits((int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces));
-    r.splits_w = product_splits((int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces));
+    const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces)}};
+    r.plan = plan_products(shapes, 2);
     r.p_x = r.sums + up((size_t)(r.padded_t / 64) * outs * 4);
     r.p_w = r.p_x + up((size_t)cols * r.padded_o * 2);
     r.q_x = r.p_w + up((size_t)cols * r.padded_t * 2);
     r.q_w = r.q_x + up((size_t)rows * r.padded_o * pieces * 2);
     r.parts_x = r.q_w + up((size_t)outs * r.padded_t * pieces * 2);
-    r.parts_w = r.parts_x + up(product_parts_bytes(r.splits_x, (int32_t)cols, (int32_t)rows));
-    r.bytes = r.parts_w + up(product_parts_bytes(r.splits_w, (int32_t)cols, (int32_t)outs));
+    r.parts_w = r.parts_x + up(product_parts_bytes(r.plan.splits[0], (int32_t)cols, (int32_t)rows));
+    r.bytes = r.parts_w + up(product_parts_bytes(r.plan.splits[1], (int32_t)cols, (int32_t)outs));
     return r;
 }
 size_t linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs) { return backward_room(dtype, rows, cols, outs).bytes; }
@@ -655,8 +659,10 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
     if (p.db) to.sums = (float *)(at + room.sums);
     to.units[0] = p.dx ? (p.cols + 127) / 128 * (room.padded_o / 64) : 0;
     to.units[1] = to.units[0] + (p.dw ? (p.cols + 127) / 128 * (room.padded_t / 64) : 0);
-    to.units[2] = to.units[1] + (to.q_x || to.q_w || to.sums ? (p.outs + 63) / 64 * (room.padded_t / 64) : 0);
-    hipLaunchKernelGGL((linear_operands_kernel<DT, WIDE>), dim3((unsigned)((to.units[2] + 3) / 4)), dim3(256), 0, s, p, to);
+    const int64_t tiles = (p.outs + 63) / 64 * (room.padded_t / 64);
+    to.units[2] = to.units[1] + (to.q_x ? tiles : 0);
+    to.units[3] = to.units[2] + (to.q_w || to.sums ? tiles : 0);
+    if (to.units[3]) hipLaunchKernelGGL((linear_operands_kernel<DT, WIDE>), dim3((unsigned)((to.units[3] + 3) / 4)), dim3(256), 0, s, p, to);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     ProductArgs a[2] = {};
     int n = 0;
@@ -669,7 +675,7 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
         x.R = (int32_t)p.cols;
         x.C = (int32_t)p.rows;
         x.p_steps = (int32_t)(room.padded_o / 64);
-        x.splits = room.splits_x;
+        x.splits = room.plan.splits[0];
         x.out = p.dx;
         x.ld_out = p.ld_dx;
         x.parts = at + room.parts_x;
@@ -683,7 +689,7 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
         w.R = (int32_t)p.cols;
         w.C = (int32_t)p.outs;
         w.p_steps = (int32_t)(room.padded_t / 64);
-        w.splits = room.splits_w;
+        w.splits = room.plan.splits[1];
         w.out = p.dw;
         w.ld_out = p.ld_dw;
         w.parts = at + room.parts_w;
@@ -693,7 +699,7 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
         a[i].dtype = DT;
     }
     const ColumnSums c{(const float *)(at + room.sums), room.padded_t / 64, p.outs, p.db, DT};
-    return launch_products_bf16(a, n, c, s);
+    return launch_products_bf16(a, n, room.plan.tile, c, s);
 }
 
 // No rows, or no outputs: what there is of the gradients is zero.
@@ -707,7 +713,7 @@ static hipError_t backward_nothing(const LinearArgs &p, hipStream_t s)
     a.out = p.rows ? p.dx : p.dw;
     a.ld_out = p.rows ? p.ld_dx : p.ld_dw;
     const ColumnSums c{nullptr, 0, p.outs, p.outs ? p.db : nullptr, p.dtype};
-    return launch_products_bf16(&a, a.out && a.C ? 1 : 0, c, s);
+    return launch_products_bf16(&a, a.out && a.C ? 1 : 0, 0, c, s);
 }
 
 hipError_t launch_linear_q8_backward(const LinearArgs &p, hipStream_t s)

@@ -34,10 +34,16 @@ struct ColumnSums {
     int32_t dtype;
 };
 
-int32_t product_splits(int32_t R, int32_t C, int32_t steps);
+// How the products of one launch are dealt to workgroups: the tile, and into how many parts each product's steps are cut.
+struct ProductShape { int32_t R, C, steps; };
+struct ProductPlan {
+    int32_t tile;               // one of kTiles, or kTile256
+    int32_t splits[2];
+};
+ProductPlan plan_products(const ProductShape *shapes, int n);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
-hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s);
-hipError_t launch_products_bf16(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s);     // one or two products, of one output type, in one launch
+hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s);
+hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s);     // one or two products, of one output type, in one launch
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s);        // the sums in `parts` to the output
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s);
 

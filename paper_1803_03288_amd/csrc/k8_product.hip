@@ -200,8 +200,9 @@ struct TileLoads {
     }
 };
 
-// A tile of 32 FR x 32 FC outputs by four waves, several workgroups per compute unit.
-template <class OP, int OUT, int FR, int FC>
+// A tile of 32 FR x 32 FC outputs by four waves, STAGES buffers in turn: while one step is computed from, up to STAGES - 1 are under way.  Two workgroups
+// fit a compute unit (kTiles).
+template <class OP, int OUT, int FR, int FC, int STAGES>
 __global__ __launch_bounds__(256) void product_kernel(Products all)
 {
     constexpr int TR = FR * 32, TC = FC * 32;
@@ -226,11 +227,18 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
 #pragma unroll
         for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
     const int frow = lane & 15, fk = lane >> 4;
-    if (first < last) loads.request(a, lds, wave);
+    constexpr int kLoads = TileLoads<TR, TC, 4, false>::LP + TileLoads<TR, TC, 4, false>::LQ;
+    for (int32_t step = first; step < last && step < first + STAGES - 1; ++step) loads.request(a, lds + (step - first) * (TR + TC) * 128, wave);
+    int buffer = 0;
     for (int32_t step = first; step < last; ++step) {
-        const int buffer = (step - first) & 1;
-        __syncthreads();                    // this step has come, and nobody reads the other buffer any more
-        if (step + 1 < last) loads.request(a, lds + (buffer ^ 1) * (TR + TC) * 128, wave);
+        // this step has come (of later ones' loads, up to STAGES - 2 steps may be under way), and nobody reads the buffer of the step before any more
+        const int32_t later = min(last - 1 - step, STAGES - 2);
+        if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (step + STAGES - 1 < last) loads.request(a, lds + (buffer ? buffer - 1 : STAGES - 1) * (TR + TC) * 128, wave);
         const char *tp = lds + buffer * (TR + TC) * 128 + (wr * FR * 16 + frow) * 128;
         const char *tq = lds + buffer * (TR + TC) * 128 + TR * 128 + (wc * FC * 16 + frow) * 128;
 #pragma unroll
@@ -246,6 +254,7 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
 #pragma unroll
                 for (int j = 0; j < FC; ++j) acc[i][j] = OP::mma(fp[i], fq[j], acc[i][j]);
         }
+        buffer = buffer + 1 < STAGES ? buffer + 1 : 0;
     }
     __syncthreads();
     char *room = lds + wave * 16 * (FR * 16 + 4) * 4;
@@ -502,36 +511,70 @@ static hipError_t join_as(const ProductArgs *a, int n, hipStream_t s)
     return hipGetLastError();
 }
 
-constexpr int32_t kSmallTile = 128;
+// The tiles by rows x columns of 32, and what a workgroup takes, in us: `fixed`, and per step with one workgroup per compute unit and (both of them
+// together) with two.  Measured with int8 on 256, 512 and 1024 workgroups of 2 to 64 steps: 128 x 128 on 256 workgroups 7.9 us for two steps and 45 for 64,
+// 128 x 64 5.7 and 32, 64 x 64 4.7 and 22; on 512 9.8 and 69, 7.1 and 44, 5.6 and 31.
+struct Tile { int32_t r, c; float fixed, step, step2; };
+constexpr Tile kTiles[] = {{4, 4, 7.0f, 0.6f, 0.95f}, {4, 2, 5.0f, 0.41f, 0.59f}, {2, 2, 4.2f, 0.28f, 0.4f}};
+constexpr int32_t kTile256 = 3;
 
-int32_t product_splits(int32_t R, int32_t C, int32_t steps)
+ProductPlan plan_products(const ProductShape *shapes, int n)
 {
-    const int64_t tiles = (int64_t)((R + kSmallTile - 1) / kSmallTile) * ((C + kSmallTile - 1) / kSmallTile);
-    if (tiles == 0 || tiles >= 256) return 1;
-    int64_t n = 512 / tiles;                            // two workgroups of small tiles per compute unit
-    if (n > steps / 4) n = steps / 4;                   // four steps at least for each
-    return (int32_t)(n < 1 ? 1 : n > 16 ? 16 : n);
+    ProductPlan best{0, {1, 1}};
+    float least = 1e30f;
+    const auto take = [&](int32_t tile, const int32_t (&splits)[2], float us) {
+        if (us >= least) return;
+        least = us;
+        best.tile = tile;
+        best.splits[0] = splits[0];
+        best.splits[1] = splits[1];
+    };
+    for (int32_t tile = 0; tile < kTile256; ++tile) {
+        const Tile &t = kTiles[tile];
+        int64_t tiles[2] = {0, 0};
+        for (int i = 0; i < n; ++i) tiles[i] = (int64_t)((shapes[i].R + 32 * t.r - 1) / (32 * t.r)) * ((shapes[i].C + 32 * t.c - 1) / (32 * t.c));
+        for (int32_t most = 1 << 30; most >= 2; most = most > 64 ? 64 : most / 2) {         // steps of a workgroup
+            int32_t splits[2] = {1, 1};
+            int64_t blocks = 0;
+            float steps = 0.0f, us = 0.0f;
+            for (int i = 0; i < n; ++i) {
+                splits[i] = std::min(16, std::max(1, (shapes[i].steps + most - 1) / most));
+                blocks += tiles[i] * splits[i];
+                steps = std::max(steps, (float)shapes[i].steps / (float)splits[i]);
+                if (splits[i] > 1) us += 1.0f + (float)splits[i] * (float)shapes[i].R * (float)shapes[i].C * (8.0f / 4.5e6f);       // written and read again
+            }
+            for (int i = 0; i < n; ++i)
+                if (splits[i] > 1) { us += 2.0f; break; }                                   // the launch that adds them up
+            const float per_cu = (float)((blocks + 255) / 256);
+            us += per_cu <= 1.0f ? t.fixed + t.step * steps : t.fixed * (0.5f + 0.35f * per_cu) + t.step2 * steps * per_cu * 0.5f;
+            take(tile, splits, us);
+        }
+    }
+    // tiles of 256 x 256, one workgroup per compute unit from tile to tile: 1.45 us a step, 6 us a tile besides
+    float us = 4.0f, steps = 0.0f;
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        tiles += (int64_t)((shapes[i].R + 255) / 256) * ((shapes[i].C + 255) / 256);
+        steps = std::max(steps, (float)shapes[i].steps);
+    }
+    us += (float)((tiles + 255) / 256) * (6.0f + 1.45f * steps);
+    take(kTile256, {1, 1}, us);
+    return best;
 }
 
 template <class OP, int OUT>
-static hipError_t launch_as(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s)
+static hipError_t launch_as(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s)
 {
     Products all{};
-    int64_t big = 0;
-    bool whole = true;
-    for (int i = 0; i < n; ++i) {
-        big += (int64_t)((a[i].R + 255) / 256) * ((a[i].C + 255) / 256);
-        whole &= a[i].splits <= 1;
-    }
-    whole &= big >= 192;
-    const int32_t tile = whole ? 256 : kSmallTile;
+    const bool large = tile == kTile256;
+    const int32_t tr = large ? 256 : 32 * kTiles[tile].r, tc = large ? 256 : 32 * kTiles[tile].c;
     int32_t blocks = 0;
     for (int i = 0; i < 2; ++i) {
         all.first[i] = blocks;
         if (i >= n) continue;
         all.a[i] = a[i];
-        all.tiles_r[i] = (a[i].R + tile - 1) / tile;
-        all.tiles_c[i] = (a[i].C + tile - 1) / tile;
+        all.tiles_r[i] = (a[i].R + tr - 1) / tr;
+        all.tiles_c[i] = (a[i].C + tc - 1) / tc;
         blocks += all.tiles_r[i] * all.tiles_c[i] * a[i].splits;
     }
     all.first[2] = blocks;
@@ -539,14 +582,15 @@ static hipError_t launch_as(const ProductArgs *a, int n, const ColumnSums &c, hi
     all.sum_blocks = c.out ? (int32_t)((c.n + 63) / 64) : 0;
     if (n == 1) all.first[1] = all.first[2];
     if (blocks + all.sum_blocks == 0) return hipSuccess;
-    if (whole) {
+    if (large) {
         int device = 0;
         if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
         blocks = std::min(blocks, (int32_t)device_cu_count(device));
     }
     blocks += all.sum_blocks;
-    const auto kernel = whole ? product_kernel_256<OP, OUT> : product_kernel<OP, OUT, 4, 4>;
-    const int lds = 2 * 2 * tile * 128 + (whole ? 768 * 4 : 0);
+    // LDS: the buffers of a step's operands; for the outputs they are enough too
+    const auto kernel = large ? product_kernel_256<OP, OUT> : tile == 0 ? product_kernel<OP, OUT, 4, 4, 2> : tile == 1 ? product_kernel<OP, OUT, 4, 2, 3> : product_kernel<OP, OUT, 2, 2, 4>;
+    const int lds = large ? 2 * 512 * 128 + 768 * 4 : (tile == 0 ? 2 : tile == 1 ? 3 : 4) * (tr + tc) * 128;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, s, all);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -554,11 +598,11 @@ static hipError_t launch_as(const ProductArgs *a, int n, const ColumnSums &c, hi
 }
 
 template <class OP>
-static hipError_t launch(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s)
+static hipError_t launch(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s)
 {
     const int32_t dt = n ? a[0].dtype : c.dtype;
-    if (dt == TICTAC_F32) return launch_as<OP, TICTAC_F32>(a, n, c, s);
-    return dt == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, n, c, s) : launch_as<OP, TICTAC_BF16>(a, n, c, s);
+    if (dt == TICTAC_F32) return launch_as<OP, TICTAC_F32>(a, n, tile, c, s);
+    return dt == TICTAC_F16 ? launch_as<OP, TICTAC_F16>(a, n, tile, c, s) : launch_as<OP, TICTAC_BF16>(a, n, tile, c, s);
 }
 
 template <class OP>
@@ -570,7 +614,7 @@ static hipError_t join(const ProductArgs &a, hipStream_t s)
 
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8>(a, s); }
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s) { return join<OpBf16>(a, s); }
-hipError_t launch_product_i8(const ProductArgs &a, hipStream_t s) { return launch<OpI8>(&a, 1, ColumnSums{}, s); }
-hipError_t launch_products_bf16(const ProductArgs *a, int n, const ColumnSums &c, hipStream_t s) { return launch<OpBf16>(a, n, c, s); }
+hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s) { return launch<OpI8>(&a, 1, tile, ColumnSums{}, s); }
+hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s) { return launch<OpBf16>(a, n, tile, c, s); }
 
 }  // namespace tictac
