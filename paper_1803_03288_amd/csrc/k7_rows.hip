@@ -43,34 +43,49 @@ __global__ __launch_bounds__(256) void quantize_groups_kernel(QuantizeArgs p, in
     }
 }
 
-// A scale per row, a workgroup per row: the row is read twice, the second time from the caches.
-template <int DT, bool WIDE, int THREADS>
+// A scale per row, a workgroup per row, which stays in registers: NC pieces of eight elements per thread.  Longer rows (NC = 0) are read twice.
+template <int DT, bool WIDE, int THREADS, int NC>
 __global__ __launch_bounds__(THREADS) void quantize_rows_kernel(QuantizeArgs p)
 {
     using E = Elem<DT>;
-    __shared__ uint32_t part[THREADS / 64];
+    __shared__ uint32_t part[2][THREADS / 64];          // (two sets in turn: one barrier a row)
     const int64_t padded = (p.cols + 127) / 128 * 128;
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, turn ^= 1) {
         const typename E::type *x = (const typename E::type *)p.x + row * p.ld_x;
+        typename E::raw raw[NC ? NC : 1];
         uint32_t m = 0;
-        for (int64_t col = threadIdx.x * 8; col < p.cols; col += THREADS * 8) {
+        const auto largest = [&](const typename E::raw &r) {
             float v[8];
-            E::floats(load8<DT, WIDE>(x, col, p.cols), v);
+            E::floats(r, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+        };
+        if (NC) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) raw[j] = load8<DT, WIDE>(x, (int64_t)(j * THREADS + threadIdx.x) * 8, p.cols);
+#pragma unroll
+            for (int j = 0; j < NC; ++j) largest(raw[j]);
+        } else {
+            for (int64_t col = threadIdx.x * 8; col < p.cols; col += THREADS * 8) largest(load8<DT, WIDE>(x, col, p.cols));
         }
         m = wave_max_u32(m);
-        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+        if ((threadIdx.x & 63) == 0) part[turn][threadIdx.x >> 6] = m;
         __syncthreads();
         m = 0;
 #pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) m = max(m, part[i]);
+        for (int i = 0; i < THREADS / 64; ++i) m = max(m, part[turn][i]);
         const RowScale s = row_scale(m);
-        __syncthreads();
-        for (int64_t col = threadIdx.x * 8; col < padded; col += THREADS * 8) {
+        const auto put = [&](const typename E::raw &r, int64_t col) {
             float v[8];
-            E::floats(load8<DT, WIDE>(x, col, p.cols), v);
-            *(uint2 *)(p.q + row * p.ld_q + col) = quantized8(v, s);
+            E::floats(r, v);
+            if (col < padded) *(uint2 *)(p.q + row * p.ld_q + col) = quantized8(v, s);
+        };
+        if (NC) {
+#pragma unroll
+            for (int j = 0; j < NC; ++j) put(raw[j], (int64_t)(j * THREADS + threadIdx.x) * 8);
+        } else {
+            for (int64_t col = threadIdx.x * 8; col < padded; col += THREADS * 8) put(load8<DT, WIDE>(x, col, p.cols), col);
         }
         if (threadIdx.x == 0) p.scale[row] = s.scale;
     }
@@ -117,9 +132,13 @@ static hipError_t quantize(const QuantizeArgs &p, hipStream_t s)
         hipLaunchKernelGGL((quantize_groups_kernel<DT, WIDE>), dim3(elementwise_blocks((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, groups, total);
     } else {
         const dim3 grid((unsigned)(p.rows < (1 << 20) ? p.rows : (1 << 20)));
-        // few long rows leave most of the chip idle: as many loads under way as a workgroup can have
-        if (p.rows <= 512 && p.cols > 2048) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 1024>), grid, dim3(1024), 0, s, p);
-        else hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 256>), grid, dim3(256), 0, s, p);
+        // few long rows leave most of the chip idle: as many threads for each as a workgroup can have
+        const int64_t c = p.cols;
+        if (c <= 2048) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 256, 1>), grid, dim3(256), 0, s, p);
+        else if (c <= 8192 && p.rows <= 512) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 1024, 1>), grid, dim3(1024), 0, s, p);
+        else if (c <= 8192) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 256, 4>), grid, dim3(256), 0, s, p);
+        else if (c <= 32768) hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 1024, 4>), grid, dim3(1024), 0, s, p);
+        else hipLaunchKernelGGL((quantize_rows_kernel<DT, WIDE, 1024, 0>), grid, dim3(1024), 0, s, p);
     }
     return hipGetLastError();
 }

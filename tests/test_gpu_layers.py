@@ -86,7 +86,7 @@ def rows8_values(r):
 
 @pytest.mark.parametrize("group", [0, 128])
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 127), (2, 128), (33, 129), (17, 1000), (4, 2049), (300, 256), (3, 20000)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (5, 127), (2, 128), (33, 129), (17, 1000), (4, 2049), (300, 256), (3, 20000), (2, 40000)])
 def test_rows_in_8_bits(L, rows, cols, dtype, group):
     g = gen(rows * 1000 + cols)
     x = values(g, rows, cols, dtype)
