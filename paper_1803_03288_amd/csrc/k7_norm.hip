@@ -366,23 +366,24 @@ __global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward
 
 // Small inputs, which the caches hold: dx by a workgroup per row, and beside them workgroups of 16 columns that go over all rows again for dw and db.
 // One launch and no workspace, where the other form's second launch would cost as much again (77 x 1023: 8 us, 11.7 in two).
-constexpr int64_t kSmall = 1 << 19;                 // elements
-static bool is_small(int64_t rows, int64_t cols) { return rows * cols <= kSmall && rows <= 1024 && cols <= 8192; }
+constexpr int64_t kSmall = 1 << 21;                 // elements
+static bool is_small(int64_t rows, int64_t cols) { return rows * cols <= kSmall && rows <= 1024 && cols <= kLongest; }
 
-template <int DT, bool WIDE, bool SAVED, int NC>
-__global__ __launch_bounds__(256) void layer_norm_backward_small_kernel(NormArgs p)
+template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
+__global__ __launch_bounds__(THREADS) void layer_norm_backward_small_kernel(NormArgs p)
 {
     if ((int64_t)blockIdx.x < p.rows) {
-        backward_rows<DT, WIDE, SAVED, 256, NC>(p, (int32_t)p.rows);
+        backward_rows<DT, WIDE, SAVED, THREADS, NC>(p, (int32_t)p.rows);
         return;
     }
     using T = typename Elem<DT>::type;
-    __shared__ float sums[2][16][17];
+    constexpr int kSlices = THREADS / 16;
+    __shared__ float sums[2][kSlices][17];
     const int c = threadIdx.x & 15, slice = threadIdx.x >> 4;
     const int64_t col = ((int64_t)blockIdx.x - p.rows) * 16 + c, at = min(col, p.cols - 1), groups = (p.cols + 127) / 128;
     float dw = 0.0f, db = 0.0f;
-#pragma unroll 4
-    for (int64_t row = slice; row < p.rows; row += 16) {
+#pragma unroll 8
+    for (int64_t row = slice; row < p.rows; row += kSlices) {
         const float g = Elem<DT>::to_float(((const T *)p.dy)[row * p.ld_dy + at]), mean = p.mean[row];
         const float d = SAVED ? fmaf((float)p.xq[row * p.ld_xq + at], p.xs[row * groups + (at >> 7)], -mean) : Elem<DT>::to_float(((const T *)p.x)[row * p.ld_x + at]) - mean;
         dw = fmaf(g, d * p.rstd[row], dw);
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(256) void layer_norm_backward_small_kernel(NormArgs
     __syncthreads();
     if (slice || col >= p.cols) return;
 #pragma unroll
-    for (int k = 1; k < 16; ++k) { dw += sums[0][k][c]; db += sums[1][k][c]; }
+    for (int k = 1; k < kSlices; ++k) { dw += sums[0][k][c]; db += sums[1][k][c]; }
     if (p.dweight) put_param(p.dweight, p.param_dtype, col, dw);
     if (p.dbias) put_param(p.dbias, p.param_dtype, col, db);
 }
@@ -459,8 +460,18 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(int32_t strips, int64
     const int64_t at = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
     const int wave = threadIdx.x >> 6, per = (strips + 15) / 16;
     float sum = 0.0f;
-    if (at < 2 * cols)
-        for (int k = wave * per; k < min(strips, (wave + 1) * per); ++k) sum += part[(int64_t)k * 2 * cols + at];
+    if (at < 2 * cols) {
+        int k = wave * per;
+        const int last = min(strips, (wave + 1) * per);
+        for (; k + 8 <= last; k += 8) {                         // (eight loads under way)
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = part[(int64_t)(k + i) * 2 * cols + at];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        for (; k < last; ++k) sum += part[(int64_t)k * 2 * cols + at];
+    }
     sums[wave][threadIdx.x & 63] = sum;
     __syncthreads();
     if (wave || at >= 2 * cols) return;
@@ -515,10 +526,12 @@ template <int DT, bool WIDE, bool SAVED>
 static hipError_t backward_small(const NormArgs &p, hipStream_t s)
 {
     const dim3 grid((unsigned)(p.rows + (p.dweight || p.dbias ? (p.cols + 15) / 16 : 0)));
-    const auto kernel = p.cols <= 2048   ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 1>
-                        : p.cols <= 4096 ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 2>
-                                         : layer_norm_backward_small_kernel<DT, WIDE, SAVED, 4>;
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p);
+    // more threads for longer rows, and for the columns of many rows
+    const bool many = p.cols > 2048 || p.rows > 256;
+    const auto kernel = !many            ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 256, 1>
+                        : p.cols <= 8192 ? layer_norm_backward_small_kernel<DT, WIDE, SAVED, 1024, 1>
+                                         : layer_norm_backward_small_kernel<DT, WIDE, SAVED, 1024, 2>;
+    hipLaunchKernelGGL(kernel, grid, dim3(many ? 1024 : 256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -95,6 +95,17 @@ struct Elem<TICTAC_BF16> {
     static __device__ __forceinline__ __bf16 from_float(float x) { return (__bf16)x; }
 };
 
+// Eight elements anywhere in memory: the same loads and stores, which this GPU does at any boundary of an element.
+template <int DT>
+__device__ __forceinline__ typename Elem<DT>::raw load_anywhere(const typename Elem<DT>::type *p)
+{
+    typename Elem<DT>::raw r;
+    __builtin_memcpy(&r, p, sizeof(r));
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ void store_anywhere(typename Elem<DT>::type *p, const typename Elem<DT>::raw &r) { __builtin_memcpy(p, &r, sizeof(r)); }
+
 // Elements `col` .. `col` + 7 of a row of `cols`, zeros behind its end.  WIDE: rows start on 16-byte boundaries and hold a multiple of
 // eight elements.
 template <int DT, bool WIDE>
@@ -105,6 +116,7 @@ __device__ __forceinline__ typename Elem<DT>::raw load8(const typename Elem<DT>:
         if (col < cols) return E::load(row + col);
         return typename E::raw{};
     }
+    if (col + 8 <= cols) return load_anywhere<DT>(row + col);
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -128,6 +140,10 @@ __device__ __forceinline__ void store8(typename Elem<DT>::type *row, int64_t col
     using E = Elem<DT>;
     if (WIDE) {
         if (col < cols) E::store(row + col, E::pack(v));
+        return;
+    }
+    if (col + 8 <= cols) {
+        store_anywhere<DT>(row + col, E::pack(v));
         return;
     }
 #pragma unroll
