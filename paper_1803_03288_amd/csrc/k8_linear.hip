@@ -107,22 +107,23 @@ __global__ __launch_bounds__(kOnceWaves * 64) void linear_once_kernel(LinearArgs
                 next[n][k] = u + n * kOnceWaves < units ? *(const i32x4 *)(w + (int64_t)(u + n * kOnceWaves) * 128 + k * 64) : i32x4{};
     };
     request(wave);
-    for (int t = 0; t < rows; ++t) {
+    // each row's largest magnitude by 16 / rows waves
+    const int each = rows <= 1 ? 16 : rows <= 2 ? 8 : rows <= 4 ? 4 : rows <= 8 ? 2 : 1, of = wave / each, piece = wave % each;
+    if (of < rows) {
         uint32_t m = 0;
-        for (int64_t col = threadIdx.x * 8; col < p.cols; col += kOnceWaves * 512) {
+        for (int64_t col = piece * 512 + lane * 8; col < p.cols; col += each * 512) {
             float v[8];
-            E::floats(load8<DT, WIDE>((const T *)p.x + t * p.ld_x, col, p.cols), v);
+            E::floats(load8<DT, WIDE>((const T *)p.x + of * p.ld_x, col, p.cols), v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
         }
         m = wave_max_u32(m);
-        if (lane == 0) part[t][wave] = m;
+        if (lane == 0) part[of][piece] = m;
     }
     __syncthreads();
     const int mine = min(row, rows - 1);
     uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < kOnceWaves; ++i) m = max(m, part[mine][i]);
+    for (int i = 0; i < each; ++i) m = max(m, part[mine][i]);
     const RowScale scale = row_scale(m);
     const T *x = (const T *)p.x + mine * p.ld_x;
     i32x4 acc{};
@@ -154,8 +155,7 @@ __global__ __launch_bounds__(kOnceWaves * 64) void linear_once_kernel(LinearArgs
 #pragma unroll
     for (int k = 0; k < kOnceWaves; ++k) sum += sums[k][(o >> 2) * 16 + t][o & 3];
     m = 0;
-#pragma unroll
-    for (int i = 0; i < kOnceWaves; ++i) m = max(m, part[t][i]);
+    for (int i = 0; i < each; ++i) m = max(m, part[t][i]);
     float v = (float)sum * (row_scale(m).scale * p.ws[o0 + o]);
     if (p.bias) v += param(p.bias, p.bias_dtype, o0 + o);
     put_param(p.y, p.dtype, t * p.ld_y + o0 + o, v);
@@ -187,11 +187,12 @@ static int32_t parts_along_k(int64_t blocks, int64_t most, int64_t room)
 }
 
 constexpr int64_t kFewRows = 64;
-static int32_t few_blocks_of(int64_t rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }       // FB: x at most half of the weights' bytes, up to 32 rows
+// FB: x at most half of the weights' bytes, up to 32 rows; with few outputs a workgroup for each 16 (x then is read few times, and the chip is idle)
+static int32_t few_blocks_of(int64_t rows, int64_t outs) { return rows <= 8 || outs <= 2048 ? 1 : rows <= 16 ? 2 : 4; }
 static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
 {
-    const int64_t blocks = (outs + 16 * few_blocks_of(rows) - 1) / (16 * few_blocks_of(rows)), units = (cols + 127) / 128;
-    return parts_along_k(blocks, units / (2 * kFewWaves), 256);              // two units for each wave at least
+    const int64_t each = 16 * few_blocks_of(rows, outs), blocks = (outs + each - 1) / each, units = (cols + 127) / 128;
+    return parts_along_k(blocks, units / kFewWaves, 256);                   // a unit for each wave at least
 }
 
 static ProductPlan forward_plan(int64_t rows, int64_t cols, int64_t outs)
@@ -235,9 +236,11 @@ hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
     const ProductPlan plan = forward_plan(p.rows, p.cols, p.outs);
     a.splits = plan.splits[0];
     if (p.rows > kFewRows) return launch_product_i8(a, plan.tile, s);
-    const int32_t outs = 16 * few_blocks_of(p.rows);
+    const int32_t fb = few_blocks_of(p.rows, p.outs), outs = 16 * fb;
     const dim3 grid((unsigned)((p.outs + outs - 1) / outs * a.splits)), block(kFewWaves * 64);
-    const auto kernel = p.rows <= 8 ? linear_few_kernel<1, 1> : p.rows <= 16 ? linear_few_kernel<1, 2> : p.rows <= 32 ? linear_few_kernel<2, 4> : linear_few_kernel<4, 4>;
+    const auto kernel = p.rows <= 16   ? (fb == 1 ? linear_few_kernel<1, 1> : linear_few_kernel<1, 2>)
+                        : p.rows <= 32 ? (fb == 1 ? linear_few_kernel<2, 1> : linear_few_kernel<2, 4>)
+                                       : (fb == 1 ? linear_few_kernel<4, 1> : linear_few_kernel<4, 4>);
     hipLaunchKernelGGL(kernel, grid, block, 0, s, p, xq, ld_xq, xs, a.splits, (int32_t *)room);
     return a.splits > 1 ? launch_product_join_i8(a, s) : hipGetLastError();
 }
@@ -464,7 +467,7 @@ static int32_t dx_few_words(int64_t rows) { return rows <= 32 ? 4 : 2; }
 static int32_t dx_few_splits(int64_t rows, int64_t cols, int64_t outs)
 {
     const int64_t wide = 64 * dx_few_words(rows), blocks = (cols + wide - 1) / wide, units = (outs + 31) / 32;
-    return parts_along_k(blocks, units / (2 * kBackWaves), 256);             // two blocks of k for each wave at least
+    return parts_along_k(blocks, units / kBackWaves, 256);                  // a block of k for each wave at least
 }
 
 // ---- backward with more rows: operands with k contiguous, for the tiles of k8_product.hip ----

@@ -200,13 +200,15 @@ struct TileLoads {
     }
 };
 
-// A tile of 32 FR x 32 FC outputs by four waves, STAGES buffers in turn: while one step is computed from, up to STAGES - 1 are under way.  Two workgroups
-// fit a compute unit (kTiles).
+// A tile of 32 FR x 32 FC outputs by four waves, STAGES buffers in turn, two workgroups per compute unit where they fit (kTiles).  A step has two halves; under the
+// matrix instructions of each the operands of the next are read:
+//   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1;
+//   - half 1 of step t reads the first half of step t + 1 and asks for step t + STAGES, into the buffer of step t.
 template <class OP, int OUT, int FR, int FC, int STAGES>
-__global__ __launch_bounds__(256) void product_kernel(Products all)
+__global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_kernel(Products all)
 {
-    constexpr int TR = FR * 32, TC = FC * 32;
-    extern __shared__ char lds[];                                       // [2][TR + TC][128]
+    constexpr int TR = FR * 32, TC = FC * 32, kBuffer = (TR + TC) * 128, kMma = FR * FC, kReads = FR + FC;
+    extern __shared__ char lds[];                                       // [STAGES][TR + TC][128]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if ((int32_t)blockIdx.x >= all.first[2]) {                          // (a workgroup per tile)
         column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
@@ -218,43 +220,65 @@ __global__ __launch_bounds__(256) void product_kernel(Products all)
     tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
     const int32_t r0 = tr * TR, c0 = tc * TC;
     const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
-    TileLoads<TR, TC, 4, false> loads;
+    typedef TileLoads<TR, TC, 4, false> Loads;
+    constexpr int kLoads = Loads::LP + Loads::LQ;
+    Loads loads;
     loads.init(a, r0, c0, first, wave);
-    const int wr = wave & 1, wc = wave >> 1;
+    const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
+    const char *const tp = lds + (wr * FR * 16 + frow) * 128, *const tq = lds + TR * 128 + (wc * FC * 16 + frow) * 128;
     typename OP::acc acc[FR][FC];
 #pragma unroll
     for (int i = 0; i < FR; ++i)
 #pragma unroll
         for (int j = 0; j < FC; ++j) acc[i][j] = typename OP::acc{};
-    const int frow = lane & 15, fk = lane >> 4;
-    constexpr int kLoads = TileLoads<TR, TC, 4, false>::LP + TileLoads<TR, TC, 4, false>::LQ;
-    for (int32_t step = first; step < last && step < first + STAGES - 1; ++step) loads.request(a, lds + (step - first) * (TR + TC) * 128, wave);
-    int buffer = 0;
-    for (int32_t step = first; step < last; ++step) {
-        // this step has come (of later ones' loads, up to STAGES - 2 steps may be under way), and nobody reads the buffer of the step before any more
-        const int32_t later = min(last - 1 - step, STAGES - 2);
-        if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    i32x4 fp[2][FR], fq[2][FC];
+    const auto read_one = [&](int half, int n, int place) {
+        if (n < FC) fq[half][n] = *(const i32x4 *)(tq + n * 2048 + place);
+        else fp[half][n - FC] = *(const i32x4 *)(tp + (n - FC) * 2048 + place);
+    };
+    // the wait for a step's loads, with `later` steps' behind them under way
+    const auto arrived = [&](int32_t later) {
+        if (STAGES > 3 && later >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kLoads) : "memory");
+        else if (STAGES > 2 && later == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");                                  // (nothing is read before the barrier)
+    };
+    const auto run = [&](int half, int place, bool read, bool ask, char *to) {
+#pragma unroll
+        for (int m = 0; m < kMma; ++m) {
+            if (read)
+#pragma unroll
+                for (int n = m * kReads / kMma; n < (m + 1) * kReads / kMma; ++n) read_one(half ^ 1, n, place);
+            if (ask)
+#pragma unroll
+                for (int n = m * kLoads / kMma; n < (m + 1) * kLoads / kMma; ++n) loads.request_one(a, to, wave, n);
+            acc[m / FC][m % FC] = OP::mma(fp[half][m / FC], fq[half][m % FC], acc[m / FC][m % FC]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ask) loads.next(a);
+    };
+    if (first < last) {
+        for (int32_t step = first; step < last && step < first + STAGES; ++step) loads.request(a, lds + (step - first) * kBuffer, wave);
+        const int32_t later = min(last - 1 - first, STAGES - 1);
+        if (STAGES > 3 && later >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kLoads) : "memory");
+        else if (STAGES > 2 && later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        else if (later >= 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (step + STAGES - 1 < last) loads.request(a, lds + (buffer ? buffer - 1 : STAGES - 1) * (TR + TC) * 128, wave);
-        const char *tp = lds + buffer * (TR + TC) * 128 + (wr * FR * 16 + frow) * 128;
-        const char *tq = lds + buffer * (TR + TC) * 128 + TR * 128 + (wc * FC * 16 + frow) * 128;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int place = ((k * 4 + fk) ^ (frow & 7)) * 16;
-            i32x4 fp[FR], fq[FC];
-#pragma unroll
-            for (int j = 0; j < FC; ++j) fq[j] = *(const i32x4 *)(tq + j * 2048 + place);
-#pragma unroll
-            for (int i = 0; i < FR; ++i) fp[i] = *(const i32x4 *)(tp + i * 2048 + place);
-#pragma unroll
-            for (int i = 0; i < FR; ++i)
-#pragma unroll
-                for (int j = 0; j < FC; ++j) acc[i][j] = OP::mma(fp[i], fq[j], acc[i][j]);
-        }
-        buffer = buffer + 1 < STAGES ? buffer + 1 : 0;
+        for (int n = 0; n < kReads; ++n) read_one(0, n, (fk ^ swizzle) * 16);
+    }
+    int buffer = 0;
+    for (int32_t step = first; step < last; ++step) {
+        const int next = buffer + 1 < STAGES ? buffer + 1 : 0;
+        run(0, buffer * kBuffer + ((4 + fk) ^ swizzle) * 16, true, false, nullptr);
+        arrived(min(last - 2 - step, STAGES - 2));
+        const int place = next * kBuffer + (fk ^ swizzle) * 16;
+        if (step + STAGES < last) run(1, place, true, true, lds + buffer * kBuffer);
+        else run(1, place, step + 1 < last, false, nullptr);
+        buffer = next;
     }
     __syncthreads();
     char *room = lds + wave * 16 * (FR * 16 + 4) * 4;
@@ -512,10 +536,11 @@ static hipError_t join_as(const ProductArgs *a, int n, hipStream_t s)
 }
 
 // The tiles by rows x columns of 32, and what a workgroup takes, in us: `fixed`, and per step with one workgroup per compute unit and (both of them
-// together) with two.  Measured with int8 on 256, 512 and 1024 workgroups of 2 to 64 steps: 128 x 128 on 256 workgroups 7.9 us for two steps and 45 for 64,
-// 128 x 64 5.7 and 32, 64 x 64 4.7 and 22; on 512 9.8 and 69, 7.1 and 44, 5.6 and 31.
+// together) with two.  Measured with int8 on 256, 512 and 1024 workgroups of 2 to 64 steps: 128 x 128 on 256 workgroups 8.7 us for two steps and 39.5 for 64,
+// 128 x 64 6.8 and 26.6, 64 x 64 5.6 and 21.6; on 512 11.1 and 63.6, 8.7 and 43.1, 6.2 and 29.2.  Full, all of them come to what the L2 gives LDS (18 to
+// 21 TB/s).
 struct Tile { int32_t r, c; float fixed, step, step2; };
-constexpr Tile kTiles[] = {{4, 4, 7.0f, 0.6f, 0.95f}, {4, 2, 5.0f, 0.41f, 0.59f}, {2, 2, 4.2f, 0.28f, 0.4f}};
+constexpr Tile kTiles[] = {{4, 4, 7.6f, 0.5f, 0.85f}, {4, 2, 6.0f, 0.33f, 0.56f}, {2, 2, 5.1f, 0.26f, 0.37f}};
 constexpr int32_t kTile256 = 3;
 
 ProductPlan plan_products(const ProductShape *shapes, int n)
@@ -588,9 +613,13 @@ static hipError_t launch_as(const ProductArgs *a, int n, int32_t tile, const Col
         blocks = std::min(blocks, (int32_t)device_cu_count(device));
     }
     blocks += all.sum_blocks;
-    // LDS: the buffers of a step's operands; for the outputs they are enough too
-    const auto kernel = large ? product_kernel_256<OP, OUT> : tile == 0 ? product_kernel<OP, OUT, 4, 4, 2> : tile == 1 ? product_kernel<OP, OUT, 4, 2, 3> : product_kernel<OP, OUT, 2, 2, 4>;
-    const int lds = large ? 2 * 512 * 128 + 768 * 4 : (tile == 0 ? 2 : tile == 1 ? 3 : 4) * (tr + tc) * 128;
+    // LDS: the buffers of a step's operands; for the outputs they are enough too.  Four buffers of the largest tile leave room for one workgroup only.
+    const bool alone = blocks <= 256;
+    const auto kernel = large       ? product_kernel_256<OP, OUT>
+                        : tile == 0 ? (alone ? product_kernel<OP, OUT, 4, 4, 4> : product_kernel<OP, OUT, 4, 4, 2>)
+                        : tile == 1 ? product_kernel<OP, OUT, 4, 2, 3>
+                                    : product_kernel<OP, OUT, 2, 2, 4>;
+    const int lds = large ? 2 * 512 * 128 + 768 * 4 : (tile == 0 ? (alone ? 4 : 2) : tile == 1 ? 3 : 4) * (tr + tc) * 128;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, s, all);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
