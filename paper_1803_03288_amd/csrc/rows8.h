@@ -168,12 +168,10 @@ __device__ __forceinline__ void put_param(void *p, int dt, int64_t i, float v)
 // Eight parameters from `col` on, zeros behind the end.
 __device__ __forceinline__ void params8(const void *p, int dt, int64_t col, int64_t cols, float *v)
 {
-    if (dt == TICTAC_F32 && col + 8 <= cols && ((uintptr_t)p & 15) == 0) {
-        Elem<TICTAC_F32>::floats(Elem<TICTAC_F32>::load((const float *)p + col), v);
-        return;
-    }
-    if (dt == TICTAC_BF16 && col + 8 <= cols && ((uintptr_t)p & 15) == 0) {
-        Elem<TICTAC_BF16>::floats(Elem<TICTAC_BF16>::load((const __bf16 *)p + col), v);
+    if (col + 8 <= cols) {
+        if (dt == TICTAC_F32) Elem<TICTAC_F32>::floats(load_anywhere<TICTAC_F32>((const float *)p + col), v);
+        else if (dt == TICTAC_F16) Elem<TICTAC_F16>::floats(load_anywhere<TICTAC_F16>((const _Float16 *)p + col), v);
+        else Elem<TICTAC_BF16>::floats(load_anywhere<TICTAC_BF16>((const __bf16 *)p + col), v);
         return;
     }
 #pragma unroll
