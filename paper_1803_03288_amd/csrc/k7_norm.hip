@@ -59,9 +59,9 @@ struct RowReduce {
     }
 };
 
-// Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns, four waves 8 192, sixteen 16 384 (the
-// backward pass keeps four floats for each column of its thread: with more, registers would spill).  Longer rows are read
-// several times (norm_long_kernel).
+// Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns, four waves 4 096, eight 8 192 (6000 x 5368 float16 with its saved
+// rows: 56 us; by four waves 65, by sixteen 74), sixteen 16 384 (the backward pass keeps four floats for each column of its thread: with more, registers
+// would spill).  Longer rows are read several times (norm_long_kernel).
 constexpr int64_t kLongest = 16384;
 
 template <int THREADS>
@@ -493,12 +493,12 @@ template <int DT, bool WIDE>
 static hipError_t forward(const NormArgs &p, hipStream_t s)
 {
     const int64_t c = p.cols;
-    // four rows' worth of workgroups per compute unit (of 256) stay for all rows
+    // as many workgroups as the compute units hold stay for all rows
     if (c <= 512) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 1>), dim3(few((p.rows + 3) / 4, 2048)), dim3(256), 0, s, p);
     else if (c <= 1024) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 2>), dim3(few((p.rows + 3) / 4, 2048)), dim3(256), 0, s, p);
     else if (c <= 2048) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 1>), dim3(few(p.rows, 2048)), dim3(256), 0, s, p);
     else if (c <= 4096) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 2>), dim3(few(p.rows, 2048)), dim3(256), 0, s, p);
-    else if (c <= 8192) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 4>), dim3(few(p.rows, 1024)), dim3(256), 0, s, p);
+    else if (c <= 8192) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 512, 2>), dim3(few(p.rows, 1024)), dim3(512), 0, s, p);
     else if (c <= kLongest) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 1024, 2>), dim3(few(p.rows, 512)), dim3(1024), 0, s, p);
     else hipLaunchKernelGGL((norm_long_kernel<DT, WIDE>), dim3(few(p.rows, 1 << 16)), dim3(1024), 0, s, p);
     return hipGetLastError();
