@@ -145,6 +145,46 @@ def check_counted_waits(asm: str) -> list:
     return bad
 
 
+# The matrix instructions of the largest tiles are written in asm, in place, so that their 256 accumulators stay where they are; the compiler does not know
+# how long their results take, so it must not move an accumulator beside them.
+ACCUMULATORS = "18product_kernel_256"
+
+
+def check_accumulators(asm: str) -> list:
+    """Violations (strings) in the device assembly of k8_product.hip: an accumulator read, written or moved in a stretch of code without labels
+    that holds matrix instructions, or read before the wait that follows them, and registers that spill; [] when it is sound."""
+    bad, seen = [], 0
+    for name, lines in _functions(asm):
+        if ACCUMULATORS not in name:
+            continue
+        seen += 1
+        multiplies = moves = waited = spilled = early = mixed = 0
+        for line in lines + [".end:"]:
+            t = line.strip()
+            if t.startswith(".") and t.split()[0].endswith(":"):
+                mixed += bool(multiplies and moves)
+                multiplies = moves = 0
+            elif t.startswith("v_mfma"):
+                multiplies += 1
+                waited = 0
+            elif t.startswith("s_nop 15"):
+                waited = 1
+            elif t.startswith("v_accvgpr"):
+                moves += 1
+                early += t.startswith("v_accvgpr_read") and not waited
+            elif t.startswith("scratch_"):
+                spilled += 1
+        if mixed:
+            bad.append(f"{name}: accumulators are moved among the matrix instructions")
+        if early:
+            bad.append(f"{name}: accumulators are read before the wait")
+        if spilled:
+            bad.append(f"{name}: register spills (scratch instructions)")
+    if not seen:
+        bad.append(f"no kernel {ACCUMULATORS} found")
+    return bad
+
+
 def device_assembly(source: str) -> str:
     cmd = [HIPCC] + [f for f in FLAGS if f not in ("-shared", "-fPIC")] + \
         ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "--cuda-device-only", "-S", "-o", "-", source]
@@ -171,10 +211,11 @@ def build(verbose: bool = False) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    bad = check_counted_waits(device_assembly(os.path.join(CSRC, "k1_propagate.hip")))
-    if bad:
-        os.remove(LIB)
-        raise RuntimeError("hand-counted memory waits no longer match the generated code:\n  " + "\n  ".join(bad))
+    for source, check in (("k1_propagate.hip", check_counted_waits), ("k8_product.hip", check_accumulators)):
+        bad = check(device_assembly(os.path.join(CSRC, source)))
+        if bad:
+            os.remove(LIB)
+            raise RuntimeError(f"{source}: what is written by hand no longer matches the generated code:\n  " + "\n  ".join(bad))
     build_layers(verbose)
     return LIB
 
