@@ -561,28 +561,37 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
         for (int32_t most = 1 << 30; most >= 2; most = most > 64 ? 64 : most / 2) {         // steps of a workgroup
             int32_t splits[2] = {1, 1};
             int64_t blocks = 0;
-            float steps = 0.0f, us = 0.0f;
+            float steps = 0.0f, all_steps = 0.0f, us = 0.0f;
             for (int i = 0; i < n; ++i) {
                 splits[i] = std::min(16, std::max(1, (shapes[i].steps + most - 1) / most));
                 blocks += tiles[i] * splits[i];
                 steps = std::max(steps, (float)shapes[i].steps / (float)splits[i]);
+                all_steps += (float)tiles[i] * (float)shapes[i].steps;
                 if (splits[i] > 1) us += 1.0f + (float)splits[i] * (float)shapes[i].R * (float)shapes[i].C * (8.0f / 4.5e6f);       // written and read again
             }
             for (int i = 0; i < n; ++i)
                 if (splits[i] > 1) { us += 2.0f; break; }                                   // the launch that adds them up
             const float per_cu = (float)((blocks + 255) / 256);
-            us += per_cu <= 1.0f ? t.fixed + t.step * steps : t.fixed * (0.5f + 0.35f * per_cu) + t.step2 * steps * per_cu * 0.5f;
+            if (per_cu <= 1.0f) {
+                us += t.fixed + t.step * steps;
+            } else {                                            // the longest of them begin at once where they are the first product's, and else may come last
+                const float mean = std::min(all_steps / (float)blocks, steps), work = t.step2 * 0.5f * mean * per_cu, one = t.step2 * steps;
+                us += t.fixed * (0.5f + 0.35f * per_cu) + (shapes[0].steps * splits[n - 1] >= shapes[n - 1].steps * splits[0] ? std::max(work, one) : work + t.step2 * (steps - mean));
+            }
             take(tile, splits, us);
         }
     }
-    // tiles of 256 x 256, one workgroup per compute unit from tile to tile: 1.45 us a step, 6 us a tile besides
-    float us = 4.0f, steps = 0.0f;
-    int64_t tiles = 0;
+    // tiles of 256 x 256, one workgroup per compute unit from tile to tile, those of the first product first: 1.45 us a step with all compute units busy, 1.0 with
+    // half of them, 6 us a tile besides; the longest of the workgroups that begin with the second product's tiles one turn earlier or later
+    float each[2] = {0.0f, 0.0f};
+    int64_t tiles[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
-        tiles += (int64_t)((shapes[i].R + 255) / 256) * ((shapes[i].C + 255) / 256);
-        steps = std::max(steps, (float)shapes[i].steps);
+        tiles[i] = (int64_t)((shapes[i].R + 255) / 256) * ((shapes[i].C + 255) / 256);
     }
-    us += (float)((tiles + 255) / 256) * (6.0f + 1.45f * steps);
+    const float step = std::min(1.45f, std::max(1.0f, (float)(tiles[0] + tiles[1]) * (1.45f / 256.0f)));
+    for (int i = 0; i < n; ++i) each[i] = 6.0f + step * (float)shapes[i].steps;
+    const int64_t turns = (tiles[0] + tiles[1] + 255) / 256, early = tiles[0] / 256, late = (tiles[0] + 255) / 256;
+    const float us = 4.0f + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
     take(kTile256, {1, 1}, us);
     return best;
 }
