@@ -1,5 +1,5 @@
 // See k8_product.h.  A workgroup has a tile of the output, its waves a part of that each; the operands come through LDS in steps of 128
-// bytes of k, two buffers in turn: while one is computed from, the next step is under way into the other, straight from memory to LDS.
+// bytes of k, several buffers in turn: while one is computed from, the next steps are under way into the others, straight from memory to LDS.
 #include <algorithm>
 
 #include "device_utils.h"
@@ -286,12 +286,13 @@ __global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_
     else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
 }
 
+__device__ __forceinline__ i32x4 i32x4_of(const float *v) { return __builtin_bit_cast(i32x4, (f32x4{v[0], v[1], v[2], v[3]})); }
+
 // Lanes 16 g + n hold, of column `column` (n on from a multiple of 16), sixteen bytes `lo` at row `row` and sixteen `hi` STEP rows behind, the four g making
 // up 64 bytes, or every other sixteen of 128.  Columns n and n + 8 exchange a half, so that each store brings eight lanes' 128 bytes of a column: whole
 // lines, which stores past the caches need.  Through the caches the outputs (25 MB at least, where tiles of this size are taken) would drive out what
 // they hold of the operands: 8192 x 4096 x 16384 int8 to bf16, all values alike: 435 us through the caches, 400 past them in parts, 374 in lines;
 // with random values 494 and 465.
-__device__ __forceinline__ i32x4 i32x4_of(const float *v) { return __builtin_bit_cast(i32x4, (f32x4{v[0], v[1], v[2], v[3]})); }
 template <int STEP, typename T>
 __device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, int64_t ld, i32x4 lo, i32x4 hi)
 {
@@ -317,7 +318,7 @@ __device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, i
 // behind the last barrier of a tile LDS is free, and the first two steps of the next tile are asked for before this one's outputs are formed.
 // Two blocks of 16 rows share 32 rows of p in turns of four (row 4 n + e of block 2 m + h is row 32 m + 8 n + 4 h + e of the tile), so that a lane has
 // eight outputs next to each other and stores sixteen bytes of bf16 straight from its registers.
-// 8192 x 4096 x 16384 int8: a step takes 1.47 us of a workgroup (2.9 POP/s), what lies between two tiles used to take 14 us.
+// 8192 x 4096 x 16384 int8: a step takes 1.45 us of a workgroup (2.9 POP/s while it lasts; the clock is down to 1.88 GHz then), 450 us in all.
 template <class OP, int OUT>
 __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 {
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 }
 
 // Adds up the splits in their order, four outputs per thread (one where rows of the sums do not start on 16-byte boundaries), the loads of
-// four splits under way.
+// four splits under way.  32 x 25088 from two splits: 5 us.
 struct Joins {
     ProductArgs a[2];
     uint32_t first1;                    // workgroups from here on: product 1
