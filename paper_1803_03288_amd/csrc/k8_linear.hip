@@ -519,6 +519,25 @@ struct Operands {
     int64_t padded_o, padded_t;
 };
 
+constexpr int dy_share(int pieces) { return pieces > 2 ? 4 : 8; }
+// half of what load8 brings
+template <int DT, bool WIDE>
+__device__ __forceinline__ void load_half(const typename Elem<DT>::type *row, int64_t col, int64_t cols, float *v)
+{
+    typename Elem<DT>::type r[4];
+    if (WIDE ? col < cols : col + 4 <= cols) {
+        __builtin_memcpy(r, row + col, sizeof(r));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = Elem<DT>::to_float(r[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float x = Elem<DT>::to_float(row[min(col + i, cols - 1)]);
+        v[i] = col + i < cols ? x : 0.0f;
+    }
+}
+
 template <int DT, bool WIDE>
 __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Operands to)
 {
@@ -538,36 +557,21 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
         return;
     }
     if (unit >= to.units[3]) return;
-    // (rows and columns of dy by waves of their own: each is a chain of a thousand instructions where dy has several pieces)
+    // Rows and columns of dy by waves of their own, and float32's by two each: a chain of a thousand instructions where dy has several pieces.
     const bool rows_only = unit < to.units[2];
     unit -= rows_only ? to.units[1] : to.units[2];
-    const int64_t tiles = (p.outs + 63) / 64, t0 = unit / tiles * 64, t = t0 + (lane & 7) * 8, o = unit % tiles * 64 + (lane >> 3) * 8;
-    float v[8][8];                                              // [row][column]
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int64_t row = min(t + e, p.rows - 1);
-        E::floats(load8<DT, WIDE>((const T *)p.dy + row * p.ld_dy, o, p.outs), v[e]);
-        if (t + e >= p.rows)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[e][i] = 0.0f;
-    }
-    if (to.sums && !rows_only) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += v[e][i];
-#pragma unroll
-            for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
-            if ((lane & 7) == 0 && o + i < p.outs) to.sums[t0 / 64 * p.outs + o + i] = sum;
-        }
-    }
+    constexpr int N = dy_share(PIECES);                         // rows, or columns, of a lane
+    const int part = (int)(unit % (8 / N)) * N;
+    unit /= 8 / N;
+    const int64_t tiles = (p.outs + 63) / 64, t0 = unit / tiles * 64, t = t0 + (lane & 7) * 8 + (rows_only ? part : 0), o = unit % tiles * 64 + (lane >> 3) * 8 + (rows_only ? 0 : part);
     if (rows_only) {
-        float s[8];
+        float v[N][8], s[8];
+#pragma unroll
+        for (int e = 0; e < N; ++e) E::floats(load8<DT, WIDE>((const T *)p.dy + min(t + e, p.rows - 1) * p.ld_dy, o, p.outs), v[e]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] = PIECES > 1 && o + i < p.outs ? p.ws[o + i] : 1.0f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             uint16_t cuts[8][PIECES];
 #pragma unroll
             for (int i = 0; i < 8; ++i) cut<PIECES>(PIECES > 1 ? v[e][i] * s[i] : v[e][i], cuts[i]);
@@ -576,21 +580,42 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
             for (int k = 0; k < PIECES; ++k)
                 *(i32x4 *)(to.q_x + ((t + e) * PIECES + k) * to.padded_o + o) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
         }
+        return;
     }
-    if (to.q_w && !rows_only) {
-        float s[8];
+    float v[8][N], s[8];                                        // [row][column]
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = PIECES > 1 ? p.xs[min(t + e, p.rows - 1)] : 1.0f;
+    for (int e = 0; e < 8; ++e) {
+        const T *const row = (const T *)p.dy + min(t + e, p.rows - 1) * p.ld_dy;
+        if constexpr (N == 8) E::floats(load8<DT, WIDE>(row, o, p.outs), v[e]);
+        else load_half<DT, WIDE>(row, o, p.outs, v[e]);
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            uint16_t cuts[8][PIECES];
+    for (int e = 0; e < 8; ++e) {
+        s[e] = PIECES > 1 ? p.xs[min(t + e, p.rows - 1)] : 1.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) cut<PIECES>(PIECES > 1 ? (t + e < p.rows ? v[e][i] * s[e] : 0.0f) : v[e][i], cuts[e]);
-            if (o + i >= p.outs) continue;
+        for (int i = 0; i < N; ++i) v[e][i] = t + e < p.rows ? v[e][i] : 0.0f;
+    }
+    if (to.sums) {
 #pragma unroll
-            for (int k = 0; k < PIECES; ++k)
-                *(i32x4 *)(to.q_w + ((o + i) * PIECES + k) * to.padded_t + t) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
+        for (int i = 0; i < N; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += v[e][i];
+#pragma unroll
+            for (int k = 1; k < 8; k <<= 1) sum += __shfl_xor(sum, k);
+            if ((lane & 7) == 0 && o + i < p.outs) to.sums[t0 / 64 * p.outs + o + i] = sum;
         }
+    }
+    if (!to.q_w) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        uint16_t cuts[8][PIECES];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) cut<PIECES>(PIECES > 1 ? (t + e < p.rows ? v[e][i] * s[e] : 0.0f) : v[e][i], cuts[e]);
+        if (o + i >= p.outs) continue;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k)
+            *(i32x4 *)(to.q_w + ((o + i) * PIECES + k) * to.padded_t + t) = i32x4{pair(cuts[0][k], cuts[1][k]), pair(cuts[2][k], cuts[3][k]), pair(cuts[4][k], cuts[5][k]), pair(cuts[6][k], cuts[7][k])};
     }
 }
 
@@ -665,7 +690,7 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
     if (p.db) to.sums = (float *)(at + room.sums);
     to.units[0] = p.dx ? (p.cols + 127) / 128 * (room.padded_o / 64) : 0;
     to.units[1] = to.units[0] + (p.dw ? (p.cols + 127) / 128 * (room.padded_t / 64) : 0);
-    const int64_t tiles = (p.outs + 63) / 64 * (room.padded_t / 64);
+    const int64_t tiles = (p.outs + 63) / 64 * (room.padded_t / 64) * (8 / dy_share(PIECES));
     to.units[2] = to.units[1] + (to.q_x ? tiles : 0);
     to.units[3] = to.units[2] + (to.q_w || to.sums ? tiles : 0);
     if (to.units[3]) hipLaunchKernelGGL((linear_operands_kernel<DT, WIDE>), dim3((unsigned)((to.units[3] + 3) / 4)), dim3(256), 0, s, p, to);
