@@ -13,10 +13,12 @@ binding   : ctypes binding of the C-ABI library (``libtictac.so``) built from
 layers    : operators of a worker's layers (8-bit rows, layer norm, products
             with 8-bit weights, forward and backward) from the same library:
             the ops between the transfers.
+measured  : a stack of such layers run on the GPU, its ops timed and its
+            transfers ordered (``python -m paper_1803_03288_amd.measured``).
 build     : compiles ``csrc/`` for gfx950 with hipcc.
 
 Nothing is imported eagerly so that the generator module can be used on a
 machine without the compiled library.
 """
 
-__all__ = ["workloads", "binding", "layers", "build"]
+__all__ = ["workloads", "binding", "layers", "measured", "build"]
