@@ -63,8 +63,7 @@ struct RowReduce {
 };
 
 // Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns, four waves 4 096, eight 8 192 (6000 x 5368 float16 with its saved
-// rows: 56 us; by four waves 65, by sixteen 74), sixteen 16 384 (the backward pass keeps four floats for each column of its thread: with more, registers
-// would spill).  Longer rows are read several times (norm_long_kernel).
+// rows: 56 us; by four waves 65, by sixteen 74), sixteen 16 384 (the backward pass keeps dw and db of those in LDS).  Longer rows are read several times (norm_long_kernel).
 constexpr int64_t kLongest = 16384;
 
 template <int THREADS>
@@ -253,11 +252,17 @@ struct NormRow {                                    // eight columns of dy and o
     }
 };
 
-template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
+// SUMS: dw and db are asked for; in LDS where the registers do not hold them beside a row (THREADS * NC > 1024): 16 bytes of a thread's own at a time, without
+// conflicts and without barriers (3887 x 9264 bfloat16: 54 us, 105 with registers that spill; 3887 x 16384 float32: 177, 294).
+constexpr bool sums_in_lds(int threads, int nc) { return threads * nc > 1024; }
+
+template <int DT, bool WIDE, bool SAVED, int THREADS, int NC, bool SUMS>
 __device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)          // the workgroups 0 .. blocks - 1
 {
     using T = typename Elem<DT>::type;
     constexpr int kRows = RowShape<THREADS>::kRows;
+    constexpr bool kRegisters = SUMS && !sums_in_lds(THREADS, NC);
+    extern __shared__ f32x4 lds[];                              // [dw, db][NC][2][THREADS]
     __shared__ float cells[2][2][RowReduce<THREADS>::kWaves];
     __shared__ float join[kRows > 1 ? kRows * 2 * NC * THREADS * 8 : 1];
     RowReduce<THREADS> r{cells};
@@ -278,6 +283,9 @@ __device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)
     for (int j = 0; j < NC; ++j) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) { w[j][i] = 1.0f; dw[j][i] = db[j][i] = 0.0f; }
+        if (SUMS && !kRegisters)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) lds[((k >> 1) * NC * 2 + j * 2 + (k & 1)) * THREADS + t] = f32x4{};
         if (p.weight) params8(p.weight, p.param_dtype, (int64_t)(j * THREADS + t) * 8, cols, w[j]);
     }
     for (; row < p.rows; row += step) {
@@ -291,8 +299,26 @@ __device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 xh[j][i] = col + i < cols ? xh[j][i] * rstd : 0.0f;
-                dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
-                db[j][i] += g[j][i];
+                if (kRegisters) {
+                    dw[j][i] = fmaf(g[j][i], xh[j][i], dw[j][i]);
+                    db[j][i] += g[j][i];
+                }
+            }
+            if (SUMS && !kRegisters)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    f32x4 &a = lds[(j * 2 + k) * THREADS + t], &b = lds[(NC * 2 + j * 2 + k) * THREADS + t];
+                    f32x4 x = a, y = b;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[i] = fmaf(g[j][k * 4 + i], xh[j][k * 4 + i], x[i]);
+                        y[i] += g[j][k * 4 + i];
+                    }
+                    a = x;
+                    b = y;
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
                 g[j][i] *= w[j][i];
                 sum_g += g[j][i];
                 sum_gx = fmaf(g[j][i], xh[j][i], sum_gx);
@@ -315,7 +341,7 @@ __device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)
             if (p.dx) store8<DT, WIDE>((T *)p.dx + row * p.ld_dx, (int64_t)(j * THREADS + t) * 8, cols, d);
         }
     }
-    if (!p.workspace) return;
+    if (!SUMS || !p.workspace) return;
     float *part = (float *)p.workspace + (int64_t)blockIdx.x * 2 * cols;
     if (kRows > 1) {                                            // the rows of a workgroup first, in order
         constexpr int kWidth = NC * THREADS * 8;
@@ -341,6 +367,10 @@ __device__ __forceinline__ void backward_rows(const NormArgs &p, int32_t blocks)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t col = (int64_t)(j * THREADS + t) * 8 + i;
+            if (!kRegisters) {
+                dw[j][i] = lds[(j * 2 + (i >> 2)) * THREADS + t][i & 3];
+                db[j][i] = lds[(NC * 2 + j * 2 + (i >> 2)) * THREADS + t][i & 3];
+            }
             if (col < cols) { part[col] = dw[j][i]; part[cols + col] = db[j][i]; }
         }
 }
@@ -364,7 +394,7 @@ __device__ __forceinline__ void inputs8(const NormArgs &p, int64_t row, int64_t 
 template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
 __global__ __launch_bounds__(RowShape<THREADS>::kBlock) void layer_norm_backward_kernel(NormArgs p)
 {
-    backward_rows<DT, WIDE, SAVED, THREADS, NC>(p, gridDim.x);
+    backward_rows<DT, WIDE, SAVED, THREADS, NC, true>(p, gridDim.x);
 }
 
 // Small inputs, which the caches hold: dx by a workgroup per row, and beside them workgroups of 16 to 64 columns that go over all rows again for dw and db.
@@ -379,7 +409,7 @@ template <int DT, bool WIDE, bool SAVED, int THREADS, int NC>
 __global__ __launch_bounds__(THREADS) void layer_norm_backward_small_kernel(NormArgs p)
 {
     if ((int64_t)blockIdx.x < p.rows) {
-        backward_rows<DT, WIDE, SAVED, THREADS, NC>(p, (int32_t)p.rows);
+        backward_rows<DT, WIDE, SAVED, THREADS, NC, false>(p, (int32_t)p.rows);
         return;
     }
     using T = typename Elem<DT>::type;
@@ -520,7 +550,7 @@ static int64_t strips_of(int64_t rows, int64_t cols)
 size_t layer_norm_backward_workspace(int64_t rows, int64_t cols) { return is_small(rows, cols) ? 0 : (size_t)strips_of(rows, cols) * 2 * cols * sizeof(float); }
 
 template <int DT, bool WIDE, bool SAVED>
-static void launch_backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
+static hipError_t launch_backward_rows(const NormArgs &p, unsigned strips, hipStream_t s)
 {
     const int64_t c = p.cols;
     if (c <= 512) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 64, 1>), dim3(strips), dim3(256), 0, s, p);
@@ -528,7 +558,13 @@ static void launch_backward_rows(const NormArgs &p, unsigned strips, hipStream_t
     else if (c <= 2048) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 256, 1>), dim3(strips), dim3(256), 0, s, p);
     else if (c <= 4096) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 256, 2>), dim3(strips), dim3(256), 0, s, p);
     else if (c <= 8192) hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 1024, 1>), dim3(strips), dim3(1024), 0, s, p);
-    else hipLaunchKernelGGL((layer_norm_backward_kernel<DT, WIDE, SAVED, 1024, 2>), dim3(strips), dim3(1024), 0, s, p);
+    else {
+        const size_t lds = 2 * 2 * 2 * 1024 * sizeof(f32x4);
+        const auto kernel = layer_norm_backward_kernel<DT, WIDE, SAVED, 1024, 2>;
+        if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3(strips), dim3(1024), lds, s, p);
+    }
+    return hipGetLastError();
 }
 
 template <int DT, bool WIDE, bool SAVED>
@@ -555,9 +591,9 @@ static hipError_t backward(const NormArgs &p, hipStream_t s)
         if (p.dx) hipLaunchKernelGGL((norm_long_dx_kernel<DT, WIDE>), dim3(few(p.rows, 1 << 16)), dim3(1024), 0, s, p);
         if (p.workspace) hipLaunchKernelGGL((norm_long_params_kernel<DT, WIDE>), dim3((unsigned)((p.cols + 2047) / 2048), strips), dim3(256), 0, s, p);
     } else if (p.x) {
-        launch_backward_rows<DT, WIDE, false>(p, strips, s);
+        if (const hipError_t e = launch_backward_rows<DT, WIDE, false>(p, strips, s); e != hipSuccess) return e;
     } else {
-        launch_backward_rows<DT, WIDE, true>(p, strips, s);
+        if (const hipError_t e = launch_backward_rows<DT, WIDE, true>(p, strips, s); e != hipSuccess) return e;
     }
     if (p.dweight || p.dbias)
         hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(1024), 0, s, (int32_t)strips, p.cols, (const float *)p.workspace, p.dweight, p.dbias, p.param_dtype);
