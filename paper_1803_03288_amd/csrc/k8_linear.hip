@@ -519,7 +519,6 @@ struct Operands {
     int64_t padded_o, padded_t;
 };
 
-constexpr int dy_share(int pieces) { return pieces > 2 ? 4 : 8; }
 // half of what load8 brings
 template <int DT, bool WIDE>
 __device__ __forceinline__ void load_half(const typename Elem<DT>::type *row, int64_t col, int64_t cols, float *v)
@@ -538,7 +537,10 @@ __device__ __forceinline__ void load_half(const typename Elem<DT>::type *row, in
     }
 }
 
-template <int DT, bool WIDE>
+// N: rows, or columns, of dy that a lane cuts to pieces.  Eight are whole lines for 16-bit types; with float32, and with float16 where there are less than four
+// waves per compute unit, four are better: a chain of a thousand instructions is cut in half (101 x 777 -> 1001 float32: 22.0 us, 19.4; 300 x 153 -> 587
+// float16: 18.6, 16.1; but 4096 x 4096 -> 4096: 388.8, 393.3).
+template <int DT, bool WIDE, int N>
 __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Operands to)
 {
     using E = Elem<DT>;
@@ -557,10 +559,9 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
         return;
     }
     if (unit >= to.units[3]) return;
-    // Rows and columns of dy by waves of their own, and float32's by two each: a chain of a thousand instructions where dy has several pieces.
+    // rows and columns of dy by waves of their own
     const bool rows_only = unit < to.units[2];
     unit -= rows_only ? to.units[1] : to.units[2];
-    constexpr int N = dy_share(PIECES);                         // rows, or columns, of a lane
     const int part = (int)(unit % (8 / N)) * N;
     unit /= 8 / N;
     const int64_t tiles = (p.outs + 63) / 64, t0 = unit / tiles * 64, t = t0 + (lane & 7) * 8 + (rows_only ? part : 0), o = unit % tiles * 64 + (lane >> 3) * 8 + (rows_only ? 0 : part);
@@ -690,10 +691,15 @@ static hipError_t backward(const LinearArgs &p, hipStream_t s)
     if (p.db) to.sums = (float *)(at + room.sums);
     to.units[0] = p.dx ? (p.cols + 127) / 128 * (room.padded_o / 64) : 0;
     to.units[1] = to.units[0] + (p.dw ? (p.cols + 127) / 128 * (room.padded_t / 64) : 0);
-    const int64_t tiles = (p.outs + 63) / 64 * (room.padded_t / 64) * (8 / dy_share(PIECES));
+    int64_t tiles = (p.outs + 63) / 64 * (room.padded_t / 64);
+    const bool halves = PIECES == 3 || (PIECES == 2 && tiles <= 512);
+    if (halves) tiles *= 2;
     to.units[2] = to.units[1] + (to.q_x ? tiles : 0);
     to.units[3] = to.units[2] + (to.q_w || to.sums ? tiles : 0);
-    if (to.units[3]) hipLaunchKernelGGL((linear_operands_kernel<DT, WIDE>), dim3((unsigned)((to.units[3] + 3) / 4)), dim3(256), 0, s, p, to);
+    if (to.units[3]) {
+        const auto kernel = PIECES == 3 || halves ? linear_operands_kernel<DT, WIDE, PIECES == 1 ? 8 : 4> : linear_operands_kernel<DT, WIDE, PIECES == 3 ? 4 : 8>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((to.units[3] + 3) / 4)), dim3(256), 0, s, p, to);
+    }
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     ProductArgs a[2] = {};
     int n = 0;
