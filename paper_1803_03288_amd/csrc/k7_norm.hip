@@ -62,7 +62,8 @@ struct RowReduce {
     }
 };
 
-// Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns, four waves 4 096, eight 8 192 (6000 x 5368 float16 with its saved
+// Threads per row and chunks of eight columns per thread: a wave holds up to 1 024 columns (forward, in whole eights,
+// 1 536: 16000 x 1536 bfloat16 17.3 us, by four waves 21.8), four waves 4 096, eight 8 192 (6000 x 5368 float16 with its saved
 // rows: 56 us; by four waves 65, by sixteen 74), sixteen 16 384 (the backward pass keeps dw and db of those in LDS).  Longer rows are read several times (norm_long_kernel).
 constexpr int64_t kLongest = 16384;
 
@@ -85,13 +86,11 @@ __global__ __launch_bounds__(RowShape<THREADS>::kBlock, 4) void layer_norm_kerne
     const float per = 1.0f / (float)cols;
     float w[NC][8], b[NC][8];
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int64_t col = (int64_t)(j * THREADS + t) * 8;
+    for (int j = 0; j < NC; ++j)
 #pragma unroll
         for (int i = 0; i < 8; ++i) { w[j][i] = 1.0f; b[j][i] = 0.0f; }
-        if (p.weight) params8(p.weight, p.param_dtype, col, cols, w[j]);
-        if (p.bias) params8(p.bias, p.param_dtype, col, cols, b[j]);
-    }
+    if (p.weight) params_at_once<THREADS, NC>(p.weight, p.param_dtype, t * 8, cols, w);
+    if (p.bias) params_at_once<THREADS, NC>(p.bias, p.param_dtype, t * 8, cols, b);
     for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS; row < p.rows; row += (int64_t)gridDim.x * kRows) {
         float v[NC][8];
         float sum = 0.0f;
@@ -530,6 +529,7 @@ static hipError_t forward(const NormArgs &p, hipStream_t s)
     // as many workgroups as the compute units hold stay for all rows (1 024 of four waves: twice as many take 3 % longer on average, half as many 15)
     if (c <= 512) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 1>), dim3(few((p.rows + 3) / 4, 1024)), dim3(256), 0, s, p);
     else if (c <= 1024) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 64, 2>), dim3(few((p.rows + 3) / 4, 1024)), dim3(256), 0, s, p);
+    else if (WIDE && c <= 1536) hipLaunchKernelGGL((layer_norm_kernel<DT, true, 64, 3>), dim3(few((p.rows + 3) / 4, 1024)), dim3(256), 0, s, p);
     else if (c <= 2048) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 1>), dim3(few(p.rows, 1024)), dim3(256), 0, s, p);
     else if (c <= 4096) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 256, 2>), dim3(few(p.rows, 1024)), dim3(256), 0, s, p);
     else if (c <= 8192) hipLaunchKernelGGL((layer_norm_kernel<DT, WIDE, 512, 2>), dim3(few(p.rows, 1024)), dim3(512), 0, s, p);

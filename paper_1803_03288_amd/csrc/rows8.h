@@ -178,6 +178,25 @@ __device__ __forceinline__ void params8(const void *p, int dt, int64_t col, int6
     for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? param(p, dt, col + i) : 0.0f;
 }
 
+// Eight parameters from each of NC columns on, THREADS * 8 apart, zeros behind the end: all loads before the first conversion, those of a row's
+// last columns too (forward, 4165 x 916 bfloat16: 7.4 us, 9.0 one chunk after the other; backward, 16000 x 2276: float32 114, 125, but 16-bit types 96, 80).
+template <int PT, int THREADS, int NC>
+__device__ __forceinline__ void params_of(const void *p, int64_t col, int64_t cols, float (&v)[NC][8])
+{
+    typename Elem<PT>::raw raw[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) raw[j] = load8<PT, false>((const typename Elem<PT>::type *)p, col + j * THREADS * 8, cols);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) Elem<PT>::floats(raw[j], v[j]);
+}
+template <int THREADS, int NC>
+__device__ __forceinline__ void params_at_once(const void *p, int dt, int64_t col, int64_t cols, float (&v)[NC][8])
+{
+    if (dt == TICTAC_F32) params_of<TICTAC_F32, THREADS, NC>(p, col, cols, v);
+    else if (dt == TICTAC_F16) params_of<TICTAC_F16, THREADS, NC>(p, col, cols, v);
+    else params_of<TICTAC_BF16, THREADS, NC>(p, col, cols, v);
+}
+
 // ---- reductions ----
 template <int CTRL>
 __device__ __forceinline__ float dpp0_f32(float v)              // a lane without a source gets zero
