@@ -583,7 +583,7 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
         }
     }
     // tiles of 256 x 256, one workgroup per compute unit from tile to tile, those of the first product first: 1.45 us a step with all compute units busy, 1.0 with
-    // half of them, 6 us a tile besides; the longest of the workgroups that begin with the second product's tiles one turn earlier or later
+    // half of them, 6 us for a first tile besides and 11 for each behind it; the longest of the workgroups that begin with the second product's tiles one turn earlier or later
     float each[2] = {0.0f, 0.0f};
     int64_t tiles[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
@@ -592,7 +592,7 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
     const float step = std::min(1.45f, std::max(1.0f, (float)(tiles[0] + tiles[1]) * (1.45f / 256.0f)));
     for (int i = 0; i < n; ++i) each[i] = 6.0f + step * (float)shapes[i].steps;
     const int64_t turns = (tiles[0] + tiles[1] + 255) / 256, early = tiles[0] / 256, late = (tiles[0] + 255) / 256;
-    const float us = 4.0f + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
+    const float us = 4.0f + 5.0f * (float)(turns - 1) + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
     take(kTile256, {1, 1}, us);
     return best;
 }

@@ -424,6 +424,26 @@ def test_large_and_small_gradients(L):
         check_linear_grads(L.linear_q8_backward(dy.cuda(), x8, w8), dy, x8, w8, dtype)
 
 
+# ---- sizes at which other kernels take over -----------------------------------------------------------------
+
+MORE_NORMS = [(4200, 136), (4200, 1200), (4200, 1207), (1200, 1999), (1100, 2300), (400, 8100), (400, 9001), (600, 9000), (150, 16384), (130, 20001)]
+
+
+@pytest.mark.parametrize("rows,cols", MORE_NORMS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layer_norm_of_more_rows(L, rows, cols, dtype):
+    """Workgroups that take several rows, and gradients whose sums do not fit the registers: bounds as above."""
+    test_layer_norm(L, rows, cols, dtype)
+    test_layer_norm_backward(L, rows, cols, dtype)
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(2100, 2100, 2100), (1030, 190, 2070), (1500, 1100, 2051), (300, 153, 587)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_backward_of_more_rows(L, rows, cols, outs, dtype):
+    """The largest tiles, sums cut along k, and dy by halves."""
+    test_linear_backward(L, rows, cols, outs, dtype)
+
+
 # ---- use ----------------------------------------------------------------------------------------------------
 
 def test_no_rows(L):
