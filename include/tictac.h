@@ -370,7 +370,8 @@ int tictac_linear_q8(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, co
                      const void *bias, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, tictac_stream stream);
 
 /* Gradients of the above, the rounding of x taken for the identity: dx[t][i] = sum_o dy[t][o] w_scale[o] wq[o][i],
- * dw[o][i] = sum_t dy[t][o] x_scale[t] xq[t][i], db[o] = sum_t dy[t][o]; all of dtype, each may be NULL. */
+ * dw[o][i] = sum_t dy[t][o] x_scale[t] xq[t][i], db[o] = sum_t dy[t][o]; all of dtype, each may be NULL.  xq and x_scale are read for dw
+ * alone, wq and w_scale for dx alone: without that output they may be NULL. */
 int tictac_linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
 int tictac_linear_q8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *dy, int64_t ld_dy, const int8_t *xq,
                               int64_t ld_xq, const float *x_scale, const int8_t *wq, int64_t ld_w, const float *w_scale, void *dx,

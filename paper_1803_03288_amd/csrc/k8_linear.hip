@@ -405,7 +405,8 @@ __global__ __launch_bounds__(kBackWaves * 64) void linear_dx_few_kernel(LinearAr
 }
 
 // dw: all of k (the rows t, up to 32 KB) is at hand.  The activations are turned round in registers as the weights above, four bytes per lane, and stay
-// there; the pieces of dy times scale lie in LDS.  A workgroup has 64 outputs and 512 columns, a wave 64 columns.  db rides along with the first columns.
+// there; the pieces of dy times scale lie in LDS.  A workgroup has 64 outputs and 512 columns, a wave 64 columns.  db rides along with the first columns, and
+// is all there is where dw is not asked for: xq and xs may be NULL then.
 // 32 rows, 4096 x 25088 float16: 47 us, 4.4 TB/s; with stores past the caches 64.
 template <int DT, bool WIDE, int KB>
 __global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
@@ -417,7 +418,7 @@ __global__ __launch_bounds__(512) void linear_dw_few_kernel(LinearArgs p)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
     const int64_t o0 = (int64_t)blockIdx.y * kOuts, i0 = (int64_t)blockIdx.x * 512 + wave * 64;
     const int o = threadIdx.x & 63;
-    for (int t = threadIdx.x >> 6; t < KB * 32; t += 8) {
+    for (int t = threadIdx.x >> 6; t < (p.dw ? KB * 32 : 0); t += 8) {
         uint16_t cuts[PIECES];
         cut<PIECES>(t < p.rows && o0 + o < p.outs ? E::to_float(((const T *)p.dy)[t * p.ld_dy + o0 + o]) * p.xs[t] : 0.0f, cuts);
 #pragma unroll
@@ -592,7 +593,7 @@ __global__ __launch_bounds__(256) void linear_operands_kernel(LinearArgs p, Oper
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        s[e] = PIECES > 1 ? p.xs[min(t + e, p.rows - 1)] : 1.0f;
+        s[e] = PIECES > 1 && to.q_w ? p.xs[min(t + e, p.rows - 1)] : 1.0f;      // (without dw there may be no xs)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[e][i] = t + e < p.rows ? v[e][i] : 0.0f;
     }
