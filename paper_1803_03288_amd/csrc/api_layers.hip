@@ -9,7 +9,7 @@ using namespace tictac;
 
 namespace {
 
-constexpr int64_t kMostCols = 131072;           // |q| <= 128: sums of the products of so many int8 values fit int32
+constexpr int64_t kMostCols = 131072;           // |q| <= 128: sums of the products of so many int8 values fit int32, but for one (exact_sum)
 constexpr int64_t kMostRows = 1 << 21;          // of the products (offsets inside a tile are 32 bits)
 constexpr int64_t kMostStride = 1 << 24;        // bytes between 8-bit rows of the products, for the same reason
 

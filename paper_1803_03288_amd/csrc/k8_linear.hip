@@ -64,16 +64,16 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs p
         // lane l of a block holds outputs 4 (l / 16) .. + 3 of row l % 16; a thread finishes one output
         for (int i = threadIdx.x; i < TB * 256; i += kFewWaves * 64) {
             const int b = i >> 8, o = i & 15, t = (i >> 4) & 15;
-            int32_t sum = 0;
+            uint32_t sum = 0;
 #pragma unroll
-            for (int k = 0; k < kFewWaves; ++k) sum += sums[k][b][(o >> 2) * 16 + t][o & 3];
+            for (int k = 0; k < kFewWaves; ++k) sum += (uint32_t)sums[k][b][(o >> 2) * 16 + t][o & 3];
             const int64_t at = (int64_t)b * 16 + t, out = o0 + f * 16 + o;
             if (at >= p.rows || out >= p.outs) continue;
             if (splits > 1) {
-                parts[((int64_t)split * p.rows + at) * p.outs + out] = sum;
+                parts[((int64_t)split * p.rows + at) * p.outs + out] = (int32_t)sum;
                 continue;
             }
-            float v = (float)sum * (xs[at] * p.ws[out]);
+            float v = exact_sum((int32_t)sum) * (xs[at] * p.ws[out]);
             if (p.bias) v += param(p.bias, p.bias_dtype, out);
             put_param(p.y, p.dtype, at * p.ld_y + out, v);
         }
@@ -195,11 +195,12 @@ static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
     return parts_along_k(blocks, units / kFewWaves, 256);                   // a unit for each wave at least
 }
 
+constexpr int64_t kWrapCols = 131072;           // (exact_sum; the most that are taken)
 static ProductPlan forward_plan(int64_t rows, int64_t cols, int64_t outs)
 {
     if (rows <= kFewRows) return {0, {few_splits(rows, cols, outs), 1}};
     const ProductShape shape{(int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128)};
-    return plan_products(&shape, 1);
+    return plan_products(&shape, 1, cols == kWrapCols);
 }
 size_t linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
@@ -639,7 +640,7 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.padded_o = (outs + 63) / 64 * 64;
     r.padded_t = (rows + 63) / 64 * 64;
     const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces)}};
-    r.plan = plan_products(shapes, 2);
+    r.plan = plan_products(shapes, 2, false);
     r.p_x = r.sums + up((size_t)(r.padded_t / 64) * outs * 4);
     r.p_w = r.p_x + up((size_t)cols * r.padded_o * 2);
     r.q_x = r.p_w + up((size_t)cols * r.padded_t * 2);

@@ -12,11 +12,15 @@ typedef const __attribute__((address_space(1))) void global_void;
 
 struct OpI8 {
     typedef i32x4 acc;
+    typedef uint32_t sum;               // (adding up wraps, defined)
+    static __device__ __forceinline__ float value(int32_t s) { return exact_sum(s); }
     static __device__ __forceinline__ acc mma(i32x4 a, i32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ void mma_in_place(i32x4 a, i32x4 b, acc &c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
 struct OpBf16 {
     typedef f32x4 acc;
+    typedef float sum;
+    static __device__ __forceinline__ float value(float s) { return s; }
     static __device__ __forceinline__ acc mma(i32x4 a, i32x4 b, acc c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -101,7 +105,7 @@ __device__ __forceinline__ void put_blocks(const ProductArgs &a, const typename 
             } else {
                 float sum[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) { sum[e] = (float)lo[e]; sum[4 + e] = (float)hi[e]; }
+                for (int e = 0; e < 4; ++e) { sum[e] = OP::value(lo[e]); sum[4 + e] = OP::value(hi[e]); }
                 finish.template store<OUT>(a, mine, column, sum, wide);
             }
         }
@@ -478,7 +482,7 @@ struct Joins {
 template <class OP, int OUT, int VEC>
 __device__ __forceinline__ void join_part(const ProductArgs &a, int64_t at)
 {
-    typedef typename std::remove_reference<decltype(typename OP::acc{}[0] + typename OP::acc{}[0])>::type N;
+    typedef typename OP::sum N;
     typedef N NV __attribute__((ext_vector_type(VEC)));
     const int32_t pieces = a.R / VEC;
     if (at >= (int64_t)pieces * a.C) return;
@@ -498,7 +502,7 @@ __device__ __forceinline__ void join_part(const ProductArgs &a, int64_t at)
     typename Elem<OUT>::type *out = (typename Elem<OUT>::type *)a.out + (int64_t)c * a.ld_out + r;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-        float v = (float)sum[i];
+        float v = OP::value(sum[i]);
         if (Scaled<OP>::value) {
             v *= a.q_scale[c] * a.p_scale[r + i];
             if (a.bias) v += param(a.bias, a.bias_dtype, r + i);
@@ -544,7 +548,7 @@ struct Tile { int32_t r, c; float fixed, step, step2; };
 constexpr Tile kTiles[] = {{4, 4, 7.6f, 0.5f, 0.85f}, {4, 2, 6.0f, 0.33f, 0.56f}, {2, 2, 5.1f, 0.26f, 0.37f}};
 constexpr int32_t kTile256 = 3;
 
-ProductPlan plan_products(const ProductShape *shapes, int n)
+ProductPlan plan_products(const ProductShape *shapes, int n, bool wraps)
 {
     ProductPlan best{0, {1, 1}};
     float least = 1e30f;
@@ -593,7 +597,7 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
     for (int i = 0; i < n; ++i) each[i] = 6.0f + step * (float)shapes[i].steps;
     const int64_t turns = (tiles[0] + tiles[1] + 255) / 256, early = tiles[0] / 256, late = (tiles[0] + 255) / 256;
     const float us = 4.0f + 5.0f * (float)(turns - 1) + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
-    take(kTile256, {1, 1}, us);
+    if (!wraps) take(kTile256, {1, 1}, us);
     return best;
 }
 

@@ -42,3 +42,21 @@ def test_linear_gradients_one_at_a_time(L, rows, cols, outs, dtype):  # noqa: F8
         print(rows, cols, outs, dtype, which, flush=True)
         for name, got in linear_backward_of(dy, x8, w8, which).items():
             assert torch.equal(got, want[name]), (which, name)
+
+
+# (by few rows with and without cuts along k, and by tiles with and without)
+@pytest.mark.parametrize("rows,outs", [(1, 16), (20, 200), (40, 5000), (70, 60), (300, 2100), (600, 6000)])
+def test_the_largest_sum(L, rows, outs):  # noqa: F811
+    """131 072 products of -128 and -128 are 2^31, and of -128 and 127 the least there is."""
+    cols = 131072
+    q = torch.full((rows, cols), -128, dtype=torch.int8, device="cuda")
+    p = torch.full((outs, cols), -128, dtype=torch.int8, device="cuda")
+    q[::2], p[1::3], p[2::3, -1] = 127, 127, -127
+    one = torch.ones(max(rows, outs), 1, device="cuda")
+    got = L.linear_q8(L.Rows8(q, one[:rows], cols), L.Rows8(p, one[:outs], cols))
+    ends = torch.full((rows, 1), -128.0, dtype=torch.float64), torch.full((outs, 1), -128.0, dtype=torch.float64)
+    ends[0][::2], ends[1][1::3] = 127, 127
+    want = cols * ends[0] * ends[1].t()
+    want[:, 2::3] = ((cols - 1) * -128.0 - 127) * ends[0]
+    assert rows == 1 or float(want.max()) == 2.0 ** 31
+    assert torch.equal(got.cpu(), want.float())
