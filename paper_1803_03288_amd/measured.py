@@ -4,7 +4,8 @@ The graphs of ``workloads`` stand in for traced models; here the ops are run.  A
 
     x <- x + relu(norm(x) W1' + b1) W2' + b2
 
-takes its weights as 8-bit rows, as they would be transferred, and keeps its activations in 8 bits for the backward pass (``layers``).
+takes its weights as 8-bit rows, as they would be transferred, and keeps its activations in 8 bits for the backward pass (``layers``), with a mask of
+where the relu is flat: what is positive and rounds to zero has a gradient.
 Every op of a training iteration is timed on the device in several runs; the smallest time of each is the time oracle (Sec. 5,
 "Time Oracle": ``time_oracle_min``).  The graph of the iteration (recvs are roots, a gradient op depends on the gradient behind it, on the forward op whose
 activations it reads and on the weights it reads) then gets its TIC and TAC orders and the makespan and Scheduling
@@ -113,16 +114,16 @@ class Iteration:
         for i, p in enumerate(self.stack):
             y8, mean, rstd, x8 = op(f"forward.norm{i}", lambda: ly.layer_norm_q8(x, p.gamma, p.beta, save=True))
             u = op(f"forward.linear1.{i}", lambda: ly.linear_q8(y8, self.w1[i], p.b1, dtype))
-            u8 = op(f"forward.relu{i}", lambda: ly.quantize_rows(u.relu_()))
+            flat, u8 = op(f"forward.relu{i}", lambda: (u <= 0, ly.quantize_rows(u.relu_())))       # (a NaN is not flat)
             v = op(f"forward.linear2.{i}", lambda: ly.linear_q8(u8, self.w2[i], p.b2, dtype))
-            kept.append((y8, mean, rstd, x8, u8))
+            kept.append((y8, mean, rstd, x8, flat, u8))
             x = op(f"forward.add{i}", lambda: x + v)
         dx, loss = op("loss", lambda: self._loss(x))
         grads: List[Layer] = []
         for i in reversed(range(len(self.stack))):
-            p, (y8, mean, rstd, x8, u8) = self.stack[i], kept.pop()
+            p, (y8, mean, rstd, x8, flat, u8) = self.stack[i], kept.pop()
             du, dw2, db2 = op(f"backward.linear2.{i}", lambda: ly.linear_q8_backward(dx, u8, self.w2[i]))
-            du = op(f"backward.relu{i}", lambda: du.masked_fill_(u8.q[:, :u8.cols] <= 0, 0))
+            du = op(f"backward.relu{i}", lambda: du.masked_fill_(flat, 0))
             dn, dw1, db1 = op(f"backward.linear1.{i}", lambda: ly.linear_q8_backward(du, y8, self.w1[i]))
             dn, dgamma, dbeta = op(f"backward.norm{i}", lambda: ly.layer_norm_backward(dn, x8, p.gamma, mean, rstd))
             dx = op(f"backward.add{i}", lambda: dx + dn)
