@@ -88,7 +88,7 @@ def iteration_graph(n: int, width: int, hidden: int) -> Graph:
     for i in reversed(range(n)):
         norm, w1, _, w2, _ = params[i]
         g.op(f"backward.linear2.{i}", before, f"forward.relu{i}", w2)
-        g.op(f"backward.relu{i}", f"backward.linear2.{i}", f"forward.linear1.{i}")
+        g.op(f"backward.relu{i}", f"backward.linear2.{i}", f"forward.relu{i}")
         g.op(f"backward.linear1.{i}", f"backward.relu{i}", f"forward.norm{i}", w1)
         g.op(f"backward.norm{i}", f"backward.linear1.{i}", f"forward.norm{i}", norm)
         before = g.op(f"backward.add{i}", f"backward.norm{i}", before)
