@@ -15,6 +15,7 @@ Efficiency of the iteration under each, beside transfers in random order, with t
 from __future__ import annotations
 
 import argparse
+import math
 from typing import Callable, Dict, List, NamedTuple, Tuple
 
 import numpy as np
@@ -101,6 +102,9 @@ class Iteration:
     def __init__(self, stack: List[Layer], x: torch.Tensor, target: torch.Tensor):
         from . import layers
         self.layers, self.stack, self.x, self.target = layers, stack, x, target
+        # The loss is a mean: its gradients in float16 would be subnormal (2^-22 at 4096 x 1024).  They are taken times a power of two, and what is returned is
+        # divided by it in float32: values of dx are then of the order of 1 / sqrt(rows), their sums over the rows of sqrt(rows) at most.
+        self.scale = 2.0 ** round(math.log2(x.shape[1] * math.sqrt(max(1, x.shape[0]))))
         self.refresh()
 
     def refresh(self) -> None:
@@ -127,12 +131,12 @@ class Iteration:
             dn, dw1, db1 = op(f"backward.linear1.{i}", lambda: ly.linear_q8_backward(du, y8, self.w1[i]))
             dn, dgamma, dbeta = op(f"backward.norm{i}", lambda: ly.layer_norm_backward(dn, x8, p.gamma, mean, rstd))
             dx = op(f"backward.add{i}", lambda: dx + dn)
-            grads.append(Layer(dgamma, dbeta, dw1.float(), db1.float(), dw2.float(), db2.float()))
+            grads.append(Layer(*(t.float() / self.scale for t in (dgamma, dbeta, dw1, db1, dw2, db2))))
         return loss, grads[::-1]
 
     def _loss(self, x):
         d = x.float() - self.target
-        return (d / d.numel()).to(x.dtype), 0.5 * d.square().mean()
+        return (d * (self.scale / d.numel())).to(x.dtype), 0.5 * d.square().mean()
 
 
 def measure(it: Iteration, names: List[str], runs: int) -> torch.Tensor:

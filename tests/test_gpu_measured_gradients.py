@@ -1,5 +1,7 @@
 """Gradients of the measured iteration (``paper_1803_03288_amd.measured``) op by op."""
 
+import math
+
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +42,28 @@ def test_relu_passes_the_gradients_of_what_rounds_to_zero(dtype):
     assert bool(torch.isnan(u[3]).all()) and int(((u > 0) & (u < 39)).sum()) > rows * hidden // 4       # (1e4 / 254 = 39)
     assert torch.equal(torch.nan_to_num(got, nan=9.0), torch.nan_to_num(torch.where(u <= 0, torch.zeros_like(du), du), nan=9.0))
     assert bool(torch.isnan(got[3]).any()) and bool(torch.isnan(grads[0].w1).any())
+
+
+def test_float16_gradients_of_a_mean_over_many():
+    """At 4096 x 1024 the loss's own gradients are subnormal in float16: they are taken times a power of two, each rounded to 11 bits.  The iteration's
+    are as near to float32's as its activations are.  Bound of those: activations in float16 step to another 8-bit value in one of 16 places, by 1 / 127 of a row's largest (some four times the typical one): 1 % of
+    their norm, on two layers' ops and both passes."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rows, width = 4096, 1024
+    stack = measured.random_layers(2, width, 1024, seed=10)
+    x, target = (torch.randn(rows, width, generator=g, device="cuda") for _ in range(2))
+    x = x.half()
+    (loss32, want), _ = run_and_keep(measured.Iteration(stack, x.float(), target))
+    (loss16, got), kept = run_and_keep(measured.Iteration(stack, x, target), "forward.add1", "loss")
+    dx, exact = kept["loss"].double(), (kept["forward.add1"].double() - target.double()) / target.numel()
+    scale = 2.0 ** round(math.log2(float(dx.norm() / exact.norm())))
+    assert float((dx - scale * exact).norm()) <= 2.0 ** -11 * scale * float(exact.norm())
+    assert abs(float(loss16) - float(loss32)) <= 1e-2 * float(loss32)
+    for a, b in zip(got, want):
+        for name in measured.Layer._fields:
+            s, t = getattr(a, name), getattr(b, name)
+            off = float((s - t).norm() / t.norm())
+            print(name, off, flush=True)
+            assert s.dtype == torch.float32 and off <= 0.04, name
