@@ -247,7 +247,8 @@ hipError_t launch_linear_q8(const LinearArgs &p, hipStream_t s)
 }
 
 // dy times a scale in PIECES bf16 values that add up to it: all but the last cut off, which leaves the rest exact, the last rounded.  An infinity
-// leaves NaN, for which the median of three takes the smallest: the pieces still add up to the infinity.
+// leaves NaN, for which the median of three takes the smallest number, zero: the other pieces then are zeros, and their products add nothing to the
+// infinity's.
 template <int PIECES>
 __device__ __forceinline__ void cut(float v, uint16_t *piece)
 {
@@ -255,7 +256,8 @@ __device__ __forceinline__ void cut(float v, uint16_t *piece)
     for (int k = 0; k < PIECES - 1; ++k) {
         const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
         piece[k] = (uint16_t)(high >> 16);
-        v = __builtin_amdgcn_fmed3f(v - __builtin_bit_cast(float, high), -0x1p126f, 0x1p126f);
+        v -= __builtin_bit_cast(float, high);
+        v = __builtin_amdgcn_fmed3f(v, v, 0.0f);
     }
     const __bf16 last = (__bf16)v;
     piece[PIECES - 1] = __builtin_bit_cast(uint16_t, last);

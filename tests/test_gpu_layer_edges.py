@@ -1,4 +1,4 @@
-"""The layers' operators where they can go wrong: gradients asked for one at a time, and others below.  Helpers and bounds are those of
+"""The layers' operators where they can go wrong: gradients asked for one at a time, the largest sums, infinities and NaN.  Helpers and bounds are those of
 ``test_gpu_layers``."""
 
 import ctypes
@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from layer_calls import call
-from test_gpu_layers import BF16, F16, F32, L, TYPES, gen, values, weights  # noqa: F401
+from test_gpu_layers import BF16, F16, F32, LEFT, OUT, TYPES, U, L, gen, rows8_values, values, weights  # noqa: F401
 
 CODE = {F32: 0, F16: 1, BF16: 2}
 
@@ -60,3 +60,64 @@ def test_the_largest_sum(L, rows, outs):  # noqa: F811
     want[:, 2::3] = ((cols - 1) * -128.0 - 127) * ends[0]
     assert rows == 1 or float(want.max()) == 2.0 ** 31
     assert torch.equal(got.cpu(), want.float())
+
+
+def check_with_infinities(got, want, bound):
+    """`got` where the definition in 64 bits is finite, its infinities with their signs, its NaN."""
+    got = got.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(got.isposinf(), want.isposinf()) and torch.equal(got.isneginf(), want.isneginf())
+    fine = torch.isfinite(want)
+    assert float(((got - want).abs() - bound)[fine].max()) <= 0
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(5, 100, 61), (40, 264, 136), (64, 130, 48), (90, 200, 77), (300, 264, 640), (2100, 2100, 2060)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_gradients_of_infinities(L, rows, cols, outs, dtype):  # noqa: F811
+    """One infinity, one minus infinity and one NaN in dy: dx has them in their rows, dw in theirs, with the signs of the 8-bit values; a zero gives NaN."""
+    g = gen(rows)
+    x8, w8 = L.quantize_rows(values(g, rows, cols, F32).cuda()), weights(L, g, outs, cols)
+    dy = values(g, rows, outs, dtype, size=0.01)
+    dy[1, 2], dy[3, 30], dy[rows - 1, outs - 1] = float("inf"), -float("inf"), float("nan")
+    dx, dw, db = L.linear_q8_backward(dy.cuda(), x8, w8)
+    x, w, d = rows8_values(x8), rows8_values(w8), dy.double()
+    small = torch.nan_to_num(d, nan=0.0, posinf=0.0, neginf=0.0).abs()
+
+    def tol(k, size):                       # (that of test_linear_backward, and the rounding of the output)
+        return (LEFT[dtype] + 2 * U + 6 * U * k + OUT[dtype][0]) * 1.01 * size + OUT[dtype][1]
+
+    def product(a, b):                      # (an infinity times zero is NaN, whatever the library's product does with zeros)
+        odd = ~torch.isfinite(a)
+        y = torch.where(odd, 0.0, a) @ b
+        for i, k in odd.nonzero().tolist():
+            y[i] = y[i] + a[i, k] * b[k]
+        return y
+
+    check_with_infinities(dx, product(d, w), tol(outs, small @ w.abs()))
+    check_with_infinities(dw, product(d.t(), x), tol(rows, small.t() @ x.abs()))
+    check_with_infinities(db, d.sum(0), tol(rows, small.sum(0)))
+
+
+@pytest.mark.parametrize("rows,cols", [(6, 100), (30, 1400), (5, 20000), (1500, 130), (600, 9000)])
+@pytest.mark.parametrize("kept", [False, True])
+def test_layer_norm_gradients_of_spoilt_rows(L, rows, cols, kept):  # noqa: F811
+    """A NaN in x, one in dy, an infinity in each: dx is NaN in those rows alone, dw in all columns of a spoilt x, db in those of a spoilt dy."""
+    g = gen(cols)
+    x, dy = values(g, rows, cols, F32), values(g, rows, cols, F32)
+    gamma = (1 + 0.3 * torch.randn(cols, generator=g)).cuda()
+    _, mean, rstd, x8 = L.layer_norm(x.cuda(), gamma, save=True)
+    clean = L.layer_norm_backward(dy.cuda(), x8 if kept else x.cuda(), gamma, mean, rstd)
+    bad = dy.clone()
+    bad[1, 5], bad[2, 7] = float("nan"), float("inf")
+    dx, dw, db = L.layer_norm_backward(bad.cuda(), x8 if kept else x.cuda(), gamma, mean, rstd)
+    others = [i for i in range(rows) if i not in (1, 2)]
+    assert torch.equal(dx[others], clean[0][others]) and bool(torch.isnan(dx[1]).all()) and not bool(torch.isfinite(dx[2]).any())
+    columns = torch.ones(cols, dtype=torch.bool)
+    columns[[5, 7]] = False
+    assert torch.isnan(dw[5]) and not torch.isfinite(dw[7]) and torch.equal(dw[columns], clean[1][columns])
+    assert torch.isnan(db[5]) and db[7] == float("inf") and torch.equal(db[columns], clean[2][columns])
+    x[3, 9], x[4, 0] = float("nan"), -float("inf")
+    _, mean, rstd, x8 = L.layer_norm(x.cuda(), gamma, save=True)
+    dx, dw, db = L.layer_norm_backward(dy.cuda(), x8 if kept else x.cuda(), gamma, mean, rstd)
+    others = [i for i in range(rows) if i not in (3, 4)]
+    assert torch.equal(dx[others], clean[0][others]) and bool(torch.isnan(dx[[3, 4]]).all()) and bool(torch.isnan(dw).all()) and torch.equal(db, clean[2])
