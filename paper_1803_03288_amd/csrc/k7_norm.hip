@@ -487,35 +487,41 @@ __global__ __launch_bounds__(256) void norm_long_params_kernel(NormArgs p)
         if (col + i < cols) { part[col + i] = dw[i]; part[cols + col + i] = db[i]; }
 }
 
-// Adds up the strips, [strips][2][cols]: 64 columns per workgroup, sixteen waves take a sixteenth of the strips each.
+// Adds up the strips, [strips][2][cols]: 64 columns per workgroup, sixteen waves take a sixteenth of the strips each.  A grid's threads are counted in 32
+// bits: workgroups go over the columns in turns where there are more than kParamsBlocks of them (2^25 columns).
+constexpr int64_t kParamsBlocks = 1 << 20;
 __global__ __launch_bounds__(1024) void norm_params_kernel(int32_t strips, int64_t cols, const float *part, void *dweight, void *dbias, int32_t dt)
 {
     __shared__ float sums[16][64];
-    const int64_t at = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
     const int wave = threadIdx.x >> 6, per = (strips + 15) / 16;
-    float sum = 0.0f;
-    if (at < 2 * cols) {
-        int k = wave * per;
-        const int last = min(strips, (wave + 1) * per);
-        for (; k + 8 <= last; k += 8) {                         // (eight loads under way)
-            float v[8];
+    for (int64_t first = (int64_t)blockIdx.x * 64; first < 2 * cols; first += (int64_t)gridDim.x * 64) {
+        const int64_t at = first + (threadIdx.x & 63);
+        float sum = 0.0f;
+        if (at < 2 * cols) {
+            int k = wave * per;
+            const int last = min(strips, (wave + 1) * per);
+            for (; k + 8 <= last; k += 8) {                     // (eight loads under way)
+                float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = part[(int64_t)(k + i) * 2 * cols + at];
+                for (int i = 0; i < 8; ++i) v[i] = part[(int64_t)(k + i) * 2 * cols + at];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[i];
+                for (int i = 0; i < 8; ++i) sum += v[i];
+            }
+            for (; k < last; ++k) sum += part[(int64_t)k * 2 * cols + at];
         }
-        for (; k < last; ++k) sum += part[(int64_t)k * 2 * cols + at];
-    }
-    sums[wave][threadIdx.x & 63] = sum;
-    __syncthreads();
-    if (wave || at >= 2 * cols) return;
-    sum = 0.0f;
+        sums[wave][threadIdx.x & 63] = sum;
+        __syncthreads();
+        if (wave == 0 && at < 2 * cols) {
+            sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) sum += sums[k][threadIdx.x & 63];
-    if (at < cols) {
-        if (dweight) put_param(dweight, dt, at, sum);
-    } else if (dbias) {
-        put_param(dbias, dt, at - cols, sum);
+            for (int k = 0; k < 16; ++k) sum += sums[k][threadIdx.x & 63];
+            if (at < cols) {
+                if (dweight) put_param(dweight, dt, at, sum);
+            } else if (dbias) {
+                put_param(dbias, dt, at - cols, sum);
+            }
+        }
+        __syncthreads();                                        // (read before the next turn's are written)
     }
 }
 
@@ -596,7 +602,7 @@ static hipError_t backward(const NormArgs &p, hipStream_t s)
         if (const hipError_t e = launch_backward_rows<DT, WIDE, true>(p, strips, s); e != hipSuccess) return e;
     }
     if (p.dweight || p.dbias)
-        hipLaunchKernelGGL(norm_params_kernel, dim3((unsigned)((2 * p.cols + 63) / 64)), dim3(1024), 0, s, (int32_t)strips, p.cols, (const float *)p.workspace, p.dweight, p.dbias, p.param_dtype);
+        hipLaunchKernelGGL(norm_params_kernel, dim3(few((2 * p.cols + 63) / 64, kParamsBlocks)), dim3(1024), 0, s, (int32_t)strips, p.cols, (const float *)p.workspace, p.dweight, p.dbias, p.param_dtype);
     return hipGetLastError();
 }
 

@@ -121,3 +121,14 @@ def test_layer_norm_gradients_of_spoilt_rows(L, rows, cols, kept):  # noqa: F811
     dx, dw, db = L.layer_norm_backward(dy.cuda(), x8 if kept else x.cuda(), gamma, mean, rstd)
     others = [i for i in range(rows) if i not in (3, 4)]
     assert torch.equal(dx[others], clean[0][others]) and bool(torch.isnan(dx[[3, 4]]).all()) and bool(torch.isnan(dw).all()) and torch.equal(db, clean[2])
+
+
+def test_gradients_of_a_row_of_many_columns(L):  # noqa: F811
+    """2^27 columns and five: more workgroups for dweight and dbias than a grid holds threads of.  One row: the sums are its own values."""
+    cols = (1 << 27) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn(1, cols, generator=g, device="cuda") for _ in range(2))
+    mean, rstd = torch.tensor([0.25], device="cuda"), torch.tensor([2.0], device="cuda")
+    _, dw, db = L.layer_norm_backward(dy, x, None, mean, rstd)
+    assert torch.equal(db, dy[0])
+    assert torch.equal(dw, dy[0] * ((x[0] - 0.25) * 2.0))
