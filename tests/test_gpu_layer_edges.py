@@ -10,7 +10,8 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 from layer_calls import call
-from test_gpu_layers import BF16, F16, F32, LEFT, OUT, TYPES, U, L, gen, rows8_values, values, weights  # noqa: F401
+from test_gpu_layers import (ADDS, BF16, F16, F32, LEFT, OUT, TYPES, U, L, check_norm_grads, close, gen, norm64, norm_tolerance,  # noqa: F401
+                             rows8_values, values, weights)
 
 CODE = {F32: 0, F16: 1, BF16: 2}
 
@@ -132,3 +133,26 @@ def test_gradients_of_a_row_of_many_columns(L):  # noqa: F811
     _, dw, db = L.layer_norm_backward(dy, x, None, mean, rstd)
     assert torch.equal(db, dy[0])
     assert torch.equal(dw, dy[0] * ((x[0] - 0.25) * 2.0))
+
+
+@pytest.mark.parametrize("cols", [16391, 1 << 20, (1 << 22) + 5])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_long_rows_to_the_bound_of_short_ones(L, cols, dtype):  # noqa: F811
+    """A constant row, whose sums round the same way every time, one on an offset and one around zero: mean, rstd, y and dx to the bounds of any length."""
+    g = gen(cols)
+    x, dy = torch.randn(3, cols, generator=g), 0.1 + 0.01 * torch.randn(3, cols, generator=g)
+    x[0], dy[0] = 0.1, 0.1
+    x[1] += 3.0
+    x, dy = x.to(dtype), dy.to(dtype)
+    gamma = 1 + 0.3 * torch.randn(cols, generator=g)
+    y, mean, rstd = L.layer_norm(x.cuda(), gamma.cuda(), None)
+    wy, wm, wr, xh = norm64(x, gamma, None, 1e-5)
+    close(mean, wm, ADDS * U * x.double().abs().mean(1), F32)
+    close(rstd, wr, ADDS * U * wr * (1 + x.double().abs().mean(1) * wr), F32)
+    close(y, wy, norm_tolerance(x, wm, wr, xh, gamma, None), dtype)
+    dx, dw, db = L.layer_norm_backward(dy.cuda(), x.cuda(), gamma.cuda(), mean, rstd)
+    check_norm_grads(dx, dw, db, dy, x.double(), gamma, mean.cpu().double(), rstd.cpu().double(), dtype, F32)
+    spoilt = x.clone()
+    spoilt[1, 7], spoilt[2, 9] = float("inf"), -float("inf")
+    mean = L.layer_norm(spoilt.cuda())[1].tolist()
+    assert mean[1:] == [float("inf"), -float("inf")]
