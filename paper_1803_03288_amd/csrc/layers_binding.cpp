@@ -76,6 +76,10 @@ void check_device(const Tensor &t, const char *name)
         value_error(std::string(name) + " is on " + t.device().str() + ", the current device is cuda:" + str(c10::hip::current_device()));
 }
 
+// The tensor itself, or a copy where it is a view of another's values with their signs turned (the imaginary part of a conjugate): what lies in memory then
+// are the others.
+Tensor own_sign(const Tensor &t) { return t.is_neg() ? t.resolve_neg() : t; }
+
 // Rows of floats: [rows][cols] with the elements of a row next to each other (copied where they are not).
 struct Rows {
     Tensor t;                   // keeps a copy alive
@@ -92,7 +96,7 @@ Rows float_rows(const Tensor &x, const char *name)
     if (dim == 0) value_error(std::string(name) + " has no dimension");
     const int64_t cols = x.size(dim - 1);
     if (cols == 0) value_error(std::string(name) + " has rows of no columns");
-    Tensor t = dim == 2 ? x : x.reshape({-1, cols});
+    Tensor t = own_sign(dim == 2 ? x : x.reshape({-1, cols}));
     if ((t.stride(1) != 1 && cols > 1) || t.stride(0) < 0) t = t.contiguous();
     const int64_t rows = t.size(0);
     return Rows{t, dt, rows, cols, rows > 1 ? t.stride(0) : cols};
@@ -112,7 +116,7 @@ Vector vector(PyObject *o, const char *name, int64_t n, at::ScalarType type, con
     if (t.dim() != 1 || t.size(0) != n) value_error(std::string(name) + " has another shape than (" + str(n) + ",)");
     if (t.scalar_type() != at::kFloat && t.scalar_type() != type) type_error(std::string(name) + " is " + toString(t.scalar_type()) + ": expected float32 or " + toString(type));
     if (t.device() != like.device()) value_error(std::string(name) + " is on " + t.device().str() + ", expected " + like.device().str());
-    v.t = t.is_contiguous() ? t : t.contiguous();
+    v.t = own_sign(t.is_contiguous() ? t : t.contiguous());
     v.data = v.t.data_ptr();
     v.dtype = dtype_code(t.scalar_type());
     return v;
@@ -122,17 +126,18 @@ Tensor statistic(PyObject *o, const char *name, int64_t rows, const Tensor &like
     const Tensor &t = tensor(o, name);
     if (t.scalar_type() != at::kFloat || t.numel() != rows || t.device() != like.device())
         value_error(std::string(name) + ": expected " + str(rows) + " float32 values on " + like.device().str());
-    return t.is_contiguous() ? t : t.contiguous();
+    return own_sign(t.is_contiguous() ? t : t.contiguous());
 }
 
 int64_t padded(int64_t cols) { return (cols + 127) / 128 * 128; }
 
 // 8-bit rows, a tuple (q, scale, cols, group).
 struct Rows8 {
-    const Tensor *q, *scale;
+    const Tensor *q;
+    Tensor scale;
     int64_t rows, cols, group, ld;
     const int8_t *data() const { return (const int8_t *)q->data_ptr(); }
-    const float *scales() const { return (const float *)scale->data_ptr(); }
+    const float *scales() const { return (const float *)scale.data_ptr(); }
 };
 bool is_rows8(PyObject *o) { return PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4; }
 Rows8 rows8(PyObject *o, const char *name, int64_t group, const at::Device *device)       // group -1: any
@@ -140,19 +145,19 @@ Rows8 rows8(PyObject *o, const char *name, int64_t group, const at::Device *devi
     if (!is_rows8(o)) type_error(std::string(name) + ": expected Rows8");
     Rows8 r;
     r.q = &tensor(PyTuple_GET_ITEM(o, 0), name);
-    r.scale = &tensor(PyTuple_GET_ITEM(o, 1), name);
+    r.scale = own_sign(tensor(PyTuple_GET_ITEM(o, 1), name));
     r.cols = PyLong_AsLongLong(PyTuple_GET_ITEM(o, 2));
     r.group = PyLong_AsLongLong(PyTuple_GET_ITEM(o, 3));
     if (PyErr_Occurred()) { PyErr_Clear(); type_error(std::string(name) + ": cols and group are whole numbers"); }
     if (r.group != 0 && r.group != kGroup) value_error(std::string(name) + ": a group of " + str(r.group) + ", expected 0 or " + str(kGroup));
     if (group >= 0 && r.group != group) value_error(std::string(name) + " has a scale per " + (r.group ? str(r.group) : "row") + ", expected one per " + (group ? str(group) : "row"));
-    if (r.q->scalar_type() != at::kChar || r.q->dim() != 2 || r.scale->scalar_type() != at::kFloat) type_error(std::string(name) + ": expected int8 rows and float32 scales");
+    if (r.q->scalar_type() != at::kChar || r.q->dim() != 2 || r.scale.scalar_type() != at::kFloat) type_error(std::string(name) + ": expected int8 rows and float32 scales");
     if (!device) check_device(*r.q, name);
-    if (r.q->device() != (device ? *device : r.scale->device()) || r.scale->device() != r.q->device()) value_error(std::string(name) + " is on another device");
+    if (r.q->device() != (device ? *device : r.scale.device()) || r.scale.device() != r.q->device()) value_error(std::string(name) + " is on another device");
     r.rows = r.q->size(0);
-    if (r.cols < 1 || r.q->size(1) < padded(r.cols) || r.q->stride(1) != 1 || !r.scale->is_contiguous())
+    if (r.cols < 1 || r.q->size(1) < padded(r.cols) || r.q->stride(1) != 1 || !r.scale.is_contiguous())
         value_error(std::string(name) + ": rows of " + str(r.cols) + " columns are padded to " + str(padded(r.cols)) + ", contiguous, and so are their scales");
-    if (r.scale->numel() != r.rows * (r.group ? (r.cols + kGroup - 1) / kGroup : 1)) value_error(std::string(name) + ": " + str(r.scale->numel()) + " scales for " + str(r.rows) + " rows");
+    if (r.scale.numel() != r.rows * (r.group ? (r.cols + kGroup - 1) / kGroup : 1)) value_error(std::string(name) + ": " + str(r.scale.numel()) + " scales for " + str(r.rows) + " rows");
     r.ld = r.rows > 1 ? r.q->stride(0) : padded(r.q->size(1));
     return r;
 }

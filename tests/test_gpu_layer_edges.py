@@ -156,3 +156,26 @@ def test_long_rows_to_the_bound_of_short_ones(L, cols, dtype):  # noqa: F811
     spoilt[1, 7], spoilt[2, 9] = float("inf"), -float("inf")
     mean = L.layer_norm(spoilt.cuda())[1].tolist()
     assert mean[1:] == [float("inf"), -float("inf")]
+
+
+def test_views_with_turned_signs(L):  # noqa: F811
+    """Tensors whose memory holds the negatives of their values (torch's lazy negation) count as their values."""
+    g = gen(12)
+    neg = torch._neg_view
+    x, dy, gamma, beta = (torch.randn(*s, generator=g).cuda() for s in ((6, 200), (6, 200), (200,), (200,)))
+    w, bias = weights(L, g, 200, 200), torch.randn(200, generator=g).cuda()
+    z = torch.view_as_complex(torch.randn(5, 2, generator=g).cuda()).conj().imag[:, None]
+    assert z.is_neg() and torch.equal(L.layer_norm(z, eps=1.0)[1], z[:, 0].clone())
+    n = L.layer_norm(-x, -gamma, -beta, save=True)
+    x8, back = n[3], L.layer_norm_backward(-dy, -x, -gamma, -n[1], -n[2])
+    turned = L.Rows8(w.q, -w.scale, 200)
+
+    def same(a, b):
+        assert all(torch.equal(s, t) for s, t in zip(a, b) if isinstance(s, torch.Tensor))
+
+    same(L.quantize_rows(neg(x)), L.quantize_rows(-x))
+    same(L.layer_norm(neg(x), neg(gamma), neg(beta), save=True)[:3], n[:3])
+    same(L.layer_norm_backward(neg(dy), neg(x), neg(gamma), neg(n[1]), neg(n[2])), back)
+    same([L.linear_q8(neg(x), L.Rows8(w.q, neg(w.scale), 200), neg(bias))], [L.linear_q8(-x, turned, -bias)])
+    same(L.linear_q8_backward(neg(dy), L.quantize_rows(x), w), L.linear_q8_backward(-dy, L.quantize_rows(x), w))
+    same([L.dequantize_rows(L.Rows8(x8.q, neg(x8.scale), 200, 128))], [-L.dequantize_rows(x8)])
