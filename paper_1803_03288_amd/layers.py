@@ -12,7 +12,8 @@ transferred in 8 bits, a quarter of the bytes of float32, and whose activations 
 
 Tensors are CUDA tensors of float32, float16 or bfloat16; the last dimension is the row, and outputs have the shape of
 the input in the others.  Rows may lie at any stride; elements of a row that are not next to each other are copied first.
-Everything runs on the current stream; there is no CPU fallback.  A wrong argument raises ``ValueError`` or ``TypeError``, what the library
+Everything runs on the current stream; there is no CPU fallback.  There is no autograd either: outputs carry no graph, also where an input requires a
+gradient, and the backward passes are calls of their own, to be made by hand or from a ``torch.autograd.Function``.  A wrong argument raises ``ValueError`` or ``TypeError``, what the library
 refuses ``TicTacError``.
 """
 

@@ -179,3 +179,13 @@ def test_views_with_turned_signs(L):  # noqa: F811
     same([L.linear_q8(neg(x), L.Rows8(w.q, neg(w.scale), 200), neg(bias))], [L.linear_q8(-x, turned, -bias)])
     same(L.linear_q8_backward(neg(dy), L.quantize_rows(x), w), L.linear_q8_backward(-dy, L.quantize_rows(x), w))
     same([L.dequantize_rows(L.Rows8(x8.q, neg(x8.scale), 200, 128))], [-L.dequantize_rows(x8)])
+
+
+def test_outputs_carry_no_graph(L):  # noqa: F811
+    """As the module says: no output requires a gradient, whatever the inputs do."""
+    x, gamma, dy = (torch.randn(*s, device="cuda", requires_grad=True) for s in ((4, 200), (200,), (4, 200)))
+    w = weights(L, gen(1), 200, 200)
+    y, mean, rstd, x8 = L.layer_norm(x, gamma, save=True)
+    out = [y, mean, rstd, x8.q, x8.scale, L.linear_q8(x, w, gamma), L.dequantize_rows(x8)]
+    out += L.layer_norm_backward(dy, x, gamma, mean, rstd) + L.linear_q8_backward(dy, L.quantize_rows(x), w)
+    assert not any(t.requires_grad or t.grad_fn for t in out) and "no autograd" in L.__doc__
