@@ -344,7 +344,8 @@ int tictac_dequantize_rows(int32_t dtype, int64_t rows, int64_t cols, const int8
  *   weight, bias [cols] of param_dtype, may be NULL (ones, zeros)
  *   y                   may be NULL
  *   mean, rstd [rows]   float32, for the backward pass
- *   yq, y_scale         may be NULL: y as 8-bit rows of group 0, formed from the float32 values
+ *   yq, y_scale         may be NULL: y as 8-bit rows of group 0, formed from the float32 values (near the middle of two steps the order of
+ *                       the float32 sums decides which of them is taken)
  *   xq, x_scale         may be NULL: x as 8-bit rows of group 128, to be kept for the backward pass */
 int tictac_layer_norm(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ld_x, int32_t param_dtype, const void *weight,
                       const void *bias, float eps, void *y, int64_t ld_y, float *mean, float *rstd, int8_t *yq, int64_t ld_yq,
@@ -370,7 +371,10 @@ int tictac_linear_q8(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, co
                      const void *bias, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, tictac_stream stream);
 
 /* Gradients of the above, the rounding of x taken for the identity: dx[t][i] = sum_o dy[t][o] w_scale[o] wq[o][i],
- * dw[o][i] = sum_t dy[t][o] x_scale[t] xq[t][i], db[o] = sum_t dy[t][o]; all of dtype, each may be NULL.  xq and x_scale are read for dw
+ * dw[o][i] = sum_t dy[t][o] x_scale[t] xq[t][i], db[o] = sum_t dy[t][o]; all of dtype, each may be NULL.  The products are of bfloat16 values,
+ * with sums in float32.  8-bit values are exact in it; dy times a scale takes three for float32 (exact) and two for float16 (off by 2^-15 at most).  For bfloat16
+ * it takes one, rounded, and with more than 64 rows dy is taken as it is and the 8-bit value times its scale is rounded: each term is off by up to 2^-8 of
+ * itself, beside the rounding of the output (1.4 times the error of that alone).  float32 dy gives the gradients without it.  xq and x_scale are read for dw
  * alone, wq and w_scale for dx alone: without that output they may be NULL. */
 int tictac_linear_q8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
 int tictac_linear_q8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *dy, int64_t ld_dy, const int8_t *xq,

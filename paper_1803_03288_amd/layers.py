@@ -78,7 +78,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
 
 
 def layer_norm_q8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, save: bool = False):
-    """``(y8, mean, rstd)``: layer norm whose output is 8-bit rows, the operand of ``linear_q8``; ``save`` as in ``layer_norm``."""
+    """``(y8, mean, rstd)``: layer norm whose output is 8-bit rows, formed from its float32 values, the operand of ``linear_q8``; ``save`` as in ``layer_norm``."""
     if not save:
         q, scale, mean, rstd = (_module or _native()).layer_norm(x, weight, bias, eps, True, False)
         return Rows8(q, scale, x.shape[-1]), mean, rstd
@@ -100,5 +100,7 @@ def linear_q8(x: Union[torch.Tensor, Rows8], w: Rows8, bias: Optional[torch.Tens
 
 def linear_q8_backward(dy: torch.Tensor, x: Rows8, w: Rows8):
     """``(dx, dw, db)`` of ``linear_q8`` from the 8-bit rows that the forward pass took, all of the type of ``dy``; the rounding of the
-    input counts as the identity."""
+    input counts as the identity.  The products are of bfloat16 values with sums in float32: ``dy`` times a scale takes three of them for float32 (exact) and
+    two for float16, but for bfloat16 one factor of each term is rounded to 8 bits (up to 2^-8 of it, beside the rounding of the outputs); ``dy`` in
+    float32 avoids that."""
     return (_module or _native()).linear_q8_backward(dy, x, w)
