@@ -322,7 +322,8 @@ __device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, i
 // behind the last barrier of a tile LDS is free, and the first two steps of the next tile are asked for before this one's outputs are formed.
 // Two blocks of 16 rows share 32 rows of p in turns of four (row 4 n + e of block 2 m + h is row 32 m + 8 n + 4 h + e of the tile), so that a lane has
 // eight outputs next to each other and stores sixteen bytes of bf16 straight from its registers.
-// 8192 x 4096 x 16384 int8: a step takes 1.45 us of a workgroup (2.9 POP/s while it lasts; the clock is down to 1.88 GHz then), 450 us in all.
+// 8192 x 4096 x 16384 int8: a step takes 1.45 us of a workgroup (2.9 POP/s while it lasts), 464 to 499 us in all, by the clock that the
+// power limit leaves (2.04 to 1.98 GHz).
 template <class OP, int OUT>
 __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 {
