@@ -195,12 +195,11 @@ static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
     return parts_along_k(blocks, units / kFewWaves, 256);                   // a unit for each wave at least
 }
 
-constexpr int64_t kWrapCols = 131072;           // (exact_sum; the most that are taken)
 static ProductPlan forward_plan(int64_t rows, int64_t cols, int64_t outs)
 {
     if (rows <= kFewRows) return {0, {few_splits(rows, cols, outs), 1}};
     const ProductShape shape{(int32_t)outs, (int32_t)rows, (int32_t)(rows8_stride(cols) / 128)};
-    return plan_products(&shape, 1, cols == kWrapCols);
+    return plan_products(&shape, 1);
 }
 size_t linear_q8_workspace(int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
@@ -642,7 +641,7 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.padded_o = (outs + 63) / 64 * 64;
     r.padded_t = (rows + 63) / 64 * 64;
     const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / 64 * pieces)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / 64 * pieces)}};
-    r.plan = plan_products(shapes, 2, false);
+    r.plan = plan_products(shapes, 2);
     r.p_x = r.sums + up((size_t)(r.padded_t / 64) * outs * 4);
     r.p_w = r.p_x + up((size_t)cols * r.padded_o * 2);
     r.q_x = r.p_w + up((size_t)cols * r.padded_t * 2);

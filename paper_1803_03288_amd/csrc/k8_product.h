@@ -27,7 +27,9 @@ struct ProductArgs {
 };
 
 // A sum of products of int8 values, as float32.  131 072 of -128 and -128 come to 2^31, one more than int32 holds, and wrap round to -2^31, which no other
-// sum of as many is: the least is 131 072 (-128) 127.  (Not in product_kernel_256, where it would cost 0.7 % of every product: that kernel takes fewer columns.)
+// sum of as many is: the least is 131 072 (-128) 127.  The tiles have kernels of their own for so many columns (the comparison costs 0.7 % of 8192 x 4096 -> 16384
+// and of 4165 x 916 -> 5071; 8192 x 131072 -> 8192 by tiles of 128 x 128 instead of 256 x 256: 9.4 ms, 8.1).
+constexpr int32_t kWidest = 131072;         // the most columns that are taken
 __device__ __forceinline__ float exact_sum(int32_t sum) { return sum == INT32_MIN ? 0x1p31f : (float)sum; }
 
 // Sums of `parts` rows of floats, [parts][n], in their order, as a vector of `dtype`: rides along with the products of a backward pass.
@@ -44,7 +46,7 @@ struct ProductPlan {
     int32_t tile;               // one of kTiles, or kTile256
     int32_t splits[2];
 };
-ProductPlan plan_products(const ProductShape *shapes, int n, bool wraps);      // wraps: sums may be 2^31 (exact_sum)
+ProductPlan plan_products(const ProductShape *shapes, int n);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
 hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s);
 hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s);     // one or two products, of one output type, in one launch

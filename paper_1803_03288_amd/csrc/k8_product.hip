@@ -13,9 +13,12 @@ typedef const __attribute__((address_space(1))) void global_void;
 struct OpI8 {
     typedef i32x4 acc;
     typedef uint32_t sum;               // (adding up wraps, defined)
-    static __device__ __forceinline__ float value(int32_t s) { return exact_sum(s); }
+    static __device__ __forceinline__ float value(int32_t s) { return (float)s; }
     static __device__ __forceinline__ acc mma(i32x4 a, i32x4 b, acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
     static __device__ __forceinline__ void mma_in_place(i32x4 a, i32x4 b, acc &c) { asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
+};
+struct OpI8Widest : OpI8 {              // of kWidest columns
+    static __device__ __forceinline__ float value(int32_t s) { return exact_sum(s); }
 };
 struct OpBf16 {
     typedef f32x4 acc;
@@ -63,6 +66,8 @@ template <class OP>
 struct Scaled { static constexpr bool value = false; };
 template <>
 struct Scaled<OpI8> { static constexpr bool value = true; };
+template <>
+struct Scaled<OpI8Widest> { static constexpr bool value = true; };
 
 constexpr int kParts = 3;           // in the place of an output type: sums of a split, as they are
 
@@ -450,7 +455,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    v[e] = (float)acc[2 * i + (e >> 2)][j][e & 3];
+                    v[e] = OP::value(acc[2 * i + (e >> 2)][j][e & 3]);
                     if (kScaled) v[e] = v[e] * (qs * s[e]) + b[e];
                 }
                 const int32_t row = row0 + r + i * 32, column = col0 + c + j * 16;
@@ -549,7 +554,7 @@ struct Tile { int32_t r, c; float fixed, step, step2; };
 constexpr Tile kTiles[] = {{4, 4, 7.6f, 0.5f, 0.85f}, {4, 2, 6.0f, 0.33f, 0.56f}, {2, 2, 5.1f, 0.26f, 0.37f}};
 constexpr int32_t kTile256 = 3;
 
-ProductPlan plan_products(const ProductShape *shapes, int n, bool wraps)
+ProductPlan plan_products(const ProductShape *shapes, int n)
 {
     ProductPlan best{0, {1, 1}};
     float least = 1e30f;
@@ -598,7 +603,7 @@ ProductPlan plan_products(const ProductShape *shapes, int n, bool wraps)
     for (int i = 0; i < n; ++i) each[i] = 6.0f + step * (float)shapes[i].steps;
     const int64_t turns = (tiles[0] + tiles[1] + 255) / 256, early = tiles[0] / 256, late = (tiles[0] + 255) / 256;
     const float us = 4.0f + 5.0f * (float)(turns - 1) + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
-    if (!wraps) take(kTile256, {1, 1}, us);
+    take(kTile256, {1, 1}, us);
     return best;
 }
 
@@ -656,9 +661,12 @@ static hipError_t join(const ProductArgs &a, hipStream_t s)
     return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(&a, 1, s) : join_as<OP, TICTAC_BF16>(&a, 1, s);
 }
 
-hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8>(a, s); }
+hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8Widest>(a, s); }
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s) { return join<OpBf16>(a, s); }
-hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s) { return launch<OpI8>(&a, 1, tile, ColumnSums{}, s); }
+hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s)
+{
+    return a.steps < kWidest / 128 ? launch<OpI8>(&a, 1, tile, ColumnSums{}, s) : launch<OpI8Widest>(&a, 1, tile, ColumnSums{}, s);
+}
 hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s) { return launch<OpBf16>(a, n, tile, c, s); }
 
 }  // namespace tictac

@@ -46,7 +46,7 @@ def test_linear_gradients_one_at_a_time(L, rows, cols, outs, dtype):  # noqa: F8
 
 
 # (by few rows with and without cuts along k, and by tiles with and without)
-@pytest.mark.parametrize("rows,outs", [(1, 16), (20, 200), (40, 5000), (70, 60), (300, 2100), (600, 6000)])
+@pytest.mark.parametrize("rows,outs", [(1, 16), (20, 200), (40, 5000), (70, 60), (300, 2100), (600, 6000), (1024, 16384)])
 def test_the_largest_sum(L, rows, outs):  # noqa: F811
     """131 072 products of -128 and -128 are 2^31, and of -128 and 127 the least there is."""
     cols = 131072
