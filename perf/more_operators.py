@@ -149,7 +149,7 @@ def _update_state(case, g, state):
     held = torch.zeros(total, dtype=torch.bool, device="cuda")
     for at, n in zip(starts, numels):
         held[at:at + n] = True
-    size = torch.empty(total, device="cuda")                # every tensor's gradients have a size of their own
+    size = torch.zeros(total, device="cuda")                # every tensor's gradients have a size of their own
     for at, n in zip(starts, numels):
         size[at:at + n] = 1e-4 * 4.0 ** (hash((n, at)) % 5)
     loss_scale = 1024.0 if case["grad"] == "f16" else 1.0
