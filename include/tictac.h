@@ -17,8 +17,9 @@
  *   7. the time oracle estimate from measured runs         (Sec. 5)
  *   8. a search for better orders by proposed exchanges,
  *      measured by 4                                       (Sec. 3.1, 4.3)
- *   9. operators of a worker's layers in 8 bits: what runs
- *      between the transfers, to be timed by 7
+ *   9. operators of a worker's layers in 8 bits, and the
+ *      update of their parameters: what runs between the
+ *      transfers, to be timed by 7
  * 3 and 4 also take the timing samples as float32 arrays (tictac_simulate_f32,
  * tictac_tac_simulate_f32).
  *
@@ -381,6 +382,97 @@ int tictac_linear_q8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t
                               int64_t ld_xq, const float *x_scale, const int8_t *wq, int64_t ld_w, const float *w_scale, void *dx,
                               int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,
                               tictac_stream stream);
+
+/*
+ * ---- Training in 8-bit floats: products with a scale per block of 128, and the update ----
+ * The format, "8-bit floats in blocks": e4m3 or e5m2 (tictac_f8; the types without and with infinities, as the matrix instructions of gfx950 take them), [rows][ld], ld a
+ * multiple of 128, on a 16-byte boundary, every row readable up to the next multiple of 128 columns and zero from its last column to there.  A block is 128 columns of one row
+ * (block = 1) or of 128 rows (block = 128); its scale is a power of two, held as a byte, exponent + 127 (255: NaN), [ceil(rows / block)][ld_scale], ld_scale a multiple of four, on a
+ * 4-byte boundary, every row readable up to the next multiple of four bytes.  The value is q times the scale.  Scales lose nothing by being powers of two but one power at the
+ * lower end of the type; scaling is exact.
+ * What stands above for the layers' operators holds for these too, strides, workspaces, streams and capture among it.
+ */
+typedef enum tictac_f8 {
+    TICTAC_E4M3 = 0,               /* largest value 448, least 2^-9 */
+    TICTAC_E5M2 = 1                /* largest value 57344, least 2^-16 */
+} tictac_f8;
+
+typedef struct tictac_float8 {
+    void *q;
+    int64_t ld;
+    uint8_t *scale;
+    int64_t ld_scale;
+    int32_t format;                /* tictac_f8 */
+    int32_t block;                 /* rows of a block: 1 or 128 */
+} tictac_float8;
+
+/* The scale of a block is the least power of two from 2^-126 on with which its largest magnitude is no larger than the type's largest value, q = x / scale, ties to even (so blocks
+ * below 2^-136, or 2^-143, read as zeros, and what would be rounded to 2^128 gets the value below it).  A NaN or an infinity makes the whole block NaN.  Written: to->q up to the next multiple of 128 columns, to->scale up to the next
+ * multiple of four, zeros behind the end. */
+int tictac_quantize_f8(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ld_x, const tictac_float8 *to, tictac_stream stream);
+
+/* x = q * scale, rounded to dtype. */
+int tictac_dequantize_f8(int32_t dtype, int64_t rows, int64_t cols, const tictac_float8 *from, void *x, int64_t ld_x, tictac_stream stream);
+
+/* y[t][o] = sum_i x[t][i] w[o][i] + bias[o].
+ *   x  [rows][cols] of dtype, rounded to e4m3 in blocks of one row in the call, or NULL: x8, of either format and block
+ *   w  [outs][cols] in e4m3, of either block
+ *   bias [outs] of bias_dtype, may be NULL
+ * float32 outputs are of exact products with sums in float32.  float16 and bfloat16 ones come from the matrix instructions for 8-bit floats, which cut
+ * off what products have below about 2^-13 of the largest that they are added with (1.4e-5 of the result for normal values; the outputs' own rounding is 2^-12 or 2^-9).
+ * At most 2^21 rows and outputs, 2^17 columns, strides up to 2^24 (TICTAC_ERR_UNSUPPORTED). */
+int tictac_linear_f8_workspace(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
+int tictac_linear_f8(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *x, int64_t ld_x, const tictac_float8 *x8, const tictac_float8 *w,
+                     int32_t bias_dtype, const void *bias, void *y, int64_t ld_y, void *workspace, size_t workspace_bytes, tictac_stream stream);
+
+/* Gradients of the above, the rounding of x taken for the identity; all of dtype, each may be NULL.  An operand's blocks lie along what is summed over:
+ *   dx[t][i] = sum_o A[t][o] W[o][i]    A: dy in `format`, blocks of 128 outputs of a row; W: w, in blocks of 128 outputs of a column
+ *   dw[o][i] = sum_t B[t][o] X[t][i]    B: dy in `format`, blocks of 128 rows of a column; X: x8, in blocks of 128 rows of a column
+ *   db[o] = sum_t dy[t][o]
+ * W and X are rounded again, to e4m3: W is w itself where its blocks are of 128 rows, and else, as X, what scales of powers of two let differ (values that
+ * get 2^-15 of a block's largest or less).  Sums as in tictac_linear_f8.  x8 is read for dw alone, w for dx alone. */
+int tictac_linear_f8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
+int tictac_linear_f8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *dy, int64_t ld_dy, int32_t format, const tictac_float8 *x8,
+                              const tictac_float8 *w, void *dx, int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,
+                              tictac_stream stream);
+
+/* norm = scale * sqrt(sum of the squares of all elements of n tensors), squares and sums in float64 in a fixed order; norm: one float on the device.  n >= 0. */
+typedef struct tictac_gradient {
+    const void *g;                 /* device, contiguous */
+    int64_t numel;
+    int32_t dtype;
+} tictac_gradient;
+int tictac_gradient_norm_workspace(int32_t n, size_t *bytes);
+int tictac_gradient_norm(int32_t n, const tictac_gradient *gradients, float scale, float *norm, void *workspace, size_t workspace_bytes, tictac_stream stream);
+
+/* One step of AdamW over n tensors, in place:
+ *     g = c gradient,  c = grad_scale min(1, max_norm / *norm)
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g
+ *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in float32, p and copy rounded to their types.  Moments in 32 bits: float32 m and v, m_scale and v_scale NULL.  In 8 bits: m and sqrt(v) as one row each of numel columns of e4m3 in
+ * blocks (above), rounded at random: with 16 bits u of a hash, steps = floor(|x| / step + u / 2^16).  The hash of element i of the tensor with index j of the call is
+ *     mix(mix(mix(mix(mix(seed low) + seed high) + step) + j) + i),   mix(x): x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0x6A09E667, x ^= x >> 16
+ * in 32 bits, its low half for m, its high half for sqrt(v): the same call has the same result.
+ * norm may be NULL (max_norm is not used then); where *norm is not finite nothing is changed.  lr_at and step_at, device, may be NULL; they stand for lr and step, for
+ * calls that are captured.  step counts from 1.  Tensors may not overlap (TICTAC_ERR_UNSUPPORTED); at most 2^32 elements each. */
+typedef struct tictac_adamw_tensor {
+    void *p;                       /* device, contiguous, of dtype, as all of these */
+    const void *g;                 /* of grad_dtype */
+    void *m, *v;
+    uint8_t *m_scale, *v_scale;
+    void *copy;                    /* NULL, or the new p in copy_dtype */
+    int64_t numel;
+    int32_t dtype, grad_dtype, copy_dtype;
+} tictac_adamw_tensor;
+typedef struct tictac_adamw_options {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;
+    uint64_t seed;
+    float grad_scale, max_norm;
+    const float *norm, *lr_at;
+    const int64_t *step_at;
+} tictac_adamw_options;
+int tictac_adamw_step(int32_t n, const tictac_adamw_tensor *tensors, const tictac_adamw_options *options, tictac_stream stream);
 
 /* Message of the last error on the calling thread; valid until its next call. */
 const char *tictac_last_error(void);

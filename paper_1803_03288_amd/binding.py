@@ -37,6 +37,8 @@ EXPORTS = (
     "tictac_quantize_rows", "tictac_dequantize_rows", "tictac_layer_norm", "tictac_layer_norm_backward_workspace",
     "tictac_layer_norm_backward", "tictac_linear_q8_workspace", "tictac_linear_q8", "tictac_linear_q8_backward_workspace",
     "tictac_linear_q8_backward",
+    "tictac_quantize_f8", "tictac_dequantize_f8", "tictac_linear_f8_workspace", "tictac_linear_f8", "tictac_linear_f8_backward_workspace",
+    "tictac_linear_f8_backward", "tictac_gradient_norm_workspace", "tictac_gradient_norm", "tictac_adamw_step",
     "tictac_last_error", "tictac_version",
 )
 

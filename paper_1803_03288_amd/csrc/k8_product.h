@@ -19,7 +19,7 @@ struct ProductArgs {
     void *out;
     int64_t ld_out;
     int32_t dtype;              // of out
-    // int8: out = sum * (q_scale[c] * p_scale[r]) + bias[r]; bf16: out = sum
+    // int8: out = sum * (q_scale[c] * p_scale[r]) + bias[r]; bf16: out = sum, or sum + bias[r]
     const float *p_scale, *q_scale;
     const void *bias;
     int32_t bias_dtype;
@@ -50,7 +50,9 @@ ProductPlan plan_products(const ProductShape *shapes, int n);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
 hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s);
 hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s);     // one or two products, of one output type, in one launch
+hipError_t launch_product_bf16_biased(const ProductArgs &a, int32_t tile, hipStream_t s);      // float32 outputs, bias added
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s);        // the sums in `parts` to the output
 hipError_t launch_product_join_bf16(const ProductArgs &a, hipStream_t s);
+hipError_t launch_product_join_biased(const ProductArgs &a, hipStream_t s);    // float32 sums, bias added
 
 }  // namespace tictac

@@ -2,13 +2,9 @@
 // bytes of k, several buffers in turn: while one is computed from, the next steps are under way into the others, straight from memory to LDS.
 #include <algorithm>
 
-#include "device_utils.h"
-#include "k8_product.h"
+#include "k8_tiles.h"
 
 namespace tictac {
-
-typedef __attribute__((address_space(3))) void lds_void;
-typedef const __attribute__((address_space(1))) void global_void;
 
 struct OpI8 {
     typedef i32x4 acc;
@@ -30,184 +26,13 @@ struct OpBf16 {
     }
     static __device__ __forceinline__ void mma_in_place(i32x4 a, i32x4 b, acc &c) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b)); }
 };
-
-// ---- outputs ----
-// Eight outputs r .. r + 7 of a column from their sums.  The scales and the bias of r are the same for all columns of a thread.
-template <bool SCALED>
-struct Finish8 {
-    float scale[8], bias[8];
-    __device__ __forceinline__ void init(const ProductArgs &a, int32_t r)
-    {
-        if (!SCALED) return;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            scale[i] = r + i < a.R ? a.p_scale[r + i] : 0.0f;
-            bias[i] = a.bias && r + i < a.R ? param(a.bias, a.bias_dtype, r + i) : 0.0f;
-        }
-    }
-    template <int DT>
-    __device__ __forceinline__ void store(const ProductArgs &a, int32_t r, int32_t c, const float *sum, bool wide) const
-    {
-        float v[8];
-        if (SCALED) {
-            const float qs = a.q_scale[c];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = sum[i] * (qs * scale[i]) + bias[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = sum[i];
-        }
-        typename Elem<DT>::type *row = (typename Elem<DT>::type *)a.out + (int64_t)c * a.ld_out;
-        if (wide) store8<DT, true>(row, r, a.R, v);
-        else store8<DT, false>(row, r, a.R, v);
-    }
-};
-template <class OP>
-struct Scaled { static constexpr bool value = false; };
+struct OpBf16Biased : OpBf16 {};
 template <>
 struct Scaled<OpI8> { static constexpr bool value = true; };
 template <>
 struct Scaled<OpI8Widest> { static constexpr bool value = true; };
-
-constexpr int kParts = 3;           // in the place of an output type: sums of a split, as they are
-
-// What a wave holds, FR x FC blocks of 16 x 16 from (r, c) on, goes column by column through its own part of LDS, so that a thread has eight
-// consecutive outputs.  Lane l of a block holds rows 4 (l / 16) .. + 3 of column l % 16.
-template <class OP, int OUT, int FR, int FC>
-__device__ __forceinline__ void put_blocks(const ProductArgs &a, const typename OP::acc (&acc)[FR][FC], int32_t r, int32_t c, int32_t split, char *room)
-{
-    typedef typename OP::acc A;
-    constexpr int kStride = FR * 16 + 4, kThreads = FR * 2, kColumns = 64 / kThreads;       // words; threads per column; columns at a time
-    const int lane = threadIdx.x & 63, part = lane % kThreads, first = lane / kThreads;
-    A *to = (A *)room + ((lane & 15) * kStride + (lane >> 4) * 4) / 4;
-    const A *from = (const A *)room + (first * kStride + part * 8) / 4;
-    const int32_t mine = r + part * 8;
-    Finish8<Scaled<OP>::value && OUT != kParts> finish;
-    finish.init(a, mine);
-    const bool wide = OUT != kParts && (a.ld_out * (OUT == TICTAC_F32 ? 4 : 2)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
-#pragma unroll
-    for (int j = 0; j < FC; ++j) {
-#pragma unroll
-        for (int i = 0; i < FR; ++i) to[i * 4] = acc[i][j];
-        wave_sync();
-#pragma unroll
-        for (int k = 0; k < 16 / kColumns; ++k) {
-            const A lo = from[k * kColumns * kStride / 4], hi = from[k * kColumns * kStride / 4 + 1];
-            const int32_t column = c + j * 16 + k * kColumns + first;
-            if (column >= a.C || mine >= a.R) continue;
-            if constexpr (OUT == kParts) {
-                A *out = (A *)((uint32_t *)a.parts + ((int64_t)split * a.C + column) * a.R + mine);
-                if (a.R % 8 == 0) {
-                    out[0] = lo;
-                    out[1] = hi;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const auto sum = e < 4 ? lo[e & 3] : hi[e & 3];         // (a bit cast of a vector's element itself takes its first element)
-                        if (mine + e < a.R) ((uint32_t *)out)[e] = __builtin_bit_cast(uint32_t, sum);
-                    }
-                }
-            } else {
-                float sum[8];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { sum[e] = OP::value(lo[e]); sum[4 + e] = OP::value(hi[e]); }
-                finish.template store<OUT>(a, mine, column, sum, wide);
-            }
-        }
-        wave_sync();
-    }
-}
-
-// ---- tiles ----
-// What one launch does: up to two products, a run of workgroups each, and the sums of columns.
-struct Products {
-    ProductArgs a[2];
-    int32_t tiles_r[2], tiles_c[2];
-    int32_t first[3];                   // tiles (times splits) from first[i] on: product 0, product 1, none
-    int32_t sum_blocks;                 // the last workgroups: sums
-    ColumnSums sums;
-};
-
-__device__ __forceinline__ void column_sums(const ColumnSums &c, int32_t block, float *room)        // 64 columns per workgroup
-{
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    const int64_t at = (int64_t)block * 64 + lane, per = (c.parts + waves - 1) / waves;
-    float sum = 0.0f;
-    if (at < c.n)
-        for (int64_t k = wave * per; k < min(c.parts, (wave + 1) * per); ++k) sum += c.sums[k * c.n + at];
-    room[wave * 64 + lane] = sum;
-    __syncthreads();
-    if (wave || at >= c.n) return;
-    sum = 0.0f;
-    for (int k = 0; k < waves; ++k) sum += room[k * 64 + lane];
-    put_param(c.out, c.dtype, at, sum);
-}
-
-// Workgroups go to the eight XCDs in turn; each XCD gets a run of consecutive tiles, and a run goes down eight columns of tiles side by side,
-// so that what an XCD's L2 holds is used again.
-__device__ __forceinline__ void tile_of(int32_t block, int32_t tiles_r, int32_t tiles_c, int32_t &split, int32_t &tr, int32_t &tc)
-{
-    const int32_t tiles = tiles_r * tiles_c;
-    int32_t at = block % tiles;
-    split = block / tiles;
-    const int32_t xcd = at & 7, whole = tiles >> 3, more = tiles & 7;
-    at = xcd * whole + min(xcd, more) + (at >> 3);
-    const int32_t band = at / (8 * tiles_r), in_band = at - band * 8 * tiles_r, width = min(8, tiles_c - band * 8);
-    tr = in_band / width;
-    tc = band * 8 + in_band % width;
-}
-
-// The loads of a tile.  A load brings 8 rows of 128 bytes to LDS, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i
-// holds the bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.  Rows behind the end are the last row again; nobody
-// stores what comes of them.
-// PAIRED: rows of p go to the places that suit the reads of product_kernel_256, j ^ (i % 4 + 4 (i / 8 % 2)).
-template <int TR, int TC, int WAVES, bool PAIRED>
-struct TileLoads {
-    static constexpr int LP = TR / 8 / WAVES, LQ = TC / 8 / WAVES;      // per wave and step
-    uint32_t off_p[LP], off_q[LQ];
-    const char *p, *q;
-    int32_t p_left;                     // steps until p starts again
-    __device__ __forceinline__ void init(const ProductArgs &a, int32_t r0, int32_t c0, int32_t first, int wave)
-    {
-        static_assert(WAVES % 2 == 0, "rows 8 (i WAVES + wave) .. + 7: bit 3 is that of the wave");
-        const int lane = threadIdx.x & 63, row = lane >> 3, col = ((lane & 7) ^ row) * 16;
-        const int col_p = PAIRED ? ((lane & 7) ^ ((row & 3) | (wave & 1) << 2)) * 16 : col;
-#pragma unroll
-        for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col_p;
-#pragma unroll
-        for (int i = 0; i < LQ; ++i) off_q[i] = (uint32_t)min(a.C - 1 - c0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_q + col;
-        const int32_t at = a.p_steps ? first % a.p_steps : 0;
-        p = a.p + (int64_t)r0 * a.ld_p + (int64_t)at * 128;
-        q = a.q + (int64_t)c0 * a.ld_q + (int64_t)first * 128;
-        p_left = a.p_steps - at;
-    }
-    // the next step, to `to`: [TR + TC][128]
-    __device__ __forceinline__ void request(const ProductArgs &a, char *to, int wave)
-    {
-#pragma unroll
-        for (int i = 0; i < LP; ++i)
-            __builtin_amdgcn_global_load_lds((global_void *)(p + off_p[i]), (lds_void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < LQ; ++i)
-            __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[i]), (lds_void *)(to + TR * 128 + (i * WAVES + wave) * 1024), 16, 0, 0);
-        next(a);
-    }
-    // one of its LP + LQ loads; next() when all have been asked for
-    __device__ __forceinline__ void request_one(const ProductArgs &a, char *to, int wave, int i)
-    {
-        if (i < LP) __builtin_amdgcn_global_load_lds((global_void *)(p + off_p[i % LP]), (lds_void *)(to + (i * WAVES + wave) * 1024), 16, 0, 0);
-        else __builtin_amdgcn_global_load_lds((global_void *)(q + off_q[(i - LP) % LQ]), (lds_void *)(to + TR * 128 + ((i - LP) * WAVES + wave) * 1024), 16, 0, 0);
-    }
-    __device__ __forceinline__ void next(const ProductArgs &a)
-    {
-        q += 128;
-        p += 128;
-        if (--p_left == 0) {
-            p_left = a.p_steps;
-            p -= (int64_t)a.p_steps * 128;
-        }
-    }
-};
+template <>
+struct Biased<OpBf16Biased> { static constexpr bool value = true; };
 
 // A tile of 32 FR x 32 FC outputs by four waves, STAGES buffers in turn, two workgroups per compute unit where they fit (kTiles).  A step has two halves; under the
 // matrix instructions of each the operands of the next are read:
@@ -295,29 +120,6 @@ __global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_
     else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
 }
 
-__device__ __forceinline__ i32x4 i32x4_of(const float *v) { return __builtin_bit_cast(i32x4, (f32x4{v[0], v[1], v[2], v[3]})); }
-
-// Lanes 16 g + n hold, of column `column` (n on from a multiple of 16), sixteen bytes `lo` at row `row` and sixteen `hi` STEP rows behind, the four g making
-// up 64 bytes, or every other sixteen of 128.  Columns n and n + 8 exchange a half, so that each store brings eight lanes' 128 bytes of a column: whole
-// lines, which stores past the caches need.  Through the caches the outputs (25 MB at least, where tiles of this size are taken) would drive out what
-// they hold of the operands: 8192 x 4096 x 16384 int8 to bf16, all values alike: 435 us through the caches, 400 past them in parts, 374 in lines;
-// with random values 494 and 465.
-template <int STEP, typename T>
-__device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, int64_t ld, i32x4 lo, i32x4 hi)
-{
-    const bool first = (threadIdx.x & 8) == 0;
-    i32x4 a, b;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int32_t mine = first ? hi[e] : lo[e], other = __builtin_amdgcn_update_dpp(0, mine, 0x128, 0xf, 0xf, true);     // row_ror:8
-        a[e] = first ? lo[e] : other;
-        b[e] = first ? other : hi[e];
-    }
-    i32x4 *const to = (i32x4 *)(out + (int64_t)(first ? column : column - 8) * ld + row + (first ? 0 : STEP)), *const next = (i32x4 *)((T *)to + 8 * ld);
-    __builtin_nontemporal_store(a, to);
-    __builtin_nontemporal_store(b, next);
-}
-
 // Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each.  A step of 128 bytes has two halves of 64 matrix instructions; under
 // each half the operands of the next are read:
 //   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1:
@@ -343,7 +145,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
     }
     const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
     const char *const tp = lds + (wr * FR * 16 + (frow >> 2) * 8 + (frow & 3)) * 128, *const tq = lds + TR * 128 + (wc * FC * 16 + frow) * 128;
-    constexpr bool kScaled = Scaled<OP>::value;
+    constexpr bool kScaled = Scaled<OP>::value, kBiased = kScaled || Biased<OP>::value;
     TileLoads<TR, TC, 4, true> loads;
     typename OP::acc acc[FR][FC];
     i32x4 fp[2][FR], fq[2][FC];
@@ -387,11 +189,9 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
         const ProductArgs &a = all.a[which];
         const int32_t steps = a.steps, row0 = r0, col0 = c0, t = threadIdx.x;
         float row_scale = 0.0f, row_bias = 0.0f, col_scale = 0.0f;
-        if (kScaled) {
-            if (row0 + t < a.R) row_scale = a.p_scale[row0 + t];
-            if (a.bias && row0 + t < a.R) row_bias = param(a.bias, a.bias_dtype, row0 + t);
-            if (col0 + t < a.C) col_scale = a.q_scale[col0 + t];
-        }
+        if (kScaled && row0 + t < a.R) row_scale = a.p_scale[row0 + t];
+        if (kBiased && a.bias && row0 + t < a.R) row_bias = param(a.bias, a.bias_dtype, row0 + t);
+        if (kScaled && col0 + t < a.C) col_scale = a.q_scale[col0 + t];
 #pragma unroll
         for (int i = 0; i < FR; ++i)
 #pragma unroll
@@ -419,7 +219,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
             meet();
             run(a, 1, step, step + 1 < steps, false);
         }
-        if (kScaled) {
+        if (kBiased) {
             scales[t] = row_scale;
             scales[256 + t] = row_bias;
             scales[512 + t] = col_scale;
@@ -442,7 +242,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 #pragma unroll
         for (int i = 0; i < FR / 2; ++i) {
             float s[8], b[8];
-            if (kScaled)
+            if (kBiased)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const f32x4 u = *(const f32x4 *)(scales + r + i * 32 + h * 4), v = *(const f32x4 *)(scales + 256 + r + i * 32 + h * 4);
@@ -457,6 +257,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
                 for (int e = 0; e < 8; ++e) {
                     v[e] = OP::value(acc[2 * i + (e >> 2)][j][e & 3]);
                     if (kScaled) v[e] = v[e] * (qs * s[e]) + b[e];
+                    else if (kBiased) v[e] += b[e];
                 }
                 const int32_t row = row0 + r + i * 32, column = col0 + c + j * 16;
                 if (!whole) {
@@ -474,76 +275,8 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
         }
         if (!more) return;
         after = whole ? 32 : 0;
-        if (kScaled) barrier();                                         // (the scales are read before the next tile's are written)
+        if (kBiased) barrier();                                         // (the scales are read before the next tile's are written)
     }
-}
-
-// Adds up the splits in their order, four outputs per thread (one where rows of the sums do not start on 16-byte boundaries), the loads of
-// four splits under way.  32 x 25088 from two splits: 5 us.
-struct Joins {
-    ProductArgs a[2];
-    uint32_t first1;                    // workgroups from here on: product 1
-};
-
-template <class OP, int OUT, int VEC>
-__device__ __forceinline__ void join_part(const ProductArgs &a, int64_t at)
-{
-    typedef typename OP::sum N;
-    typedef N NV __attribute__((ext_vector_type(VEC)));
-    const int32_t pieces = a.R / VEC;
-    if (at >= (int64_t)pieces * a.C) return;
-    const int32_t c = (int32_t)(at / pieces), r = (int32_t)(at % pieces) * VEC;
-    const NV *part = (const NV *)((const N *)a.parts + (int64_t)c * a.R + r);
-    const int64_t step = (int64_t)a.C * a.R / VEC;
-    NV sum = {};
-    int32_t k = 0;
-    for (; k + 4 <= a.splits; k += 4) {
-        NV v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = part[(k + i) * step];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += v[i];
-    }
-    for (; k < a.splits; ++k) sum += part[k * step];
-    typename Elem<OUT>::type *out = (typename Elem<OUT>::type *)a.out + (int64_t)c * a.ld_out + r;
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        float v = OP::value(sum[i]);
-        if (Scaled<OP>::value) {
-            v *= a.q_scale[c] * a.p_scale[r + i];
-            if (a.bias) v += param(a.bias, a.bias_dtype, r + i);
-        }
-        out[i] = Elem<OUT>::from_float(v);
-    }
-}
-
-template <class OP, int OUT>
-__global__ __launch_bounds__(256) void product_join_kernel(Joins all)
-{
-    const int which = blockIdx.x >= all.first1;
-    const ProductArgs &a = all.a[which];
-    const int64_t at = (int64_t)(blockIdx.x - (which ? all.first1 : 0)) * 256 + threadIdx.x;
-    if (a.R % 4 == 0) join_part<OP, OUT, 4>(a, at);
-    else join_part<OP, OUT, 1>(a, at);
-}
-
-template <class OP, int OUT>
-static hipError_t join_as(const ProductArgs *a, int n, hipStream_t s)
-{
-    Joins all{};
-    uint32_t blocks = 0;
-    int m = 0;
-    for (int i = 0; i < n; ++i) {
-        if (a[i].splits <= 1) continue;
-        all.a[m] = a[i];
-        if (m == 1) all.first1 = blocks;
-        blocks += (uint32_t)(((int64_t)(a[i].R % 4 ? a[i].R : a[i].R / 4) * a[i].C + 255) / 256);
-        ++m;
-    }
-    if (m == 0) return hipSuccess;
-    if (m == 1) all.first1 = UINT32_MAX;
-    hipLaunchKernelGGL((product_join_kernel<OP, OUT>), dim3(blocks), dim3(256), 0, s, all);
-    return hipGetLastError();
 }
 
 // The tiles by rows x columns of 32, and what a workgroup takes, in us: `fixed`, and per step with one workgroup per compute unit and (both of them
@@ -643,7 +376,8 @@ static hipError_t launch_as(const ProductArgs *a, int n, int32_t tile, const Col
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, s, all);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    return join_as<OP, OUT>(a, n, s);
+    const ProductArgs *const joined[2] = {a, a + 1};
+    return join_as<OP, OUT>(joined, n, s);
 }
 
 template <class OP>
@@ -657,8 +391,9 @@ static hipError_t launch(const ProductArgs *a, int n, int32_t tile, const Column
 template <class OP>
 static hipError_t join(const ProductArgs &a, hipStream_t s)
 {
-    if (a.dtype == TICTAC_F32) return join_as<OP, TICTAC_F32>(&a, 1, s);
-    return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(&a, 1, s) : join_as<OP, TICTAC_BF16>(&a, 1, s);
+    const ProductArgs *const joined = &a;
+    if (a.dtype == TICTAC_F32) return join_as<OP, TICTAC_F32>(&joined, 1, s);
+    return a.dtype == TICTAC_F16 ? join_as<OP, TICTAC_F16>(&joined, 1, s) : join_as<OP, TICTAC_BF16>(&joined, 1, s);
 }
 
 hipError_t launch_product_join_i8(const ProductArgs &a, hipStream_t s) { return join<OpI8Widest>(a, s); }
@@ -668,5 +403,7 @@ hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s)
     return a.steps < kWidest / 128 ? launch<OpI8>(&a, 1, tile, ColumnSums{}, s) : launch<OpI8Widest>(&a, 1, tile, ColumnSums{}, s);
 }
 hipError_t launch_products_bf16(const ProductArgs *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s) { return launch<OpBf16>(a, n, tile, c, s); }
+hipError_t launch_product_bf16_biased(const ProductArgs &a, int32_t tile, hipStream_t s) { return launch_as<OpBf16Biased, TICTAC_F32>(&a, 1, tile, ColumnSums{}, s); }
+hipError_t launch_product_join_biased(const ProductArgs &a, hipStream_t s) { return join<OpBf16Biased>(a, s); }
 
 }  // namespace tictac

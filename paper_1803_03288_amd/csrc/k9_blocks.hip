@@ -1,0 +1,312 @@
+// Rounding to 8-bit floats in blocks (f8.h), back, and the operands of a backward pass.
+#include "device_utils.h"
+#include "f8.h"
+
+namespace tictac {
+
+// Blocks of 128 columns of one row: eight elements of each of 16 lanes, a row of the data-parallel primitives, so the maximum takes four steps without LDS.  kTurns blocks of a
+// group of lanes are under way at once.
+constexpr int kTurns = 4;
+
+// A block's scale; behind the last of a row, zeros up to the next multiple of four.  `lane` counts the lanes that have the block.
+__device__ __forceinline__ void put_scale(uint8_t *row, int64_t at, int64_t blocks, int lane, uint32_t scale)
+{
+    if (lane == 0 || (lane < 4 && at == blocks - 1 && at + lane < (blocks + 3) / 4 * 4)) row[at + lane] = lane ? (uint8_t)0 : (uint8_t)scale;
+}
+
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int64_t blocks, int64_t total)
+{
+    using E = Elem<DT>;
+    const int lane = threadIdx.x & 15;
+    const int64_t first = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 16, step = (int64_t)gridDim.x * 16;
+    for (int64_t at = first; at < total; at += kTurns * step) {
+        typename E::raw raw[kTurns];
+        int64_t row[kTurns], col[kTurns];
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            const int64_t i = at + k * step;
+            if (i >= total) continue;
+            row[k] = total < (1ll << 31) ? (int64_t)((uint32_t)i / (uint32_t)blocks) : i / blocks;
+            col[k] = (i - row[k] * blocks) * 128 + lane * 8;
+            raw[k] = load8<DT, WIDE>((const typename E::type *)p.x + row[k] * p.ld_x, col[k], p.cols);
+        }
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            if (at + k * step >= total) continue;
+            float v[8];
+            E::floats(raw[k], v);
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+            const uint32_t scale = f8_scale(row16_max(m), p.format);
+            const uint2 q = f8_quantized8(v, scale, p.format, p.cols - col[k]);     // (also the zeros behind the end)
+            if (p.wide) {
+                f8_values8(q, scale, p.format, v);
+                *(i32x4 *)(p.wide + row[k] * p.ld_q + col[k]) = f8_bf16(v);
+                continue;
+            }
+            *(uint2 *)(p.q + row[k] * p.ld_q + col[k]) = q;
+            put_scale(p.scale + row[k] * p.ld_scale, col[k] >> 7, blocks, lane, scale);
+        }
+    }
+}
+
+// The tile that a workgroup of 256 has: thread t has rows 8 (t / 16) .. + 7 and columns 8 (t % 16) .. + 7 of 128 x 128.
+struct Tile128 {
+    int lane, group;
+    int64_t r, c;               // of the thread's first element
+    __device__ __forceinline__ Tile128(int64_t tile_r, int64_t tile_c) : lane(threadIdx.x & 15), group(threadIdx.x >> 4), r(tile_r * 128 + group * 8), c(tile_c * 128 + lane * 8) {}
+};
+
+template <int DT, bool WIDE>
+__device__ __forceinline__ void load_tile(const void *x, int64_t ld, int64_t rows, int64_t cols, const Tile128 &t, typename Elem<DT>::raw (&raw)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        raw[e] = typename Elem<DT>::raw{};
+        if (t.r + e < rows) raw[e] = load8<DT, WIDE>((const typename Elem<DT>::type *)x + (t.r + e) * ld, t.c, cols);
+    }
+}
+
+// Blocks of 128 x 128: a workgroup each, which stays in registers between its maximum and its rounding.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p, int64_t across)
+{
+    using E = Elem<DT>;
+    __shared__ uint32_t part[4];
+    const int64_t tile_r = blockIdx.x / across, tile_c = blockIdx.x % across;
+    const Tile128 t(tile_r, tile_c);
+    typename E::raw raw[8];
+    load_tile<DT, WIDE>(p.x, p.ld_x, p.rows, p.cols, t, raw);
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float v[8];
+        E::floats(raw[e], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+    }
+    m = wave_max_u32(m);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
+    __syncthreads();
+    const uint32_t scale = f8_scale(max(max(part[0], part[1]), max(part[2], part[3])), p.format);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (t.r + e >= p.rows) continue;
+        float v[8];
+        E::floats(raw[e], v);
+        *(uint2 *)(p.q + (t.r + e) * p.ld_q + t.c) = f8_quantized8(v, scale, p.format, p.cols - t.c);
+    }
+    put_scale(p.scale + tile_r * p.ld_scale, tile_c, across, threadIdx.x, scale);
+}
+
+// Back: eight values a thread.
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void dequantize_f8_kernel(F8QuantizeArgs p, int64_t chunks, int64_t total)
+{
+    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    const int shift = p.block == 1 ? 0 : 7;
+    for (int64_t at = first; at < total; at += kTurns * step) {
+        uint2 q[kTurns];
+        uint32_t s[kTurns];
+        int64_t row[kTurns], col[kTurns];
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            const int64_t i = at + k * step;
+            if (i >= total) continue;
+            row[k] = total < (1ll << 31) ? (int64_t)((uint32_t)i / (uint32_t)chunks) : i / chunks;
+            col[k] = (i - row[k] * chunks) * 8;
+            q[k] = *(const uint2 *)(p.q + row[k] * p.ld_q + col[k]);
+            s[k] = p.scale[(row[k] >> shift) * p.ld_scale + (col[k] >> 7)];
+        }
+#pragma unroll
+        for (int k = 0; k < kTurns; ++k) {
+            if (at + k * step >= total) continue;
+            float v[8];
+            f8_values8(q[k], s[k], p.format, v);
+            store8<DT, WIDE>((typename Elem<DT>::type *)p.out + row[k] * p.ld_x, col[k], p.cols, v);
+        }
+    }
+}
+
+static unsigned blocks_of(int64_t n) { return (unsigned)(n < 1 ? 1 : n > 256 * 16 ? 256 * 16 : n); }
+
+template <int DT, bool WIDE>
+static hipError_t quantize(const F8QuantizeArgs &p, hipStream_t s)
+{
+    const int64_t blocks = f8_blocks(p.cols);
+    if (p.block == 1) {
+        const int64_t total = blocks * p.rows;
+        hipLaunchKernelGGL((quantize_f8_kernel<DT, WIDE>), dim3(blocks_of((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, blocks, total);
+    } else {
+        hipLaunchKernelGGL((quantize_f8_tiles_kernel<DT, WIDE>), dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, blocks);
+    }
+    return hipGetLastError();
+}
+
+template <int DT, bool WIDE>
+static hipError_t dequantize(const F8QuantizeArgs &p, hipStream_t s)
+{
+    const int64_t chunks = (p.cols + 7) / 8, total = chunks * p.rows;
+    hipLaunchKernelGGL((dequantize_f8_kernel<DT, WIDE>), dim3(blocks_of((total + 256 * kTurns - 1) / (256 * kTurns))), dim3(256), 0, s, p, chunks, total);
+    return hipGetLastError();
+}
+
+hipError_t launch_quantize_f8(const F8QuantizeArgs &p, hipStream_t s)
+{
+    return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), quantize, p, s);
+}
+hipError_t launch_dequantize_f8(const F8QuantizeArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.out, p.dtype, p.ld_x, p.cols), dequantize, p, s); }
+
+// ---- the operands of a backward pass ----
+// A workgroup has a tile of 128 x 128 of dy, of x or of w as floats in registers; blocks of its rows are maxima over 16 lanes, those of its columns meet in LDS, through which they are
+// turned round too, so that reads and writes are whole lines.  BF16: the values that 8 bits keep, as bf16.
+struct TurnRoom {
+    uint32_t part[16][128];             // maxima, sums
+    uint8_t scale[128];
+};
+
+// v: 8 x 8 of a tile; the blocks of its columns go to `to`, [columns][ld], in the format
+template <bool BF16>
+__device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8][8], int64_t rows, int64_t cols, int64_t tile_r, int64_t tile_c, int format, const F8Operand &to,
+                                            TurnRoom &room, char *turned)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[e][i]));
+        room.part[t.group][t.lane * 8 + i] = m;
+    }
+    __syncthreads();
+    if (threadIdx.x < 128) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int g = 0; g < 16; ++g) m = max(m, room.part[g][threadIdx.x]);
+        const uint32_t scale = f8_scale(m, format);
+        room.scale[threadIdx.x] = (uint8_t)scale;
+        const int64_t c = tile_c * 128 + threadIdx.x;
+        if (!BF16 && c < cols) to.scale[c * to.ld_scale + tile_r] = (uint8_t)scale;
+    }
+    __syncthreads();
+    // Eight rows of a column are one piece; piece g of column c lies at place g ^ c / 8 of its 16: a wave's stores and loads then meet all banks alike.
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float u[8];
+        const uint32_t scale = room.scale[t.lane * 8 + i];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = v[e][i];
+        const uint2 q = f8_quantized8(u, scale, format, rows - t.r);
+        const int at = (t.lane * 8 + i) * 16 + (t.group ^ t.lane);
+        if (BF16) {
+            f8_values8(q, scale, format, u);
+            *(i32x4 *)(turned + at * 16) = f8_bf16(u);
+        } else {
+            *(uint2 *)(turned + at * 8) = q;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < (BF16 ? 8 : 4); ++k) {
+        const int n = k * 256 + threadIdx.x, c = n / (BF16 ? 16 : 8), piece = n % (BF16 ? 16 : 8), lane = c >> 3;
+        if (tile_c * 128 + c >= cols) continue;
+        if (BF16) {
+            *(i32x4 *)((uint16_t *)to.q + (tile_c * 128 + c) * to.ld + tile_r * 128 + piece * 8) = *(const i32x4 *)(turned + (c * 16 + (piece ^ lane)) * 16);
+        } else {
+            const i32x4 two = *(const i32x4 *)(turned + (c * 16 + ((2 * piece ^ lane) & ~1)) * 8);
+            *(i32x4 *)((uint8_t *)to.q + (tile_c * 128 + c) * to.ld + tile_r * 128 + piece * 16) = lane & 1 ? i32x4{two[2], two[3], two[0], two[1]} : two;
+        }
+    }
+}
+
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_tiles, int64_t x_tiles)
+{
+    using E = Elem<DT>;
+    constexpr bool BF16 = DT == TICTAC_F32;
+    __shared__ TurnRoom room;
+    __shared__ __align__(16) char turned[128 * 16 * (BF16 ? 16 : 8)];
+    int64_t unit = blockIdx.x;
+    float v[8][8];
+    if (unit < dy_tiles) {
+        const int64_t across = (p.outs + 127) / 128, tile_r = unit / across, tile_c = unit % across;
+        const Tile128 t(tile_r, tile_c);
+        {
+            typename E::raw raw[8];
+            load_tile<DT, WIDE>(p.dy, p.ld_dy, p.rows, p.outs, t, raw);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) E::floats(raw[e], v[e]);
+        }
+        if (p.dy_rows.q) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t m = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[e][i]));
+                const uint32_t scale = f8_scale(row16_max(m), p.format);
+                if (t.r + e >= p.rows) continue;
+                const uint2 q = f8_quantized8(v[e], scale, p.format, p.outs - t.c);
+                const int64_t at = (t.r + e) * p.dy_rows.ld + t.c;
+                if (BF16) {
+                    float u[8];
+                    f8_values8(q, scale, p.format, u);
+                    *(i32x4 *)((uint16_t *)p.dy_rows.q + at) = f8_bf16(u);
+                } else {
+                    *(uint2 *)((uint8_t *)p.dy_rows.q + at) = q;
+                    if (t.lane == 0) p.dy_rows.scale[(t.r + e) * p.dy_rows.ld_scale + tile_c] = (uint8_t)scale;
+                }
+            }
+        }
+        if (p.sums) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += v[e][i];
+                room.part[t.group][t.lane * 8 + i] = __builtin_bit_cast(uint32_t, sum);
+            }
+            __syncthreads();
+            const int64_t c = tile_c * 128 + threadIdx.x;
+            if (threadIdx.x < 128 && c < p.outs) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int g = 0; g < 16; ++g) sum += __builtin_bit_cast(float, room.part[g][threadIdx.x]);
+                p.sums[tile_r * p.outs + c] = sum;
+            }
+            __syncthreads();
+        }
+        if (p.dy_cols.q) put_columns<BF16>(t, v, p.rows, p.outs, tile_r, tile_c, p.format, p.dy_cols, room, turned);
+        return;
+    }
+    unit -= dy_tiles;
+    const bool is_x = unit < x_tiles;
+    if (!is_x) unit -= x_tiles;
+    const F8Rows &from = is_x ? p.x : p.w;
+    const int64_t rows = is_x ? p.rows : p.outs, across = (p.cols + 127) / 128, tile_r = unit / across, tile_c = unit % across;
+    const Tile128 t(tile_r, tile_c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint2 q{0, 0};
+        uint32_t scale = 127;
+        if (t.r + e < rows) {
+            q = *(const uint2 *)(from.q + (t.r + e) * from.ld + t.c);
+            scale = from.scale[((t.r + e) >> from.shift) * from.ld_scale + tile_c];
+        }
+        f8_values8(q, scale, from.format, v[e]);
+    }
+    put_columns<BF16>(t, v, rows, p.cols, tile_r, tile_c, TICTAC_E4M3, is_x ? p.x_cols : p.w_cols, room, turned);
+}
+
+template <int DT, bool WIDE>
+static hipError_t turn(const F8TurnArgs &p, hipStream_t s)
+{
+    const int64_t dy = p.dy_rows.q || p.dy_cols.q || p.sums ? f8_blocks(p.rows) * f8_blocks(p.outs) : 0, x = p.x_cols.q ? f8_blocks(p.rows) * f8_blocks(p.cols) : 0,
+                  w = p.w_cols.q ? f8_blocks(p.outs) * f8_blocks(p.cols) : 0;
+    if (dy + x + w == 0) return hipSuccess;
+    hipLaunchKernelGGL((turn_f8_kernel<DT, WIDE>), dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, dy, x);
+    return hipGetLastError();
+}
+hipError_t launch_turn_f8(const F8TurnArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.dy, p.dtype, p.ld_dy, p.outs), turn, p, s); }
+
+}  // namespace tictac

@@ -1,0 +1,325 @@
+// A layer with weights in 8-bit floats, y[t][o] = sum_i x[t][i] w[o][i] + bias[o], and its gradients
+//   dx[t][i] = sum_o dy'[t][o] w'[o][i],   dw[o][i] = sum_t dy"[t][o] x"[t][i],   db[o] = sum_t dy[t][o]
+// dy' is dy in blocks of 128 outputs, dy" and x" are dy and x in blocks of 128 rows, w' is w in blocks of 128 outputs: an operand's blocks lie along what is summed over.
+// Outputs of 16 bits come from the matrix instructions for 8-bit floats (k9_product.hip says what those cut off); float32 ones from those for bf16, in which the
+// operands' values are exact, with sums in float32.
+#include "device_utils.h"
+#include "k9_product.h"
+
+namespace tictac {
+
+__device__ __forceinline__ f32x4 mma_bf16(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// ---- few rows: bound by the bytes of the weights ----
+// A workgroup has 16 FB outputs and a part of k, its eight waves blocks of 128 of that in turn: weights go from memory to the matrix instruction without LDS, 32 bytes per lane, the next
+// block under way while one is computed.  TB blocks of 16 rows of x come from the caches.  The sums of the waves meet in LDS, those of several workgroups along k in the
+// workspace.  EXACT: bf16 instructions.
+constexpr int kFewWaves = 8;
+
+// sixteen 8-bit floats times a power of two as operands of two bf16 instructions
+__device__ __forceinline__ void widen(i32x4 q, float s, int format, i32x4 (&to)[2])
+{
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float v[8];
+        f8_values4((uint32_t)q[2 * h], format, v);
+        f8_values4((uint32_t)q[2 * h + 1], format, v + 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= s;
+        to[h] = f8_bf16(v);
+    }
+}
+
+template <bool EXACT, int QF, int TB, int FB>
+__global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8Args p, F8Rows xq, int32_t splits, float *parts)
+{
+    __shared__ f32x4 sums[kFewWaves][TB][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 16;
+    const int64_t blocks = gridDim.x / splits, o0 = blockIdx.x % blocks * (16 * FB);
+    const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.cols + 127) / 128);
+    const int32_t first = (int32_t)((int64_t)all * split / splits), units = (int32_t)((int64_t)all * (split + 1) / splits);
+    const uint8_t *w[FB], *x[TB], *we[FB], *xe[TB];
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+        const int64_t o = min(o0 + f * 16 + row, p.outs - 1);
+        w[f] = p.w.q + o * p.w.ld + fk;
+        we[f] = p.w.scale + (o >> p.w.shift) * p.w.ld_scale;
+    }
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+        const int64_t t = min((int64_t)b * 16 + row, p.rows - 1);
+        x[b] = xq.q + t * xq.ld + fk;
+        xe[b] = xq.scale + (t >> xq.shift) * xq.ld_scale;
+    }
+    struct Weights {
+        i32x4 q[FB][2];
+        int e[FB];
+    } now, next;
+    f32x4 acc[FB][TB] = {};
+    const auto request = [&](int32_t u) {
+#pragma unroll
+        for (int f = 0; f < FB; ++f) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) next.q[f][k] = *(const i32x4 *)(w[f] + (int64_t)u * 128 + k * 64);
+            next.e[f] = we[f][u];
+        }
+    };
+    if (first + wave < units) request(first + wave);
+    for (int32_t u = first + wave; u < units; u += kFewWaves) {
+        i32x4 fx[TB][2];
+        int ex[TB];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) fx[b][k] = *(const i32x4 *)(x[b] + (int64_t)u * 128 + k * 64);
+            ex[b] = xe[b][u];
+        }
+        now = next;
+        if (u + kFewWaves < units) request(u + kFewWaves);
+        if constexpr (EXACT) {
+            i32x4 wide_x[TB][2][2];
+#pragma unroll
+            for (int b = 0; b < TB; ++b)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) widen(fx[b][k], f8_factor(ex[b]), QF, wide_x[b][k]);
+#pragma unroll
+            for (int f = 0; f < FB; ++f)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    i32x4 wide_w[2];
+                    widen(now.q[f][k], f8_factor(now.e[f]), TICTAC_E4M3, wide_w);
+#pragma unroll
+                    for (int b = 0; b < TB; ++b)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) acc[f][b] = mma_bf16(wide_w[h], wide_x[b][k][h], acc[f][b]);
+                }
+        } else {
+            const auto whole = [](const i32x4 (&v)[2]) { return i32x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]}; };
+#pragma unroll
+            for (int f = 0; f < FB; ++f)
+#pragma unroll
+                for (int b = 0; b < TB; ++b)
+                    acc[f][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(now.q[f]), whole(fx[b]), acc[f][b], TICTAC_E4M3, QF, 0, now.e[f], 0, ex[b]);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < FB; ++f) {
+        if (f) __syncthreads();
+#pragma unroll
+        for (int b = 0; b < TB; ++b) sums[wave][b][lane] = acc[f][b];
+        __syncthreads();
+        // lane l of a block holds outputs 4 (l / 16) .. + 3 of row l % 16; a thread finishes one output
+        for (int i = threadIdx.x; i < TB * 256; i += kFewWaves * 64) {
+            const int b = i >> 8, o = i & 15, t = (i >> 4) & 15;
+            float sum = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kFewWaves; ++k) sum += sums[k][b][(o >> 2) * 16 + t][o & 3];
+            const int64_t at = (int64_t)b * 16 + t, out = o0 + f * 16 + o;
+            if (at >= p.rows || out >= p.outs) continue;
+            if (splits > 1) {
+                parts[((int64_t)split * p.rows + at) * p.outs + out] = sum;
+                continue;
+            }
+            if (p.bias) sum += param(p.bias, p.bias_dtype, out);
+            put_param(p.y, p.dtype, at * p.ld_y + out, sum);
+        }
+    }
+}
+
+// Into how many parts along k the work of `blocks` workgroups is cut, at most `most`, where `room` workgroups run at a time: rounds times the length of a
+// part, an eighth of the whole added for what each part costs by itself.
+static int32_t parts_along_k(int64_t blocks, int64_t most, int64_t room)
+{
+    int32_t best = 1;
+    float least = 1e30f;
+    for (int32_t n = 1; n <= 16 && n <= most; ++n) {
+        const float cost = (float)((blocks * n + room - 1) / room) * (1.0f / (float)n + 0.125f);
+        if (cost < least) { least = cost; best = n; }
+    }
+    return best;
+}
+
+constexpr int64_t kFewRows = 64;
+static int32_t few_blocks_of(int64_t rows, int64_t outs) { return rows <= 8 || outs <= 2048 ? 1 : rows <= 16 ? 2 : 4; }
+static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
+{
+    const int64_t each = 16 * few_blocks_of(rows, outs), blocks = (outs + each - 1) / each, units = (cols + 127) / 128;
+    return parts_along_k(blocks, units / kFewWaves, 256);
+}
+
+static size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+// The workspace of a forward call.
+struct ForwardRoom {
+    ProductPlan plan;
+    size_t x, xe, w, parts, bytes;          // offsets: x in 8 bits and its scales, or as bf16; w as bf16; sums of splits
+};
+static ForwardRoom forward_room(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
+{
+    ForwardRoom r{};
+    const int64_t ld = rows8_stride(cols);
+    const bool exact = dtype == TICTAC_F32, few = rows <= kFewRows;
+    if (few) {
+        r.plan = {0, {few_splits(rows, cols, outs), 1}};
+    } else {
+        const ProductShape shape{(int32_t)outs, (int32_t)rows, (int32_t)(exact ? ld / 64 : ld / 128)};
+        r.plan = exact ? plan_products(&shape, 1) : plan_products_f8(&shape, 1);
+    }
+    const bool wide = exact && !few;
+    r.xe = r.x + up(wide ? (size_t)rows * ld * 2 : from_floats ? (size_t)rows * ld : 0);
+    r.w = r.xe + up(from_floats && !wide ? (size_t)rows * f8_scale_stride(cols) : 0);
+    r.parts = r.w + up(wide ? (size_t)outs * ld * 2 : 0);
+    r.bytes = r.parts + up(product_parts_bytes(r.plan.splits[0], (int32_t)outs, (int32_t)rows));
+    return r;
+}
+size_t linear_f8_workspace(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs) { return forward_room(dtype, from_floats, rows, cols, outs).bytes; }
+
+// the values of 8-bit floats as bf16, [rows][padded]
+static hipError_t launch_widen(const F8Rows &r, int64_t rows, int64_t padded, uint16_t *to, hipStream_t s)
+{
+    F8QuantizeArgs a{};
+    a.dtype = TICTAC_BF16; a.format = r.format; a.block = 1 << r.shift; a.rows = rows; a.cols = padded; a.out = to; a.ld_x = padded;
+    a.q = const_cast<uint8_t *>(r.q); a.ld_q = r.ld; a.scale = const_cast<uint8_t *>(r.scale); a.ld_scale = r.ld_scale;
+    return launch_dequantize_f8(a, s);
+}
+
+template <bool EXACT, int QF>
+static auto few_kernel(int64_t rows, int32_t fb)
+{
+    return rows <= 16   ? (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 1, 1> : linear_f8_few_kernel<EXACT, QF, 1, 2>)
+           : rows <= 32 ? (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 2, 1> : linear_f8_few_kernel<EXACT, QF, 2, 4>)
+                        : (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 4, 1> : linear_f8_few_kernel<EXACT, QF, 4, 4>);
+}
+
+hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
+{
+    const ForwardRoom room = forward_room(p.dtype, p.x != nullptr, p.rows, p.cols, p.outs);
+    const int64_t ld = rows8_stride(p.cols);
+    const bool exact = p.dtype == TICTAC_F32, few = p.rows <= kFewRows, wide = exact && !few;
+    char *at = (char *)p.workspace;
+    F8Rows x = p.x8;
+    if (p.x) {
+        F8QuantizeArgs q{};
+        q.dtype = p.dtype; q.format = TICTAC_E4M3; q.block = 1; q.rows = p.rows; q.cols = p.cols; q.x = p.x; q.ld_x = p.ld_x; q.ld_q = ld;
+        if (wide) {
+            q.wide = (uint16_t *)(at + room.x);
+        } else {
+            q.q = (uint8_t *)at + room.x;
+            q.scale = (uint8_t *)at + room.xe;
+            q.ld_scale = f8_scale_stride(p.cols);
+        }
+        if (const hipError_t e = launch_quantize_f8(q, s); e != hipSuccess) return e;
+        x = F8Rows{q.q, ld, q.scale, q.ld_scale, TICTAC_E4M3, 0};
+    } else if (wide) {
+        if (const hipError_t e = launch_widen(p.x8, p.rows, ld, (uint16_t *)(at + room.x), s); e != hipSuccess) return e;
+    }
+    const int32_t splits = room.plan.splits[0];
+    ProductF8Args a{};
+    a.R = (int32_t)p.outs; a.C = (int32_t)p.rows; a.splits = splits;
+    a.out = p.y; a.ld_out = p.ld_y; a.dtype = p.dtype; a.bias = p.bias; a.bias_dtype = p.bias_dtype; a.parts = at + room.parts;
+    if (few) {
+        const int32_t fb = few_blocks_of(p.rows, p.outs), outs = 16 * fb;
+        const auto kernel = exact ? (x.format == TICTAC_E5M2 ? few_kernel<true, TICTAC_E5M2>(p.rows, fb) : few_kernel<true, TICTAC_E4M3>(p.rows, fb))
+                                  : (x.format == TICTAC_E5M2 ? few_kernel<false, TICTAC_E5M2>(p.rows, fb) : few_kernel<false, TICTAC_E4M3>(p.rows, fb));
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.outs + outs - 1) / outs * splits)), dim3(kFewWaves * 64), 0, s, p, x, splits, (float *)a.parts);
+        return splits > 1 ? launch_product_join_biased(a, s) : hipGetLastError();
+    }
+    if (wide) {
+        if (const hipError_t e = launch_widen(p.w, p.outs, ld, (uint16_t *)(at + room.w), s); e != hipSuccess) return e;
+        a.p = at + room.w; a.ld_p = ld * 2;
+        a.q = at + room.x; a.ld_q = ld * 2;
+        a.steps = a.p_steps = (int32_t)(ld / 64);
+        return launch_product_bf16_biased(a, room.plan.tile, s);
+    }
+    a.p = (const char *)p.w.q; a.ld_p = p.w.ld; a.p_e = p.w.scale; a.ld_pe = p.w.ld_scale; a.p_shift = p.w.shift;
+    a.q = (const char *)x.q; a.ld_q = x.ld; a.q_e = x.scale; a.ld_qe = x.ld_scale; a.q_shift = x.shift; a.q_format = x.format;
+    a.steps = a.p_steps = (int32_t)(ld / 128);
+    return launch_products_f8(&a, 1, room.plan.tile, ColumnSums{}, s);
+}
+
+// ---- backward ----
+struct BackwardRoom {
+    int64_t padded_o, padded_t;
+    ProductPlan plan;                       // dx, dw
+    size_t sums, w, we, x, xe, dy_rows, dy_rows_e, dy_cols, dy_cols_e, parts_x, parts_w, bytes;
+};
+static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int64_t outs)
+{
+    const bool exact = dtype == TICTAC_F32;
+    const size_t size = exact ? 2 : 1;
+    BackwardRoom r{};
+    r.padded_o = rows8_stride(outs);
+    r.padded_t = rows8_stride(rows);
+    const int64_t step = exact ? 64 : 128;
+    const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / step)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / step)}};
+    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes, 2);
+    const size_t e = exact ? 0 : 1;         // (values as bf16 have no scales)
+    r.w = r.sums + up((size_t)f8_blocks(rows) * outs * 4);
+    r.we = r.w + up((size_t)cols * r.padded_o * size);
+    r.x = r.we + up(e * cols * f8_scale_stride(outs));
+    r.xe = r.x + up((size_t)cols * r.padded_t * size);
+    r.dy_rows = r.xe + up(e * cols * f8_scale_stride(rows));
+    r.dy_rows_e = r.dy_rows + up((size_t)rows * r.padded_o * size);
+    r.dy_cols = r.dy_rows_e + up(e * rows * f8_scale_stride(outs));
+    r.dy_cols_e = r.dy_cols + up((size_t)outs * r.padded_t * size);
+    r.parts_x = r.dy_cols_e + up(e * outs * f8_scale_stride(rows));
+    r.parts_w = r.parts_x + up(product_parts_bytes(r.plan.splits[0], (int32_t)cols, (int32_t)rows));
+    r.bytes = r.parts_w + up(product_parts_bytes(r.plan.splits[1], (int32_t)cols, (int32_t)outs));
+    return r;
+}
+size_t linear_f8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs) { return backward_room(dtype, rows, cols, outs).bytes; }
+
+// No rows, or no outputs: what there is of the gradients is zero.
+static hipError_t backward_nothing(const LinearF8Args &p, hipStream_t s)
+{
+    ProductArgs a{};
+    a.splits = 1;
+    a.R = (int32_t)p.cols;
+    a.dtype = p.dtype;
+    a.C = (int32_t)(p.rows ? p.rows : p.outs);
+    a.out = p.rows ? p.dx : p.dw;
+    a.ld_out = p.rows ? p.ld_dx : p.ld_dw;
+    const ColumnSums c{nullptr, 0, p.outs, p.outs ? p.db : nullptr, p.dtype};
+    return launch_products_bf16(&a, a.out && a.C ? 1 : 0, 0, c, s);
+}
+
+hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
+{
+    if (p.rows == 0 || p.outs == 0) return backward_nothing(p, s);
+    const BackwardRoom room = backward_room(p.dtype, p.rows, p.cols, p.outs);
+    const bool exact = p.dtype == TICTAC_F32;
+    const int64_t size = exact ? 2 : 1, step = exact ? 64 : 128;
+    char *at = (char *)p.workspace;
+    F8TurnArgs t{};
+    t.dtype = p.dtype; t.format = p.format; t.rows = p.rows; t.cols = p.cols; t.outs = p.outs; t.dy = p.dy; t.ld_dy = p.ld_dy; t.x = p.x8; t.w = p.w;
+    if (p.dx) {
+        t.w_cols = {at + room.w, room.padded_o, (uint8_t *)at + room.we, f8_scale_stride(p.outs)};
+        t.dy_rows = {at + room.dy_rows, room.padded_o, (uint8_t *)at + room.dy_rows_e, f8_scale_stride(p.outs)};
+    }
+    if (p.dw) {
+        t.x_cols = {at + room.x, room.padded_t, (uint8_t *)at + room.xe, f8_scale_stride(p.rows)};
+        t.dy_cols = {at + room.dy_cols, room.padded_t, (uint8_t *)at + room.dy_cols_e, f8_scale_stride(p.rows)};
+    }
+    if (p.db) t.sums = (float *)(at + room.sums);
+    if (const hipError_t e = launch_turn_f8(t, s); e != hipSuccess) return e;
+    ProductF8Args a[2] = {};
+    int n = 0;
+    const auto add = [&](const F8Operand &rows_p, const F8Operand &rows_q, int64_t padded, int64_t outputs, void *out, int64_t ld, int32_t splits, size_t parts) {
+        ProductF8Args &x = a[n++];
+        x.p = (const char *)rows_p.q; x.ld_p = rows_p.ld * size; x.p_e = rows_p.scale; x.ld_pe = rows_p.ld_scale;
+        x.q = (const char *)rows_q.q; x.ld_q = rows_q.ld * size; x.q_e = rows_q.scale; x.ld_qe = rows_q.ld_scale; x.q_format = p.format;
+        x.R = (int32_t)p.cols; x.C = (int32_t)outputs; x.steps = x.p_steps = (int32_t)(padded / step);
+        x.splits = splits; x.out = out; x.ld_out = ld; x.parts = at + parts; x.dtype = p.dtype;
+    };
+    if (p.dx) add(t.w_cols, t.dy_rows, room.padded_o, p.rows, p.dx, p.ld_dx, room.plan.splits[0], room.parts_x);
+    if (p.dw) add(t.x_cols, t.dy_cols, room.padded_t, p.outs, p.dw, p.ld_dw, room.plan.splits[1], room.parts_w);
+    const ColumnSums c{t.sums, f8_blocks(p.rows), p.outs, p.db, p.dtype};
+    if (!exact) return launch_products_f8(a, n, room.plan.tile, c, s);
+    const ProductArgs wide[2] = {a[0], a[1]};
+    return launch_products_bf16(wide, n, room.plan.tile, c, s);
+}
+
+}  // namespace tictac

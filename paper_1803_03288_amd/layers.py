@@ -8,6 +8,16 @@ transferred in 8 bits, a quarter of the bytes of float32, and whose activations 
     dn, dw, db = layers.linear_q8_backward(dy, y8, w8)                        # backward, from y8 and x8 alone
     dx, dgamma, dbeta = layers.layer_norm_backward(dn, x8, gamma, mean, rstd)
 
+The same in 8-bit floats, with powers of two as scales of blocks of 128, the backward products in 8 bits too, and the update that ends the step:
+
+    w8 = layers.quantize_f8(w, 128)                                           # as it is sent
+    x8 = layers.quantize_f8(x)
+    y = layers.linear_f8(x8, w8, bias, dtype=x.dtype)
+    dx, dw, db = layers.linear_f8_backward(dy, x8, w8)
+    moments = layers.adamw_moments([w, bias], bits=8)                         # once
+    norm = layers.gradient_norm([dw, db])
+    layers.adamw_step([w, bias], [dw, db], moments, step, lr=1e-3, norm=norm, max_norm=1.0)
+
 ``python -m paper_1803_03288_amd.measured`` runs a stack of such layers, measures their ops and orders their transfers.
 
 Tensors are CUDA tensors of float32, float16 or bfloat16; the last dimension is the row, and outputs have the shape of
@@ -20,7 +30,7 @@ refuses ``TicTacError``.
 from __future__ import annotations
 
 import ctypes
-from typing import NamedTuple, Optional, Union
+from typing import List, NamedTuple, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -28,7 +38,8 @@ from .binding import _check, lib
 
 GROUP = 128                     # columns per scale of kept activations
 _CALLS = ("quantize_rows", "dequantize_rows", "layer_norm", "layer_norm_backward_workspace", "layer_norm_backward", "linear_q8_workspace", "linear_q8",
-          "linear_q8_backward_workspace", "linear_q8_backward")
+          "linear_q8_backward_workspace", "linear_q8_backward", "quantize_f8", "dequantize_f8", "linear_f8_workspace", "linear_f8", "linear_f8_backward_workspace",
+          "linear_f8_backward", "gradient_norm_workspace", "gradient_norm", "adamw_step")
 _module = None
 
 
@@ -104,3 +115,90 @@ def linear_q8_backward(dy: torch.Tensor, x: Rows8, w: Rows8):
     two for float16, but for bfloat16 one factor of each term is rounded to 8 bits (up to 2^-8 of it, beside the rounding of the outputs); ``dy`` in
     float32 avoids that."""
     return (_module or _native()).linear_q8_backward(dy, x, w)
+
+
+# ---- 8-bit floats, a scale per block of 128 -----------------------------------------------------------------
+
+class Float8(NamedTuple):
+    """8-bit floats in blocks: the values ``q * scale`` of ``[rows][cols]``.  ``q`` is float8_e4m3fn or float8_e5m2 ``[rows][ld]``, ``ld`` a multiple of 128, zeros behind
+    column ``cols``; a block is 128 columns of ``block`` rows, 1 or 128; ``scale`` is float8_e8m0fnu (powers of two) ``[ceil(rows / block)][ceil(cols / 128)]``,
+    rounded up to a multiple of four in the last dimension (scales that are not, or whose rows do not start on 4-byte boundaries, are copied in each call)."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    cols: int
+    block: int = 1
+
+    @property
+    def shape(self):
+        return (self.q.shape[0], self.cols)
+
+
+def quantize_f8(x: torch.Tensor, block: int = 1, dtype: torch.dtype = torch.float8_e4m3fn) -> Float8:
+    """``x`` in 8-bit floats.  ``block`` 1: a scale per row and 128 columns (operands of products); 128: one per 128 x 128 (weights).  A scale is the least power of two, from
+    2^-126 on, with which its block fits the type (largest value 448, or 57344 for float8_e5m2).  A block with a NaN or an infinity reads as NaN throughout."""
+    q, scale = (_module or _native()).quantize_f8(x, block, dtype)
+    return Float8(q, scale, x.shape[-1], block)
+
+
+def dequantize_f8(r: Float8, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """The values of 8-bit floats, ``[rows][cols]``, rounded to ``dtype``."""
+    return (_module or _native()).dequantize_f8(r, dtype)
+
+
+def linear_f8(x: Union[torch.Tensor, Float8], w: Float8, bias: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """``x @ w.T + bias`` with both operands in 8-bit floats, ``w`` ``[outs][cols]`` in float8_e4m3fn.  ``x`` is rounded to float8_e4m3fn in blocks of one row in the call, unless it is
+    given as ``Float8``; then ``dtype`` is the output's type (float32 unless given).  float32 outputs are of exact products with sums in float32; those of 16 bits come from the matrix
+    instructions for 8-bit floats, which cut off what products have below about 2^-13 of the largest that they are added with (1.4e-5 of the result for normal values)."""
+    return (_module or _native()).linear_f8(x, w, bias, dtype)
+
+
+def linear_f8_backward(dy: torch.Tensor, x: Float8, w: Float8, grad_dtype: torch.dtype = torch.float8_e4m3fn):
+    """``(dx, dw, db)`` of ``linear_f8`` from the 8-bit operands that the forward pass took, all of the type of ``dy``; the rounding of the input counts as the
+    identity.  ``dy`` is rounded to ``grad_dtype`` (float8_e4m3fn, or float8_e5m2 for a wider range) in blocks of 128 along what is summed over: its outputs for dx, its
+    rows for dw; ``x``, and ``w`` where its blocks are of one row, are rounded again to float8_e4m3fn in such blocks, which changes only values of 2^-15 of a block's
+    largest and less.  ``db`` is of ``dy`` itself.  Sums as in ``linear_f8``.  A NaN or an infinity in ``dy`` makes its row of dx and the rows of dw that its block reaches NaN."""
+    return (_module or _native()).linear_f8_backward(dy, x, w, grad_dtype)
+
+
+# ---- the update ---------------------------------------------------------------------------------------------
+
+class Moments(NamedTuple):
+    """Moments of one parameter, in the order in which its elements lie in memory: float32 ``m`` and ``v`` of its number of elements; or in 8 bits ``m`` and the root of
+    ``v``, each a ``Float8`` of one row, blocks of one row, float8_e4m3fn."""
+    m: Union[torch.Tensor, Float8]
+    v: Union[torch.Tensor, Float8]
+
+
+def adamw_moments(params: Sequence[torch.Tensor], bits: int = 8) -> List[Moments]:
+    """Moments of zeros for ``adamw_step``, in 8 or 32 bits."""
+    if bits not in (8, 32):
+        raise ValueError(f"bits: {bits}, expected 8 or 32")
+
+    def zeros(p: torch.Tensor):
+        n = p.numel()
+        if bits == 32 or n == 0:
+            return torch.zeros(n, dtype=torch.float32, device=p.device)
+        q = torch.zeros(1, -(-n // 128) * 128, dtype=torch.uint8, device=p.device)
+        scale = torch.ones(1, -(-n // 512) * 4, dtype=torch.uint8, device=p.device)
+        return Float8(q.view(torch.float8_e4m3fn), scale.view(torch.float8_e8m0fnu), n)
+
+    return [Moments(zeros(p), zeros(p)) for p in params]
+
+
+def gradient_norm(grads: Sequence[torch.Tensor], scale: float = 1.0) -> torch.Tensor:
+    """``scale`` times the 2-norm of all elements of the tensors, a float32 value on the device, with squares and sums in float64.  The same bits at every run."""
+    return (_module or _native()).gradient_norm(grads, scale)
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], moments: Sequence[Moments], step: Union[int, torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3,
+               betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2, grad_scale: float = 1.0, norm: Optional[torch.Tensor] = None,
+               max_norm: Optional[float] = None, copies: Optional[Sequence[Optional[torch.Tensor]]] = None, seed: int = 0) -> None:
+    """One step of AdamW over all ``params``, in place, in few launches.
+
+    ``grads`` are multiplied by ``grad_scale``, and where ``max_norm`` is given by ``min(1, max_norm / norm)`` too.  ``norm`` is what ``gradient_norm`` gives for the same
+    ``grad_scale``; where it is not finite, nothing is changed.  Parameters and gradients may each be float32, float16 or bfloat16; arithmetic is float32.  ``copies`` receive
+    the new parameters in their own types, for parameters in float32 with layers that take 16 bits.  ``step`` counts from 1; it and ``lr`` may be tensors of one element
+    on the device (int64, float32), which are read when the step runs, so that a captured one goes on.  Moments in 8 bits are rounded at random by a hash of ``seed``,
+    ``step``, the index in ``params`` and the element's: the same call has the same result.  Tensors may not overlap.  Parameters may have any strides without gaps; gradients
+    in another order are copied first."""
+    (_module or _native()).adamw_step(params, grads, moments, step, lr, betas, eps, weight_decay, grad_scale, norm, max_norm, copies, seed)

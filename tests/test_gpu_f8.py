@@ -1,0 +1,353 @@
+"""Products in 8-bit floats with a scale per block (``paper_1803_03288_amd.layers``) against their definitions in 64 bits (``f8_reference``).
+
+Tolerances follow from the arithmetic, before any run: rounding to blocks is compared bit by bit; sums as ``f8_reference.product`` says, and half a step of the output's type."""
+
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import f8_reference as ref
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+TYPES = [F32, F16, BF16]
+E4, E5 = torch.float8_e4m3fn, torch.float8_e5m2
+HALF = {F32: (2.0 ** -24, 2.0 ** -149), F16: (2.0 ** -11, 2.0 ** -25), BF16: (2.0 ** -8, 2.0 ** -134)}
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_1803_03288_amd import layers
+    return layers
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def values(g, rows, cols, dtype, size=1.0):
+    return (torch.randn(rows, cols, generator=g) * torch.exp(0.5 * torch.randn(rows, 1, generator=g)) * size).to(dtype)
+
+
+def close(got, want, bound, dtype):
+    got = got.cpu().double()
+    rel, least = HALF[dtype]
+    assert got.shape == want.shape and torch.isfinite(got).all()
+    off = (got - want).abs() - (bound + rel * (want.abs() + bound) + least)
+    assert float(off.max()) <= 0, (float(off.max()), int((off > 0).sum()))
+
+
+def check_blocks(r, x, block, dtype):
+    q, _, byte = ref.blocks(x, block, dtype)
+    cols = x.shape[1]
+    along = -(-cols // 128)
+    assert r.cols == cols and r.block == block and r.q.dtype == dtype and r.q.shape == (x.shape[0], along * 128)
+    assert r.scale.dtype == torch.float8_e8m0fnu and r.scale.shape == (-(-x.shape[0] // block), -(-along // 4) * 4)
+    scale = r.scale.cpu().view(torch.uint8)
+    assert torch.equal(scale[:, :along], byte) and not scale[:, along:].any()
+    got = r.q.cpu()
+    assert torch.equal(got[:, :cols].double().nan_to_num(1e6), q.nan_to_num(1e6))
+    assert not got.view(torch.uint8)[:, cols:].any()
+
+
+# ---- rounding -----------------------------------------------------------------------------------------------
+
+SIZES = [(1, 1), (3, 7), (5, 127), (2, 128), (33, 129), (130, 1000), (4, 2049), (300, 256), (257, 640), (3, 20000)]
+
+
+@pytest.mark.parametrize("block,f8", [(1, E4), (1, E5), (128, E4), (128, E5)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", SIZES)
+def test_blocks(L, rows, cols, dtype, block, f8):
+    x = values(gen(rows * 1000 + cols), rows, cols, dtype)
+    x[0, 0] = 0.0
+    r = L.quantize_f8(x.cuda(), block, f8)
+    check_blocks(r, x, block, f8)
+    for out in TYPES:
+        assert torch.equal(L.dequantize_f8(r, out).cpu(), ref.values(r).to(out))
+
+
+@pytest.mark.parametrize("block", [1, 128])
+@pytest.mark.parametrize("f8", [E4, E5])
+def test_blocks_at_the_ends_of_the_range(L, block, f8):
+    largest, least, bits = ref.F8[f8]
+    x = torch.zeros(12 * block, 300)
+    rows = x[::block]                                       # the first row of each block
+    rows[1] = 2.0 ** -126                                   # the least normal number
+    rows[2] = 2.0 ** -149                                   # the least there is
+    rows[3, 5], rows[3, 200] = 3.4028234663852886e38, -3.0e38
+    rows[4, 299] = math.inf
+    rows[5, 0] = math.nan
+    rows[6, 130] = -math.inf
+    rows[7] = torch.linspace(-largest, largest, 300)
+    rows[8, 0], rows[8, 1:120] = largest, torch.arange(119) * 2.0 ** (least - bits - 1)     # halves of the least step: ties to even
+    rows[9, 0], rows[9, 1] = largest, largest * (1 - 2.0 ** -24)
+    rows[10, 0] = largest * (1 + 2.0 ** -23)                # the next scale
+    rows[11, 0], rows[11, 1:200] = 1.0, (1 + torch.arange(199) / 256.0)                     # near all the midpoints of a binade
+    r = L.quantize_f8(x.cuda(), block, f8)
+    check_blocks(r, x, block, f8)
+    back = L.dequantize_f8(r).cpu()[::block]
+    assert torch.isnan(back[4, 256:]).all() and torch.isnan(back[5, :128]).all() and torch.isnan(back[6, 128:256]).all() and torch.isfinite(back[4, :256]).all()
+    assert torch.isfinite(back[[0, 1, 2, 3, 7, 8, 9, 10, 11]]).all()
+
+
+@pytest.mark.parametrize("block", [1, 128])
+def test_strides_of_blocks(L, block):
+    """Rows at odd places and strides, one row for all, columns first, a view with its signs turned lazily; scales of another stride."""
+    g = gen(3)
+    room = torch.randn(200, 403, generator=g).cuda()
+    for x in (room[:, 1:301], room[::2, 3:260], room[5:6].expand(140, 403), room.t(), room[:, ::2], torch.randn(9, 130, 2, generator=g).cuda()[..., 0], room.half()[:, 1:200],
+              torch._neg_view(room)):
+        check_blocks(L.quantize_f8(x, block), x.cpu().contiguous().reshape(-1, x.shape[-1]), block, E4)
+    r = L.quantize_f8(room, block)
+    tight = L.Float8(r.q, r.scale[:, :4].contiguous().view(torch.uint8)[:, :4].view(torch.float8_e8m0fnu), 403, block)
+    odd = torch.zeros(r.scale.shape[0], 7, dtype=torch.uint8, device="cuda")
+    odd[:, 1:5] = r.scale.view(torch.uint8)
+    wide = torch.zeros(200, 1024, dtype=torch.uint8, device="cuda")
+    wide[:, 128:640] = r.q.view(torch.uint8)
+    for other in (tight, L.Float8(r.q, odd.view(torch.float8_e8m0fnu)[:, 1:5], 403, block), L.Float8(wide.view(E4)[:, 128:640], r.scale, 403, block)):
+        assert torch.equal(L.dequantize_f8(other), L.dequantize_f8(r))
+
+
+# ---- products -----------------------------------------------------------------------------------------------
+
+# few rows in each number of blocks, with and without sums cut along k; tiles of every size; nothing a multiple of anything
+PRODUCTS = [(1, 1, 1), (1, 4096, 100), (2, 129, 17), (7, 1000, 33), (16, 130, 2100), (17, 2050, 65), (31, 3000, 2500), (33, 640, 130), (64, 5000, 4100), (65, 128, 64), (70, 1, 5), (100, 1000, 100),
+            (129, 385, 131), (200, 4000, 300), (333, 1001, 777), (520, 129, 1030), (1, 20000, 3), (300, 7000, 40)]
+
+
+def operands(L, g, rows, cols, outs, wblock, dtype=F32, f8=E4):
+    x = values(g, rows, cols, dtype)
+    w = L.quantize_f8(torch.randn(outs, cols, generator=g).cuda() / math.sqrt(cols), wblock)
+    return x, L.quantize_f8(x.cuda(), 1, f8), w
+
+
+def wide(r):
+    q, s = ref.parts(r)
+    return q, s, ref.F8[r.q.dtype][1]
+
+
+@pytest.mark.parametrize("rows,cols,outs", PRODUCTS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear(L, rows, cols, outs, dtype):
+    g = gen(rows * 31 + cols * 7 + outs)
+    wblock = 128 if (rows + cols) % 2 else 1
+    x, x8, w = operands(L, g, rows, cols, outs, wblock, dtype)
+    bias = torch.randn(outs, generator=g)
+    want, bound = ref.product(wide(x8), wide(w), dtype != F32)
+    y = L.linear_f8(x.cuda(), w, bias.cuda())
+    close(y, want + bias.double(), bound + ref.U * (want.abs() + bias.abs()), dtype)
+    assert torch.equal(y, L.linear_f8(x8, w, bias.cuda(), dtype))              # the same bits from the rows rounded before, and at another run
+    close(L.linear_f8(x8, w, bias.to(dtype).cuda(), dtype), want + bias.to(dtype).double(), bound + ref.U * (want.abs() + bias.abs()), dtype)
+    close(L.linear_f8(x.cuda(), w), want, bound, dtype)
+
+
+@pytest.mark.parametrize("rows,cols,outs", [(5, 300, 40), (40, 1000, 90), (90, 1000, 200), (200, 4000, 300)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("xblock,f8", [(1, E5), (128, E4), (128, E5)])
+def test_linear_of_other_blocks(L, rows, cols, outs, dtype, xblock, f8):
+    g = gen(rows)
+    x = values(g, rows, cols, F32)
+    x8 = L.quantize_f8(x.cuda(), xblock, f8)
+    for wblock in (1, 128):
+        w = L.quantize_f8(torch.randn(outs, cols, generator=g).cuda(), wblock)
+        want, bound = ref.product(wide(x8), wide(w), dtype != F32)
+        close(L.linear_f8(x8, w, None, dtype), want, bound, dtype)
+
+
+@pytest.mark.parametrize("rows", [1, 9, 40, 100])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_on_blocks_that_spoil_their_rows_only(L, rows, dtype):
+    g = gen(rows)
+    x, _, w = operands(L, g, rows + 1, 300, 140, 128, dtype)
+    good = L.linear_f8(x.cuda(), w)
+    x[rows, 290] = math.inf
+    bad = L.linear_f8(x.cuda(), w)
+    assert torch.isnan(bad[rows]).all() and torch.equal(bad[:rows], good[:rows])
+    v = torch.randn(140, 300, generator=g)
+    v[3, 5] = math.nan
+    y = L.linear_f8(x[:rows].cuda(), L.quantize_f8(v.cuda(), 1))
+    assert torch.isnan(y[:, 3]).all() and torch.isfinite(y[:, :3]).all() and torch.isfinite(y[:, 4:]).all()
+
+
+GRADIENTS = [(1, 1, 1), (1, 300, 200), (3, 1000, 129), (32, 4100, 260), (33, 130, 500), (64, 257, 2000), (65, 130, 70), (101, 777, 1001), (128, 128, 128), (129, 500, 131), (300, 153, 587),
+             (700, 256, 384), (1100, 300, 200)]
+
+
+@pytest.mark.parametrize("rows,cols,outs", GRADIENTS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_backward(L, rows, cols, outs, dtype):
+    g = gen(rows * 31 + cols * 7 + outs)
+    wblock, f8 = (128 if (rows + cols) % 2 else 1), (E5 if outs % 2 else E4)
+    _, x8, w = operands(L, g, rows, cols, outs, wblock)
+    dy = values(g, rows, outs, dtype, 1e-2)
+    (dx, bx), (dw, bw) = ref.gradients(dy, x8, w, f8, dtype != F32)
+    got = L.linear_f8_backward(dy.cuda(), x8, w, f8)
+    close(got[0], dx, bx, dtype)
+    close(got[1], dw, bw, dtype)
+    size = dy.double().abs().sum(0)
+    close(got[2], dy.double().sum(0), ref.U * (rows + 16) * size, dtype)
+    assert all(torch.equal(a, b) for a, b in zip(got, L.linear_f8_backward(dy.cuda(), x8, w, f8)))
+
+
+def test_linear_backward_of_other_blocks(L):
+    g = gen(5)
+    for rows, cols, outs in ((40, 300, 200), (200, 300, 260)):
+        for xblock, f8 in ((1, E5), (128, E4)):
+            x8 = L.quantize_f8(values(g, rows, cols, F32).cuda(), xblock, f8)
+            w = L.quantize_f8(torch.randn(outs, cols, generator=g).cuda(), 1)
+            dy = values(g, rows, outs, BF16)
+            (dx, bx), (dw, bw) = ref.gradients(dy, x8, w, E4, True)
+            got = L.linear_f8_backward(dy.cuda(), x8, w)
+            close(got[0], dx, bx, BF16)
+            close(got[1], dw, bw, BF16)
+
+
+def test_linear_gradient_against_differences(L):
+    """The products by themselves: dy that 8 bits hold exactly, so that nothing but sums is between the gradients and the loss's slopes."""
+    g = gen(21)
+    rows, cols, outs, h = 5, 30, 7, 1e-3
+    w8 = L.quantize_f8(torch.randn(outs, cols, generator=g).cuda(), 128)
+    x8 = L.quantize_f8(torch.randint(-8, 9, (rows, cols), generator=g).float().cuda())
+    dy = torch.randint(-8, 9, (rows, outs), generator=g).float()
+    dx, dw, db = (t.cpu().double() for t in L.linear_f8_backward(dy.cuda(), x8, w8))
+    at = [ref.values(x8), ref.values(w8), torch.zeros(outs).double()]
+
+    def loss(x, w, b):
+        return float(((x @ w.t() + b) * dy.double()).sum())
+
+    for k, grad in enumerate((dx, dw, db)):
+        v = torch.randn(at[k].shape, generator=g).double()
+        up, down = (loss(*(t + s * h * v if i == k else t for i, t in enumerate(at))) for s in (1, -1))
+        assert abs((up - down) / (2 * h) - float((grad * v).sum())) <= 1e-5 * float((grad * v).abs().sum()) + 1e-9
+
+
+@pytest.mark.parametrize("dtype,size", [(F32, 1e30), (F32, 1e-30), (BF16, 1e30), (BF16, 1e-30), (F16, 1e3), (F16, 1e-6)])
+def test_large_and_small_gradients(L, dtype, size):
+    g = gen(22)
+    rows, cols, outs = 140, 200, 150
+    _, x8, w = operands(L, g, rows, cols, outs, 128)
+    dy = values(g, rows, outs, dtype, size)
+    (dx, bx), (dw, bw) = ref.gradients(dy, x8, w, E4, dtype != F32)
+    got = L.linear_f8_backward(dy.cuda(), x8, w)
+    if dtype != F16 or size < 1:                            # (sums of float16 may overflow where dy is large)
+        close(got[0], dx, bx, dtype)
+        close(got[1], dw, bw, dtype)
+
+
+def test_gradients_of_infinities(L):
+    """What is not finite spoils its row of dx and the rows of dw of its block, nothing else; db keeps an infinity."""
+    g = gen(23)
+    rows, cols, outs = 200, 150, 260
+    _, x8, w = operands(L, g, rows, cols, outs, 128)
+    dy = values(g, rows, outs, BF16)
+    good = L.linear_f8_backward(dy.cuda(), x8, w)
+    dy[130, 7] = math.inf
+    dx, dw, db = L.linear_f8_backward(dy.cuda(), x8, w)
+    rest = [i for i in range(rows) if i != 130]
+    assert torch.isnan(dx[130]).all() and torch.equal(dx[rest], good[0][rest])
+    rest = [i for i in range(outs) if i != 7]
+    assert torch.isnan(dw[7]).all() and torch.equal(dw[rest], good[1][rest])
+    assert float(db[7]) == math.inf and torch.equal(db[rest], good[2][rest])
+
+
+# ---- use ----------------------------------------------------------------------------------------------------
+
+def test_no_rows(L):
+    x = torch.empty(0, 130, device="cuda", dtype=BF16)
+    w = L.quantize_f8(torch.randn(60, 130).cuda(), 128)
+    x8 = L.quantize_f8(x)
+    assert L.dequantize_f8(x8).shape == (0, 130) and L.linear_f8(x, w).shape == (0, 60) and L.linear_f8(x8, w).shape == (0, 60)
+    dx, dw, db = L.linear_f8_backward(torch.empty(0, 60, device="cuda", dtype=BF16), x8, w)
+    assert dx.shape == (0, 130) and dw.shape == (60, 130) and not dw.any() and not db.any()
+    none = L.quantize_f8(torch.empty(0, 130, device="cuda"), 128)
+    assert L.linear_f8(torch.randn(5, 130).cuda(), none).shape == (5, 0)
+    with pytest.raises(ValueError):                         # (rows of no columns are refused, as everywhere)
+        L.linear_f8_backward(torch.empty(5, 0, device="cuda"), L.quantize_f8(torch.randn(5, 130).cuda()), none)
+
+
+def test_more_dimensions(L):
+    g = gen(2)
+    w = L.quantize_f8(torch.randn(40, 96, generator=g).cuda(), 128)
+    for shape in ((96,), (3, 4, 96), (2, 3, 2, 96)):
+        x = torch.randn(*shape, generator=g).cuda().to(BF16)
+        flat = x.reshape(-1, 96)
+        y = L.linear_f8(x, w)
+        assert y.shape == shape[:-1] + (40,) and torch.equal(y.reshape(-1, 40), L.linear_f8(flat, w))
+        assert L.linear_f8_backward(y, L.quantize_f8(x), w)[0].shape == x.shape
+
+
+def test_another_stream_and_a_graph(L):
+    """The same bits on a stream of the caller's and from a captured graph, replayed on new inputs, and from two graphs in turn."""
+    g = gen(9)
+    for rows in (12, 96):
+        cols, outs = 520, 260
+        v = torch.randn(outs, cols, generator=g).cuda()
+        inputs = [(values(g, rows, cols, BF16).cuda(), values(g, rows, outs, BF16).cuda()) for _ in range(3)]
+
+        def step(x, dy):
+            w = L.quantize_f8(v, 128)
+            x8 = L.quantize_f8(x)
+            return (L.linear_f8(x, w), L.linear_f8(x8, w), L.dequantize_f8(x8)) + L.linear_f8_backward(dy, x8, w) + L.linear_f8_backward(dy.float(), x8, w)
+
+        want = [step(*i) for i in inputs]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for i, e in zip(inputs, want):
+                assert all(torch.equal(a, b) for a, b in zip(step(*i), e))
+        torch.cuda.current_stream().wait_stream(side)
+        x, dy = (t.clone() for t in inputs[0])
+        graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+        got = []
+        for graph in graphs:
+            with torch.cuda.graph(graph):
+                got.append(step(x, dy))
+        for turn in range(2):
+            for i, e in zip(inputs, want):
+                x.copy_(i[0])
+                dy.copy_(i[1])
+                for graph, out in zip(graphs, got):
+                    graph.replay()
+                    torch.cuda.synchronize()
+                    assert all(torch.equal(a, b) for a, b in zip(out, e))
+                assert all(torch.equal(a, b) for a, b in zip(step(*i), e))
+
+
+def test_outputs_carry_no_graph(L):
+    x = torch.randn(70, 128, device="cuda", requires_grad=True)
+    w = L.quantize_f8(torch.randn(64, 128, device="cuda", requires_grad=True), 128)
+    x8 = L.quantize_f8(x)
+    for t in (w.q, x8.q, x8.scale, L.dequantize_f8(x8), L.linear_f8(x, w)) + L.linear_f8_backward(L.linear_f8(x, w).detach().requires_grad_(), x8, w):
+        assert not t.requires_grad
+
+
+def test_refusals(L):
+    x = torch.randn(4, 256, device="cuda")
+    w, x8 = L.quantize_f8(torch.randn(8, 256, device="cuda"), 128), L.quantize_f8(x)
+    dy = torch.randn(4, 8, device="cuda")
+    kept = L.quantize_rows(x)
+    bad = [
+        (ValueError, lambda: L.quantize_f8(x, 64)), (TypeError, lambda: L.quantize_f8(x, 1, torch.int8)), (TypeError, lambda: L.quantize_f8(x.double())), (ValueError, lambda: L.quantize_f8(x.cpu())),
+        (ValueError, lambda: L.quantize_f8(x[:, :0])), (TypeError, lambda: L.dequantize_f8(x8, torch.int8)), (ValueError, lambda: L.dequantize_f8(kept)),
+        (TypeError, lambda: L.linear_q8(x, L.Rows8(x8.q, x8.scale, 256))),
+        (ValueError, lambda: L.linear_f8(x[:, :200], w)), (TypeError, lambda: L.linear_f8(x, w, dtype=F16)), (ValueError, lambda: L.linear_f8(x, w, torch.ones(7, device="cuda"))),
+        (ValueError, lambda: L.linear_f8(x, L.Float8(w.q[:, :200], w.scale, 200, 128))), (ValueError, lambda: L.linear_f8(x, L.Float8(w.q, w.scale, 256, 1))),
+        (ValueError, lambda: L.linear_f8(x, L.Float8(w.q, w.scale[:, :1], 256, 128))), (ValueError, lambda: L.linear_f8(x, L.Float8(w.q, w.scale, 256, 2))),
+        (TypeError, lambda: L.linear_f8(x, L.Float8(w.q.view(torch.uint8), w.scale, 256, 128))), (TypeError, lambda: L.linear_f8(x, L.Float8(w.q, w.scale.view(torch.uint8), 256, 128))),
+        (ValueError, lambda: L.linear_f8_backward(x, x8, w)), (TypeError, lambda: L.linear_f8_backward(dy, x8, w, torch.float16)), (TypeError, lambda: L.linear_f8_backward(dy, x, w)),
+    ]
+    for error, call in bad:
+        with pytest.raises(error):
+            call()
+    from paper_1803_03288_amd import binding
+    for call in (lambda: L.linear_f8(x, L.quantize_f8(x, 1, E5)),                       # weights are e4m3
+                 lambda: L.linear_f8(x, L.Float8(torch.zeros(8, 256 + 16, dtype=torch.uint8, device="cuda").view(E4)[:, :256], w.scale, 256, 128))):
+        with pytest.raises(binding.TicTacError) as e:
+            call()
+        assert e.value.code == -9
