@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_
     tile_of(blockIdx.x - all.first[which], all.tiles_r[which], all.tiles_c[which], split, tr, tc);
     const int32_t r0 = tr * TR, c0 = tc * TC;
     const int32_t first = (int32_t)((int64_t)a.steps * split / a.splits), last = (int32_t)((int64_t)a.steps * (split + 1) / a.splits);
-    typedef TileLoads<TR, TC, 4, false> Loads;
+    typedef TileLoads<TR, TC, 4, 0> Loads;
     constexpr int kLoads = Loads::LP + Loads::LQ;
     Loads loads;
     loads.init(a, r0, c0, first, wave);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
     const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
     const char *const tp = lds + (wr * FR * 16 + (frow >> 2) * 8 + (frow & 3)) * 128, *const tq = lds + TR * 128 + (wc * FC * 16 + frow) * 128;
     constexpr bool kScaled = Scaled<OP>::value, kBiased = kScaled || Biased<OP>::value;
-    TileLoads<TR, TC, 4, true> loads;
+    TileLoads<TR, TC, 4, 1> loads;
     typename OP::acc acc[FR][FC];
     i32x4 fp[2][FR], fq[2][FC];
     int32_t r0, c0, which;

@@ -141,8 +141,8 @@ __device__ __forceinline__ void tile_of(int32_t block, int32_t tiles_r, int32_t 
 // The loads of a tile.  A load brings 8 rows of 128 bytes to LDS, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i
 // holds the bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.  Rows behind the end are the last row again; nobody
 // stores what comes of them.
-// PAIRED: rows of p go to the places that suit the reads of product_kernel_256, j ^ (i % 4 + 4 (i / 8 % 2)).
-template <int TR, int TC, int WAVES, bool PAIRED>
+// ORDER: rows of p go to the places that suit the reads of product_kernel_256, j ^ (i % 4 + 4 (i / 8 % 2)) (1), or of product_f8_kernel_256, j ^ (i % 4 + 4 (i / 16 % 2)) (2).
+template <int TR, int TC, int WAVES, int ORDER>
 struct TileLoads {
     static constexpr int LP = TR / 8 / WAVES, LQ = TC / 8 / WAVES;      // per wave and step
     uint32_t off_p[LP], off_q[LQ];
@@ -150,9 +150,9 @@ struct TileLoads {
     int32_t p_left;                     // steps until p starts again
     __device__ __forceinline__ void init(const ProductArgs &a, int32_t r0, int32_t c0, int32_t first, int wave)
     {
-        static_assert(WAVES % 2 == 0, "rows 8 (i WAVES + wave) .. + 7: bit 3 is that of the wave");
+        static_assert(WAVES % 4 == 0, "rows 8 (i WAVES + wave) .. + 7: bits 3 and 4 are those of the wave");
         const int lane = threadIdx.x & 63, row = lane >> 3, col = ((lane & 7) ^ row) * 16;
-        const int col_p = PAIRED ? ((lane & 7) ^ ((row & 3) | (wave & 1) << 2)) * 16 : col;
+        const int col_p = ORDER ? ((lane & 7) ^ ((row & 3) | (wave >> (ORDER - 1) & 1) << 2)) * 16 : col;
 #pragma unroll
         for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col_p;
 #pragma unroll
