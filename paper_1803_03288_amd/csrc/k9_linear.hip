@@ -3,6 +3,8 @@
 // dy' is dy in blocks of 128 outputs, dy" and x" are dy and x in blocks of 128 rows, w' is w in blocks of 128 outputs: an operand's blocks lie along what is summed over.
 // Outputs of 16 bits come from the matrix instructions for 8-bit floats (k9_product.hip says what those cut off); float32 ones from those for bf16, in which the
 // operands' values are exact, with sums in float32.
+#include <algorithm>
+
 #include "device_utils.h"
 #include "k9_product.h"
 
@@ -240,6 +242,112 @@ hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
     return launch_products_f8(&a, 1, room.plan.tile, ColumnSums{}, s);
 }
 
+// ---- dx with few rows: bound by the bytes of the weights ----
+// The weights, in blocks of 128 x 128, have k (the outputs o) as rows, and the matrix instruction wants 32 of k per lane.  A lane reads eight bytes of each of 32 rows, a wave 128 rows of
+// 128 columns, one block; squares of 4 x 4 bytes are turned round in registers, and byte j of the eight is an operand whose row r is column 8 r + j, so that a lane's results are columns
+// next to each other.  A workgroup has 128 columns and a part of k, its eight waves blocks of that in turn; their sums meet in LDS, in fixed order.  The 16 KB that each wave
+// has under way are more than memory's latency asks for.
+constexpr int kBackWaves = 8;
+
+// four rows of four bytes to four columns
+__device__ __forceinline__ void turn4(uint32_t &a, uint32_t &b, uint32_t &c, uint32_t &d)
+{
+    const uint32_t ab_lo = __builtin_amdgcn_perm(b, a, 0x05010400), ab_hi = __builtin_amdgcn_perm(b, a, 0x07030602);       // a0 b0 a1 b1, a2 b2 a3 b3
+    const uint32_t cd_lo = __builtin_amdgcn_perm(d, c, 0x05010400), cd_hi = __builtin_amdgcn_perm(d, c, 0x07030602);
+    a = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x05040100);
+    b = __builtin_amdgcn_perm(cd_lo, ab_lo, 0x07060302);
+    c = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x05040100);
+    d = __builtin_amdgcn_perm(cd_hi, ab_hi, 0x07060302);
+}
+
+template <int QF, int TB>
+__global__ __launch_bounds__(kBackWaves * 64) void linear_f8_dx_few_kernel(LinearF8Args p, F8Operand dy, int32_t splits, float *parts)
+{
+    extern __shared__ float room[];                             // [waves][8][64 lanes][4]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int64_t strips = gridDim.x / splits, strip = blockIdx.x % strips, i0 = strip * 128;
+    const int32_t split = (int32_t)(blockIdx.x / strips), all = (int32_t)((p.outs + 127) / 128);
+    const int32_t first = (int32_t)((int64_t)all * split / splits), last = (int32_t)((int64_t)all * (split + 1) / splits);
+    f32x4 acc[8][TB] = {};
+    for (int32_t u = first + wave; u < last; u += kBackWaves) {
+        const int64_t o0 = (int64_t)u * 128 + g * 32, rest = p.outs - o0;       // (rows behind the end: the last again, times zeros)
+        const uint8_t *const w = p.w.q + i0 + r * 8;
+        uint32_t v[2][32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const uint2 two = *(const uint2 *)(w + (e < rest ? o0 + e : p.outs - 1) * p.w.ld);
+            v[0][e] = two.x;
+            v[1][e] = two.y;
+        }
+        const int we = p.w.scale[(int64_t)u * p.w.ld_scale + strip];
+        i32x8 q[TB];
+        int qe[TB];
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+            const int64_t t = min((int64_t)b * 16 + r, p.rows - 1);
+            const i32x4 *const from = (const i32x4 *)((const uint8_t *)dy.q + t * dy.ld + o0);
+            const i32x4 lo = from[0], hi = from[1];
+            q[b] = i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            qe[b] = dy.scale[t * dy.ld_scale + u];
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) turn4(v[h][e], v[h][e + 1], v[h][e + 2], v[h][e + 3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                i32x8 f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (int32_t)v[h][e * 4 + j];
+#pragma unroll
+                for (int b = 0; b < TB; ++b)
+                    acc[h * 4 + j][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f, q[b], acc[h * 4 + j][b], TICTAC_E4M3, QF, 0, we, 0, qe[b]);
+            }
+        }
+    }
+    // A thread adds up eight columns of one row over the waves, in their order: element e of lane l.
+    const int le = threadIdx.x & 255, from = le >> 2;
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+        if (b) __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *(f32x4 *)(room + ((wave * 8 + j) * 64 + lane) * 4) = acc[j][b];
+        __syncthreads();
+        const int64_t t = b * 16 + (from & 15), i = i0 + 8 * (4 * (from >> 4) + (le & 3));
+        if (threadIdx.x >= 256 || t >= p.rows) continue;
+        float sum[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            sum[j] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kBackWaves; ++k) sum[j] += room[(k * 8 + j) * 256 + le];
+        }
+        if (splits > 1) {
+            store8<TICTAC_F32, false>(parts + ((int64_t)split * p.rows + t) * p.cols, i, p.cols, sum);
+        } else if (p.dtype == TICTAC_F16) {
+            store8<TICTAC_F16, false>((_Float16 *)p.dx + t * p.ld_dx, i, p.cols, sum);
+        } else {
+            store8<TICTAC_BF16, false>((__bf16 *)p.dx + t * p.ld_dx, i, p.cols, sum);
+        }
+    }
+}
+
+static int32_t dx_few_splits(int64_t cols, int64_t outs) { return parts_along_k(f8_blocks(cols), f8_blocks(outs) / kBackWaves, 256); }     // a block for each wave at least
+
+template <int QF>
+static hipError_t launch_dx_few(const LinearF8Args &p, const F8Operand &dy, void *parts, hipStream_t s)
+{
+    const int32_t splits = dx_few_splits(p.cols, p.outs);
+    const auto kernel = p.rows <= 16 ? linear_f8_dx_few_kernel<QF, 1> : p.rows <= 32 ? linear_f8_dx_few_kernel<QF, 2> : linear_f8_dx_few_kernel<QF, 4>;
+    const size_t lds = (size_t)kBackWaves * 8 * 64 * 16;
+    if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(f8_blocks(p.cols) * splits)), dim3(kBackWaves * 64), lds, s, p, dy, splits, (float *)parts);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess || splits == 1) return e;
+    ProductArgs a{};
+    a.R = (int32_t)p.cols; a.C = (int32_t)p.rows; a.splits = splits; a.out = p.dx; a.ld_out = p.ld_dx; a.dtype = p.dtype; a.parts = parts;
+    return launch_product_join_bf16(a, s);
+}
+
 // ---- backward ----
 struct BackwardRoom {
     int64_t padded_o, padded_t;
@@ -255,7 +363,9 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.padded_t = rows8_stride(rows);
     const int64_t step = exact ? 64 : 128;
     const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / step)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / step)}};
-    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes, 2);
+    const bool few = rows <= kFewRows && !exact;            // (where dx may come from weights as they lie: dw by itself)
+    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes + few, 2 - few);
+    if (few) r.plan.splits[1] = r.plan.splits[0];
     const size_t e = exact ? 0 : 1;         // (values as bf16 have no scales)
     r.w = r.sums + up((size_t)f8_blocks(rows) * outs * 4);
     r.we = r.w + up((size_t)cols * r.padded_o * size);
@@ -266,7 +376,7 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.dy_cols = r.dy_rows_e + up(e * rows * f8_scale_stride(outs));
     r.dy_cols_e = r.dy_cols + up((size_t)outs * r.padded_t * size);
     r.parts_x = r.dy_cols_e + up(e * outs * f8_scale_stride(rows));
-    r.parts_w = r.parts_x + up(product_parts_bytes(r.plan.splits[0], (int32_t)cols, (int32_t)rows));
+    r.parts_w = r.parts_x + up(product_parts_bytes(few ? std::max(r.plan.splits[0], dx_few_splits(cols, outs)) : r.plan.splits[0], (int32_t)cols, (int32_t)rows));
     r.bytes = r.parts_w + up(product_parts_bytes(r.plan.splits[1], (int32_t)cols, (int32_t)outs));
     return r;
 }
@@ -295,8 +405,9 @@ hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
     char *at = (char *)p.workspace;
     F8TurnArgs t{};
     t.dtype = p.dtype; t.format = p.format; t.rows = p.rows; t.cols = p.cols; t.outs = p.outs; t.dy = p.dy; t.ld_dy = p.ld_dy; t.x = p.x8; t.w = p.w;
+    const bool dx_few = p.dx && p.rows <= kFewRows && !exact && p.w.shift;
     if (p.dx) {
-        t.w_cols = {at + room.w, room.padded_o, (uint8_t *)at + room.we, f8_scale_stride(p.outs)};
+        if (!dx_few) t.w_cols = {at + room.w, room.padded_o, (uint8_t *)at + room.we, f8_scale_stride(p.outs)};
         t.dy_rows = {at + room.dy_rows, room.padded_o, (uint8_t *)at + room.dy_rows_e, f8_scale_stride(p.outs)};
     }
     if (p.dw) {
@@ -314,7 +425,10 @@ hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
         x.R = (int32_t)p.cols; x.C = (int32_t)outputs; x.steps = x.p_steps = (int32_t)(padded / step);
         x.splits = splits; x.out = out; x.ld_out = ld; x.parts = at + parts; x.dtype = p.dtype;
     };
-    if (p.dx) add(t.w_cols, t.dy_rows, room.padded_o, p.rows, p.dx, p.ld_dx, room.plan.splits[0], room.parts_x);
+    if (dx_few) {
+        if (const hipError_t e = p.format == TICTAC_E5M2 ? launch_dx_few<TICTAC_E5M2>(p, t.dy_rows, at + room.parts_x, s) : launch_dx_few<TICTAC_E4M3>(p, t.dy_rows, at + room.parts_x, s); e != hipSuccess) return e;
+    }
+    if (p.dx && !dx_few) add(t.w_cols, t.dy_rows, room.padded_o, p.rows, p.dx, p.ld_dx, room.plan.splits[0], room.parts_x);
     if (p.dw) add(t.x_cols, t.dy_cols, room.padded_t, p.outs, p.dw, p.ld_dw, room.plan.splits[1], room.parts_w);
     const ColumnSums c{t.sums, f8_blocks(p.rows), p.outs, p.db, p.dtype};
     if (!exact) return launch_products_f8(a, n, room.plan.tile, c, s);

@@ -147,6 +147,14 @@ def test_linear(L, rows, cols, outs, dtype):
     close(L.linear_f8(x.cuda(), w), want, bound, dtype)
 
 
+@pytest.mark.parametrize("rows,cols,outs", [(520, 300, 700), (1100, 1300, 2100), (1030, 129, 2304), (2048, 600, 1027)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_products_by_the_largest_tiles(L, rows, cols, outs, dtype):
+    """Two steps and more, odd and even numbers of them, whole tiles and ends of rows and columns, aligned and not."""
+    test_linear(L, rows, cols, outs, dtype)
+    test_linear_backward(L, rows, cols, outs, dtype)
+
+
 @pytest.mark.parametrize("rows,cols,outs", [(5, 300, 40), (40, 1000, 90), (90, 1000, 200), (200, 4000, 300)])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("xblock,f8", [(1, E5), (128, E4), (128, E5)])
@@ -175,7 +183,7 @@ def test_linear_on_blocks_that_spoil_their_rows_only(L, rows, dtype):
     assert torch.isnan(y[:, 3]).all() and torch.isfinite(y[:, :3]).all() and torch.isfinite(y[:, 4:]).all()
 
 
-GRADIENTS = [(1, 1, 1), (1, 300, 200), (3, 1000, 129), (32, 4100, 260), (33, 130, 500), (64, 257, 2000), (65, 130, 70), (101, 777, 1001), (128, 128, 128), (129, 500, 131), (300, 153, 587),
+GRADIENTS = [(1, 1, 1), (1, 300, 201), (16, 1000, 4097), (17, 2304, 2000), (48, 500, 3000), (2, 4097, 130), (3, 1000, 129), (32, 4100, 260), (33, 130, 500), (64, 257, 2000), (65, 130, 70), (101, 777, 1001), (128, 128, 128), (129, 500, 131), (300, 153, 587),
              (700, 256, 384), (1100, 300, 200)]
 
 
