@@ -13,7 +13,6 @@ namespace tictac {
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kF8Block = 128;
-constexpr uint32_t kF8NaN = 0x7f7f7f7fu;                // of either type
 
 __device__ __forceinline__ int f8_top(int format) { return format == TICTAC_E5M2 ? 16 : 9; }
 
@@ -29,9 +28,10 @@ __device__ __forceinline__ float f8_factor(uint32_t scale)
     return __builtin_bit_cast(float, scale == 255 ? 0x7fc00000u : scale == 0 ? 0x00400000u : scale << 23);
 }
 
-__device__ __forceinline__ uint32_t f8_pack4(float a, float b, float c, float d, int format)
+template <int FORMAT>
+__device__ __forceinline__ uint32_t f8_pack4(float a, float b, float c, float d)
 {
-    if (format == TICTAC_E5M2) return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(c, d, __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false), true);
+    if (FORMAT == TICTAC_E5M2) return (uint32_t)__builtin_amdgcn_cvt_pk_bf8_f32(c, d, __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false), true);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 __device__ __forceinline__ void f8_values4(uint32_t w, int format, float *v)
@@ -41,23 +41,23 @@ __device__ __forceinline__ void f8_values4(uint32_t w, int format, float *v)
     else put(__builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true));
 }
 
-// Eight values of a block in 8 bits, elements `left` and on of them zeros (those behind a row's end, where the block is NaN).
-__device__ __forceinline__ uint2 f8_quantized8(const float *v, uint32_t scale, int format, int64_t left)
+// What eight values of a block that is NaN become: `left` of them lie before the row's end.
+__device__ __forceinline__ uint2 f8_nans(int64_t left)
 {
-    if (scale == 255) {
-        uint64_t all = (uint64_t)kF8NaN << 32 | kF8NaN;
-        if (left < 8) all = left <= 0 ? 0 : all >> (8 * (8 - left));
-        return uint2{(uint32_t)all, (uint32_t)(all >> 32)};
-    }
-    const float inv = f8_inverse(scale);
-    if (scale >= 256u - f8_top(format)) {                   // (what would be rounded to 2^128, which float32 does not hold, gets the value below it)
-        const float most = format == TICTAC_E5M2 ? 28672.0f : 240.0f;
-        float u[8];
+    const uint64_t all = left <= 0 ? 0 : 0x7f7f7f7f7f7f7f7full >> (8 * (8 - (left < 8 ? left : 8)));
+    return uint2{(uint32_t)all, (uint32_t)(all >> 32)};
+}
+// Eight values of a block in 8 bits, without a branch: the kernels that turn operands round hold dozens of these, and what they wait for is their code.
+template <int FORMAT>
+__device__ __forceinline__ uint2 f8_quantized8(const float *v, uint32_t scale, uint2 nans)
+{
+    constexpr uint32_t kTop = FORMAT == TICTAC_E5M2 ? 16 : 9;
+    const float inv = f8_inverse(scale), most = scale >= 256 - kTop ? (FORMAT == TICTAC_E5M2 ? 28672.0f : 240.0f) : (FORMAT == TICTAC_E5M2 ? 57344.0f : 448.0f);
+    float u[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) u[i] = fminf(fmaxf(v[i] * inv, -most), most);
-        return uint2{f8_pack4(u[0], u[1], u[2], u[3], format), f8_pack4(u[4], u[5], u[6], u[7], format)};
-    }
-    return uint2{f8_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, format), f8_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv, format)};
+    for (int i = 0; i < 8; ++i) u[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -most, most);        // (2^128 is out of float32's range)
+    const uint2 q{f8_pack4<FORMAT>(u[0], u[1], u[2], u[3]), f8_pack4<FORMAT>(u[4], u[5], u[6], u[7])};
+    return scale == 255 ? nans : q;
 }
 __device__ __forceinline__ void f8_values8(uint2 q, uint32_t scale, int format, float *v)
 {

@@ -204,8 +204,8 @@ __device__ __forceinline__ void update8(const UpdateTable &table, const UpdateTe
             r[i] = f8_at_random(r[i], ir, bits >> 16);
         }
         const auto put8 = [&](void *to, uint8_t *scales, uint32_t scale, const float *x) {
-            uint2 q{f8_pack4(x[0], x[1], x[2], x[3], TICTAC_E4M3), f8_pack4(x[4], x[5], x[6], x[7], TICTAC_E4M3)};
-            if (scale == 255) q = f8_quantized8(x, 255, TICTAC_E4M3, t.numel - at);
+            uint2 q{f8_pack4<TICTAC_E4M3>(x[0], x[1], x[2], x[3]), f8_pack4<TICTAC_E4M3>(x[4], x[5], x[6], x[7])};
+            if (scale == 255) q = f8_nans(t.numel - at);
             *(uint2 *)((uint8_t *)to + at) = q;
             if ((threadIdx.x & 15) == 0) scales[at >> 7] = (uint8_t)scale;
         };

@@ -14,7 +14,7 @@ __device__ __forceinline__ void put_scale(uint8_t *row, int64_t at, int64_t bloc
     if (lane == 0 || (lane < 4 && at == blocks - 1 && at + lane < (blocks + 3) / 4 * 4)) row[at + lane] = lane ? (uint8_t)0 : (uint8_t)scale;
 }
 
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, int FORMAT>
 __global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int64_t blocks, int64_t total)
 {
     using E = Elem<DT>;
@@ -39,10 +39,10 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int6
             uint32_t m = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
-            const uint32_t scale = f8_scale(row16_max(m), p.format);
-            const uint2 q = f8_quantized8(v, scale, p.format, p.cols - col[k]);     // (also the zeros behind the end)
+            const uint32_t scale = f8_scale(row16_max(m), FORMAT);
+            const uint2 q = f8_quantized8<FORMAT>(v, scale, f8_nans(p.cols - col[k]));      // (also the zeros behind the end)
             if (p.wide) {
-                f8_values8(q, scale, p.format, v);
+                f8_values8(q, scale, FORMAT, v);
                 *(i32x4 *)(p.wide + row[k] * p.ld_q + col[k]) = f8_bf16(v);
                 continue;
             }
@@ -70,7 +70,7 @@ __device__ __forceinline__ void load_tile(const void *x, int64_t ld, int64_t row
 }
 
 // Blocks of 128 x 128: a workgroup each, which stays in registers between its maximum and its rounding.
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, int FORMAT>
 __global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p, int64_t across)
 {
     using E = Elem<DT>;
@@ -90,13 +90,14 @@ __global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p
     m = wave_max_u32(m);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = m;
     __syncthreads();
-    const uint32_t scale = f8_scale(max(max(part[0], part[1]), max(part[2], part[3])), p.format);
+    const uint32_t scale = f8_scale(max(max(part[0], part[1]), max(part[2], part[3])), FORMAT);
+    const uint2 nans = f8_nans(p.cols - t.c);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         if (t.r + e >= p.rows) continue;
         float v[8];
         E::floats(raw[e], v);
-        *(uint2 *)(p.q + (t.r + e) * p.ld_q + t.c) = f8_quantized8(v, scale, p.format, p.cols - t.c);
+        *(uint2 *)(p.q + (t.r + e) * p.ld_q + t.c) = f8_quantized8<FORMAT>(v, scale, nans);
     }
     put_scale(p.scale + tile_r * p.ld_scale, tile_c, across, threadIdx.x, scale);
 }
@@ -136,11 +137,14 @@ template <int DT, bool WIDE>
 static hipError_t quantize(const F8QuantizeArgs &p, hipStream_t s)
 {
     const int64_t blocks = f8_blocks(p.cols);
+    const bool e5 = p.format == TICTAC_E5M2;
     if (p.block == 1) {
         const int64_t total = blocks * p.rows;
-        hipLaunchKernelGGL((quantize_f8_kernel<DT, WIDE>), dim3(blocks_of((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, blocks, total);
+        const auto kernel = e5 ? quantize_f8_kernel<DT, WIDE, TICTAC_E5M2> : quantize_f8_kernel<DT, WIDE, TICTAC_E4M3>;
+        hipLaunchKernelGGL(kernel, dim3(blocks_of((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, blocks, total);
     } else {
-        hipLaunchKernelGGL((quantize_f8_tiles_kernel<DT, WIDE>), dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, blocks);
+        const auto kernel = e5 ? quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E5M2> : quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E4M3>;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, blocks);
     }
     return hipGetLastError();
 }
@@ -168,8 +172,8 @@ struct TurnRoom {
 };
 
 // v: 8 x 8 of a tile; the blocks of its columns go to `to`, [columns][ld], in the format
-template <bool BF16>
-__device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8][8], int64_t rows, int64_t cols, int64_t tile_r, int64_t tile_c, int format, const F8Operand &to,
+template <bool BF16, int FORMAT>
+__device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8][8], int64_t rows, int64_t cols, int64_t tile_r, int64_t tile_c, const F8Operand &to,
                                             TurnRoom &room, char *turned)
 {
 #pragma unroll
@@ -184,12 +188,13 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
         uint32_t m = 0;
 #pragma unroll
         for (int g = 0; g < 16; ++g) m = max(m, room.part[g][threadIdx.x]);
-        const uint32_t scale = f8_scale(m, format);
+        const uint32_t scale = f8_scale(m, FORMAT);
         room.scale[threadIdx.x] = (uint8_t)scale;
         const int64_t c = tile_c * 128 + threadIdx.x;
         if (!BF16 && c < cols) to.scale[c * to.ld_scale + tile_r] = (uint8_t)scale;
     }
     __syncthreads();
+    const uint2 nans = f8_nans(rows - t.r);
     // Eight rows of a column are one piece; piece g of column c lies at place g ^ c / 8 of its 16: a wave's stores and loads then meet all banks alike.
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -197,10 +202,10 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
         const uint32_t scale = room.scale[t.lane * 8 + i];
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] = v[e][i];
-        const uint2 q = f8_quantized8(u, scale, format, rows - t.r);
+        const uint2 q = f8_quantized8<FORMAT>(u, scale, nans);
         const int at = (t.lane * 8 + i) * 16 + (t.group ^ t.lane);
         if (BF16) {
-            f8_values8(q, scale, format, u);
+            f8_values8(q, scale, FORMAT, u);
             *(i32x4 *)(turned + at * 16) = f8_bf16(u);
         } else {
             *(uint2 *)(turned + at * 8) = q;
@@ -220,7 +225,7 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
     }
 }
 
-template <int DT, bool WIDE>
+template <int DT, bool WIDE, int FORMAT>
 __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_tiles, int64_t x_tiles)
 {
     using E = Elem<DT>;
@@ -239,18 +244,19 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_t
             for (int e = 0; e < 8; ++e) E::floats(raw[e], v[e]);
         }
         if (p.dy_rows.q) {
+            const uint2 nans = f8_nans(p.outs - t.c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 uint32_t m = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[e][i]));
-                const uint32_t scale = f8_scale(row16_max(m), p.format);
+                const uint32_t scale = f8_scale(row16_max(m), FORMAT);
                 if (t.r + e >= p.rows) continue;
-                const uint2 q = f8_quantized8(v[e], scale, p.format, p.outs - t.c);
+                const uint2 q = f8_quantized8<FORMAT>(v[e], scale, nans);
                 const int64_t at = (t.r + e) * p.dy_rows.ld + t.c;
                 if (BF16) {
                     float u[8];
-                    f8_values8(q, scale, p.format, u);
+                    f8_values8(q, scale, FORMAT, u);
                     *(i32x4 *)((uint16_t *)p.dy_rows.q + at) = f8_bf16(u);
                 } else {
                     *(uint2 *)((uint8_t *)p.dy_rows.q + at) = q;
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_t
             }
             __syncthreads();
         }
-        if (p.dy_cols.q) put_columns<BF16>(t, v, p.rows, p.outs, tile_r, tile_c, p.format, p.dy_cols, room, turned);
+        if (p.dy_cols.q) put_columns<BF16, FORMAT>(t, v, p.rows, p.outs, tile_r, tile_c, p.dy_cols, room, turned);
         return;
     }
     unit -= dy_tiles;
@@ -295,7 +301,7 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_t
         }
         f8_values8(q, scale, from.format, v[e]);
     }
-    put_columns<BF16>(t, v, rows, p.cols, tile_r, tile_c, TICTAC_E4M3, is_x ? p.x_cols : p.w_cols, room, turned);
+    put_columns<BF16, TICTAC_E4M3>(t, v, rows, p.cols, tile_r, tile_c, is_x ? p.x_cols : p.w_cols, room, turned);
 }
 
 template <int DT, bool WIDE>
@@ -304,7 +310,8 @@ static hipError_t turn(const F8TurnArgs &p, hipStream_t s)
     const int64_t dy = p.dy_rows.q || p.dy_cols.q || p.sums ? f8_blocks(p.rows) * f8_blocks(p.outs) : 0, x = p.x_cols.q ? f8_blocks(p.rows) * f8_blocks(p.cols) : 0,
                   w = p.w_cols.q ? f8_blocks(p.outs) * f8_blocks(p.cols) : 0;
     if (dy + x + w == 0) return hipSuccess;
-    hipLaunchKernelGGL((turn_f8_kernel<DT, WIDE>), dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, dy, x);
+    const auto kernel = p.format == TICTAC_E5M2 ? turn_f8_kernel<DT, WIDE, TICTAC_E5M2> : turn_f8_kernel<DT, WIDE, TICTAC_E4M3>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, dy, x);
     return hipGetLastError();
 }
 hipError_t launch_turn_f8(const F8TurnArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.dy, p.dtype, p.ld_dy, p.outs), turn, p, s); }

@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "device_utils.h"
+#include "k8_tiles.h"
 #include "k9_product.h"
 
 namespace tictac {
@@ -332,6 +333,81 @@ __global__ __launch_bounds__(kBackWaves * 64) void linear_f8_dx_few_kernel(Linea
     }
 }
 
+// dw where the rows are one block: a matrix instruction is all that an output takes, and dw's bytes are what bounds it.  A wave has 64 columns, whose operands (turned round before, 128
+// bytes of k each, of which those behind the last row are not read) stay in registers, and 128 outputs, a workgroup 512 columns.  Row r of operand j is the column at(r) + j: a lane's results (rows 4 g + e) then are eight next to each other at
+// 8 g, and eight at 32 + 8 g, and four lanes store 64 bytes in a row.
+constexpr int kDwOuts = 128;
+
+template <int QF, int DT, bool WIDE>
+__global__ __launch_bounds__(512) void linear_f8_dw_few_kernel(LinearF8Args p, F8Operand x, F8Operand dy, ColumnSums sums)
+{
+    using T = typename Elem<DT>::type;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+    const int64_t o0 = (int64_t)blockIdx.y * kDwOuts, i0 = (int64_t)blockIdx.x * 512 + wave * 64;
+    if (sums.out && blockIdx.x == 0 && (int)threadIdx.x < kDwOuts && o0 + threadIdx.x < p.outs) put_param(sums.out, DT, o0 + threadIdx.x, sums.sums[o0 + threadIdx.x]);
+    if (i0 >= p.cols) return;
+    const auto operand = [&](const F8Operand &from, int64_t row) {
+        const i32x4 *const at = (const i32x4 *)((const uint8_t *)from.q + row * from.ld + g * 32);
+        i32x4 lo{}, hi{};
+        if (g * 32 < p.rows) { lo = at[0]; hi = at[1]; }
+        return i32x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    const int64_t column = i0 + ((c & 2) << 4) + ((c >> 2) << 3) + ((c & 1) << 2);
+    const bool whole = WIDE && i0 + 64 <= p.cols;
+    i32x8 f[4], q;
+    int fe[4], qe;
+    const auto request = [&](int b) {
+        const int64_t o = min(o0 + b * 16 + c, p.outs - 1);
+        q = operand(dy, o);
+        qe = dy.scale[o * dy.ld_scale];
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t i = min(column + j, p.cols - 1);
+        f[j] = operand(x, i);
+        fe[j] = x.scale[i * x.ld_scale];
+    }
+    request(0);
+#pragma unroll 2
+    for (int b = 0; b < kDwOuts / 16; ++b) {
+        const i32x8 now = q;
+        const int e = qe;
+        if (b + 1 < kDwOuts / 16) request(b + 1);
+        f32x4 acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f[j], now, f32x4{}, TICTAC_E4M3, QF, 0, fe[j], 0, e);
+        const int64_t out = o0 + b * 16 + c;
+        if (whole && o0 + b * 16 + 16 <= p.outs) {
+            i32x4 piece[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) v[n] = acc[n & 3][h * 2 + (n >> 2)];
+                piece[h] = __builtin_bit_cast(i32x4, Elem<DT>::pack(v));
+            }
+            put_lines<32>((T *)p.dw + i0, g * 8, (int32_t)out, p.ld_dw, piece[0], piece[1]);
+            continue;
+        }
+        if (out >= p.outs) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float v[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) v[n] = acc[n & 3][h * 2 + (n >> 2)];
+            store8<DT, WIDE>((T *)p.dw + out * p.ld_dw, i0 + h * 32 + g * 8, p.cols, v);
+        }
+    }
+}
+
+template <int DT, bool WIDE>
+static hipError_t launch_dw_few(const LinearF8Args &p, const F8Operand &x, const F8Operand &dy, const ColumnSums &sums, hipStream_t s)
+{
+    const auto kernel = p.format == TICTAC_E5M2 ? linear_f8_dw_few_kernel<TICTAC_E5M2, DT, WIDE> : linear_f8_dw_few_kernel<TICTAC_E4M3, DT, WIDE>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p.cols + 511) / 512), (unsigned)((p.outs + kDwOuts - 1) / kDwOuts)), dim3(512), 0, s, p, x, dy, sums);
+    return hipGetLastError();
+}
+
 static int32_t dx_few_splits(int64_t cols, int64_t outs) { return parts_along_k(f8_blocks(cols), f8_blocks(outs) / kBackWaves, 256); }     // a block for each wave at least
 
 template <int QF>
@@ -363,9 +439,9 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.padded_t = rows8_stride(rows);
     const int64_t step = exact ? 64 : 128;
     const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / step)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / step)}};
-    const bool few = rows <= kFewRows && !exact;            // (where dx may come from weights as they lie: dw by itself)
-    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes + few, 2 - few);
-    if (few) r.plan.splits[1] = r.plan.splits[0];
+    const bool few = rows <= kFewRows && !exact;            // (dx then may come from the weights as they lie)
+    // up to a block of rows dw is by itself, and the tiles are dx's alone
+    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes, rows <= kF8Block ? 1 : 2);
     const size_t e = exact ? 0 : 1;         // (values as bf16 have no scales)
     r.w = r.sums + up((size_t)f8_blocks(rows) * outs * 4);
     r.we = r.w + up((size_t)cols * r.padded_o * size);
@@ -429,8 +505,15 @@ hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
         if (const hipError_t e = p.format == TICTAC_E5M2 ? launch_dx_few<TICTAC_E5M2>(p, t.dy_rows, at + room.parts_x, s) : launch_dx_few<TICTAC_E4M3>(p, t.dy_rows, at + room.parts_x, s); e != hipSuccess) return e;
     }
     if (p.dx && !dx_few) add(t.w_cols, t.dy_rows, room.padded_o, p.rows, p.dx, p.ld_dx, room.plan.splits[0], room.parts_x);
-    if (p.dw) add(t.x_cols, t.dy_cols, room.padded_t, p.outs, p.dw, p.ld_dw, room.plan.splits[1], room.parts_w);
     const ColumnSums c{t.sums, f8_blocks(p.rows), p.outs, p.db, p.dtype};
+    if (p.dw && !exact && p.rows <= kF8Block) {
+        const bool wide = wide_rows(p.dw, p.dtype, p.ld_dw, p.cols);
+        const hipError_t e = p.dtype == TICTAC_F16 ? (wide ? launch_dw_few<TICTAC_F16, true>(p, t.x_cols, t.dy_cols, c, s) : launch_dw_few<TICTAC_F16, false>(p, t.x_cols, t.dy_cols, c, s))
+                                                   : (wide ? launch_dw_few<TICTAC_BF16, true>(p, t.x_cols, t.dy_cols, c, s) : launch_dw_few<TICTAC_BF16, false>(p, t.x_cols, t.dy_cols, c, s));
+        if (e != hipSuccess || !n) return e;
+        return launch_products_f8(a, n, room.plan.tile, ColumnSums{}, s);
+    }
+    if (p.dw) add(t.x_cols, t.dy_cols, room.padded_t, p.outs, p.dw, p.ld_dw, room.plan.splits[1], room.parts_w);
     if (!exact) return launch_products_f8(a, n, room.plan.tile, c, s);
     const ProductArgs wide[2] = {a[0], a[1]};
     return launch_products_bf16(wide, n, room.plan.tile, c, s);
