@@ -59,23 +59,35 @@ struct Tile128 {
     __device__ __forceinline__ Tile128(int64_t tile_r, int64_t tile_c) : lane(threadIdx.x & 15), group(threadIdx.x >> 4), r(tile_r * 128 + group * 8), c(tile_c * 128 + lane * 8) {}
 };
 
+// (rows and, with WIDE, columns behind the end: the last again, made zeros, so that all loads are under way at once)
 template <int DT, bool WIDE>
 __device__ __forceinline__ void load_tile(const void *x, int64_t ld, int64_t rows, int64_t cols, const Tile128 &t, typename Elem<DT>::raw (&raw)[8])
 {
+    using E = Elem<DT>;
+    const typename E::type *const from = (const typename E::type *)x;
+    if (WIDE || t.c + 8 <= cols) {
+        const int64_t c = WIDE ? min(t.c, cols - 8) : t.c;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        raw[e] = typename Elem<DT>::raw{};
-        if (t.r + e < rows) raw[e] = load8<DT, WIDE>((const typename Elem<DT>::type *)x + (t.r + e) * ld, t.c, cols);
+        for (int e = 0; e < 8; ++e) {
+            const typename E::type *const at = from + min(t.r + e, rows - 1) * ld + c;
+            raw[e] = WIDE ? E::load(at) : load_anywhere<DT>(at);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[e] = load8<DT, false>(from + min(t.r + e, rows - 1) * ld, t.c, cols);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (t.r + e >= rows || (WIDE && t.c >= cols)) raw[e] = typename E::raw{};
 }
 
 // Blocks of 128 x 128: a workgroup each, which stays in registers between its maximum and its rounding.
 template <int DT, bool WIDE, int FORMAT>
-__global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p, int64_t across)
+__global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p, uint32_t across)
 {
     using E = Elem<DT>;
     __shared__ uint32_t part[4];
-    const int64_t tile_r = blockIdx.x / across, tile_c = blockIdx.x % across;
+    const uint32_t tile_r = blockIdx.x / across, tile_c = blockIdx.x % across;
     const Tile128 t(tile_r, tile_c);
     typename E::raw raw[8];
     load_tile<DT, WIDE>(p.x, p.ld_x, p.rows, p.cols, t, raw);
@@ -144,7 +156,7 @@ static hipError_t quantize(const F8QuantizeArgs &p, hipStream_t s)
         hipLaunchKernelGGL(kernel, dim3(blocks_of((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, blocks, total);
     } else {
         const auto kernel = e5 ? quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E5M2> : quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E4M3>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, blocks);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, (uint32_t)blocks);
     }
     return hipGetLastError();
 }
@@ -226,16 +238,16 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
 }
 
 template <int DT, bool WIDE, int FORMAT>
-__global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_tiles, int64_t x_tiles)
+__global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_tiles, uint32_t x_tiles)
 {
     using E = Elem<DT>;
     constexpr bool BF16 = DT == TICTAC_F32;
     __shared__ TurnRoom room;
     __shared__ __align__(16) char turned[128 * 16 * (BF16 ? 16 : 8)];
-    int64_t unit = blockIdx.x;
+    uint32_t unit = blockIdx.x;
     float v[8][8];
     if (unit < dy_tiles) {
-        const int64_t across = (p.outs + 127) / 128, tile_r = unit / across, tile_c = unit % across;
+        const uint32_t across = (uint32_t)((p.outs + 127) / 128), tile_r = unit / across, tile_c = unit % across;
         const Tile128 t(tile_r, tile_c);
         {
             typename E::raw raw[8];
@@ -289,17 +301,21 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, int64_t dy_t
     const bool is_x = unit < x_tiles;
     if (!is_x) unit -= x_tiles;
     const F8Rows &from = is_x ? p.x : p.w;
-    const int64_t rows = is_x ? p.rows : p.outs, across = (p.cols + 127) / 128, tile_r = unit / across, tile_c = unit % across;
+    const int64_t rows = is_x ? p.rows : p.outs;
+    const uint32_t across = (uint32_t)((p.cols + 127) / 128), tile_r = unit / across, tile_c = unit % across;
     const Tile128 t(tile_r, tile_c);
+    uint2 q[8];
+    uint32_t scale[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        uint2 q{0, 0};
-        uint32_t scale = 127;
-        if (t.r + e < rows) {
-            q = *(const uint2 *)(from.q + (t.r + e) * from.ld + t.c);
-            scale = from.scale[((t.r + e) >> from.shift) * from.ld_scale + tile_c];
-        }
-        f8_values8(q, scale, from.format, v[e]);
+        const int64_t row = min(t.r + e, rows - 1);
+        q[e] = *(const uint2 *)(from.q + row * from.ld + t.c);
+        scale[e] = from.scale[(row >> from.shift) * from.ld_scale + tile_c];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const bool in = t.r + e < rows;
+        f8_values8(uint2{in ? q[e].x : 0, in ? q[e].y : 0}, in ? scale[e] : 127, from.format, v[e]);
     }
     put_columns<BF16, TICTAC_E4M3>(t, v, rows, p.cols, tile_r, tile_c, is_x ? p.x_cols : p.w_cols, room, turned);
 }
@@ -311,7 +327,7 @@ static hipError_t turn(const F8TurnArgs &p, hipStream_t s)
                   w = p.w_cols.q ? f8_blocks(p.outs) * f8_blocks(p.cols) : 0;
     if (dy + x + w == 0) return hipSuccess;
     const auto kernel = p.format == TICTAC_E5M2 ? turn_f8_kernel<DT, WIDE, TICTAC_E5M2> : turn_f8_kernel<DT, WIDE, TICTAC_E4M3>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, dy, x);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, (uint32_t)dy, (uint32_t)x);
     return hipGetLastError();
 }
 hipError_t launch_turn_f8(const F8TurnArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.dy, p.dtype, p.ld_dy, p.outs), turn, p, s); }

@@ -132,6 +132,103 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8A
     }
 }
 
+// Up to sixteen rows of floats, rounded to 8 bits here: every workgroup does that again, into LDS, under its first loads of the weights, which costs less than a launch before it while there
+// are few elements for each thread (kOnceElements).  A workgroup has 16 outputs, its waves blocks of 128 of k in turn, kUnits of them under way.  The 8-bit values are those
+// of quantize_f8_kernel.
+constexpr int kOnceRows = 16, kOnceUnits = 4;
+constexpr int64_t kOnceElements = 32768;
+
+template <int DT, bool WIDE, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void linear_f8_once_kernel(LinearF8Args p)
+{
+    using E = Elem<DT>;
+    constexpr bool EXACT = DT == TICTAC_F32;
+    extern __shared__ __align__(16) uint8_t held[];             // [rows][stride] 8-bit values, [rows][blocks] scales; then [waves][64] sums
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 16;
+    const int32_t units = (int32_t)((p.cols + 127) / 128), rows = (int32_t)p.rows, stride = units * 128 + 16;
+    const int64_t o0 = (int64_t)blockIdx.x * 16, o = min(o0 + row, p.outs - 1);
+    const uint8_t *const w = p.w.q + o * p.w.ld + fk, *const we = p.w.scale + (o >> p.w.shift) * p.w.ld_scale;
+    uint8_t *const scales = held + rows * stride;
+    struct Unit {
+        i32x4 q[2];
+        int e;
+    } unit[kOnceUnits];
+    const auto request = [&](int n, int32_t u) {
+        u = min(u, units - 1);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) unit[n].q[k] = *(const i32x4 *)(w + (int64_t)u * 128 + k * 64);
+        unit[n].e = we[u];
+    };
+#pragma unroll
+    for (int n = 0; n < kOnceUnits; ++n) request(n, wave + n * WAVES);
+    for (int32_t at = (int32_t)threadIdx.x >> 4; at < rows * units; at += WAVES * 4) {
+        const int32_t t = at / units, b = at - t * units, part = (int32_t)threadIdx.x & 15, col = b * 128 + part * 8;
+        float v[8];
+        E::floats(load8<DT, WIDE>((const typename E::type *)p.x + t * p.ld_x, col, p.cols), v);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
+        const uint32_t scale = f8_scale(row16_max(m), TICTAC_E4M3);
+        *(uint2 *)(held + t * stride + col) = f8_quantized8<TICTAC_E4M3>(v, scale, f8_nans(p.cols - col));
+        if (part == 0) scales[at] = (uint8_t)scale;
+    }
+    __syncthreads();
+    const int mine = min(row, rows - 1);
+    const uint8_t *const x = held + mine * stride + fk, *const xe = scales + mine * units;
+    f32x4 acc{};
+    for (int32_t u0 = wave; u0 < units; u0 += kOnceUnits * WAVES) {
+#pragma unroll
+        for (int n = 0; n < kOnceUnits; ++n) {
+            const int32_t u = u0 + n * WAVES;
+            if (u >= units) break;
+            const Unit now = unit[n];
+            if (u + kOnceUnits * WAVES < units) request(n, u + kOnceUnits * WAVES);
+            const i32x4 lo = *(const i32x4 *)(x + u * 128), hi = *(const i32x4 *)(x + u * 128 + 64);
+            const int e = xe[u];
+            if constexpr (EXACT) {
+                i32x4 a[2], b[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    widen(now.q[k], f8_factor(now.e), TICTAC_E4M3, a);
+                    widen(k ? hi : lo, f8_factor(e), TICTAC_E4M3, b);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) acc = mma_bf16(a[h], b[h], acc);
+                }
+            } else {
+                const i32x8 a{now.q[0][0], now.q[0][1], now.q[0][2], now.q[0][3], now.q[1][0], now.q[1][1], now.q[1][2], now.q[1][3]};
+                const i32x8 b{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, TICTAC_E4M3, TICTAC_E4M3, 0, now.e, 0, e);
+            }
+        }
+    }
+    __syncthreads();
+    f32x4 *const sums = (f32x4 *)held;
+    sums[threadIdx.x] = acc;
+    __syncthreads();
+    const int out = threadIdx.x & 15, t = threadIdx.x >> 4;
+    if (t >= rows || o0 + out >= p.outs) return;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) sum += sums[k * 64 + (out >> 2) * 16 + t][out & 3];
+    if (p.bias) sum += param(p.bias, p.bias_dtype, o0 + out);
+    put_param(p.y, p.dtype, t * p.ld_y + o0 + out, sum);
+}
+
+static bool once(int64_t rows, int64_t cols) { return rows <= kOnceRows && rows * rows8_stride(cols) <= kOnceElements; }
+
+template <int DT, bool WIDE>
+static hipError_t launch_once(const LinearF8Args &p, hipStream_t s)
+{
+    // (few workgroups: more waves in each)
+    const int64_t blocks = (p.outs + 15) / 16;
+    const int waves = blocks <= 512 ? 16 : 8;
+    const auto kernel = waves == 16 ? linear_f8_once_kernel<DT, WIDE, 16> : linear_f8_once_kernel<DT, WIDE, 8>;
+    const int64_t units = f8_blocks(p.cols);
+    const size_t lds = std::max<size_t>((size_t)(p.rows * (units * 128 + 16 + units)), (size_t)waves * 1024);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), (lds + 15) / 16 * 16, s, p);
+    return hipGetLastError();
+}
+
 // Into how many parts along k the work of `blocks` workgroups is cut, at most `most`, where `room` workgroups run at a time: rounds times the length of a
 // part, an eighth of the whole added for what each part costs by itself.
 static int32_t parts_along_k(int64_t blocks, int64_t most, int64_t room)
@@ -163,6 +260,7 @@ struct ForwardRoom {
 static ForwardRoom forward_room(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
     ForwardRoom r{};
+    if (from_floats && once(rows, cols)) return r;
     const int64_t ld = rows8_stride(cols);
     const bool exact = dtype == TICTAC_F32, few = rows <= kFewRows;
     if (few) {
@@ -199,6 +297,7 @@ static auto few_kernel(int64_t rows, int32_t fb)
 
 hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
 {
+    if (p.x && once(p.rows, p.cols)) return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), launch_once, p, s);
     const ForwardRoom room = forward_room(p.dtype, p.x != nullptr, p.rows, p.cols, p.outs);
     const int64_t ld = rows8_stride(p.cols);
     const bool exact = p.dtype == TICTAC_F32, few = p.rows <= kFewRows, wide = exact && !few;
