@@ -1,4 +1,4 @@
-// See k9_product.h.  A step of 128 bytes of k is one matrix instruction of 16 x 16 x 128 for each block of outputs, which takes the scales of its operands' rows too.
+// See k9_product.h.  A step of 128 bytes of k is two matrix instructions of 32 x 32 x 64 for each block of outputs, which take the scales of their operands' rows too.
 // The instruction adds the 128 products with what they exceed about 2^-13 of the largest by (measured: 1.4e-5 of the result's norm for normal values, 5e-5 where values
 // are spread over many powers of two); outputs here have 16 bits, and their own rounding is off by 2^-9 or 2^-12.  float32 outputs take bf16 instructions, whose sums are float32.
 #include "k9_product.h"
@@ -9,21 +9,34 @@
 
 namespace tictac {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
 template <int QF>                       // format of q
 struct OpF8 {
     typedef f32x4 acc;
     typedef float sum;
     static __device__ __forceinline__ float value(float s) { return s; }
-    static __device__ __forceinline__ acc mma(i32x8 a, i32x8 b, acc c, int ea, int eb)
+    // In assembly, so that the compiler neither moves accumulators nor multiplies ahead of a branch.  It does not know that this is a matrix instruction: one that reads a register right
+    // behind a vector instruction that wrote it would be too early (hence the s_nop, which a matrix instruction under way hides), and results take a while (results_settled).
+    static __device__ __forceinline__ void mma(i32x8 a, i32x8 b, f32x16 &c, int ea, int eb)
     {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, TICTAC_E4M3, QF, 0, ea, 0, eb);
+        asm volatile("s_nop 1\n\tv_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] blgp:%5" : "+a"(c) : "v"(a), "v"(b), "v"(ea), "v"(eb), "n"(QF));
     }
 };
 template <int QF>
 struct Biased<OpF8<QF>> { static constexpr bool value = true; };
 
+// what the matrix instructions wrote can be read behind this
+template <int BR, int BC>
+__device__ __forceinline__ void results_settled(f32x16 (&acc)[BR][BC])
+{
+#pragma unroll
+    for (int i = 0; i < BR; ++i)
+#pragma unroll
+        for (int j = 0; j < BC; ++j) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]));
+}
+
 typedef ProductsOf<ProductF8Args> ProductsF8;
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // The loads of the scales of a step: the four bytes that hold it, of TR rows of p and TC of q, 64 rows a load.  A wave makes NS of them, the same number in every wave and at every
 // step, so that loads can be counted; where there are less than that, the last rows come again, to a place that nobody reads.
@@ -59,19 +72,59 @@ struct ScaleLoads {
     }
 };
 
-// A tile of 32 FR x 32 FC outputs by four waves, STAGES buffers in turn.  While a step is multiplied from registers, the operands of the next are read from LDS; then a barrier, before
-// which each wave has waited for its reads and for its loads of the step behind that, and the buffer of the step that was read is asked to take the one STAGES on.
-template <int QF, int OUT, int FR, int FC, int STAGES>
-__global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_f8_kernel(ProductsF8 all)
+// What a wave holds, BR x BC blocks of 32 x 32 from (r, c) on, goes column by column through its own part of LDS, so that a thread has eight consecutive outputs.  Lane l of a block holds
+// rows 8 n + 4 (l / 32) .. + 3, n = 0 .. 3, of column l % 32.
+template <class OP, int OUT, int BR, int BC>
+__device__ __forceinline__ void put_blocks32(const ProductArgs &a, const f32x16 (&acc)[BR][BC], int32_t r, int32_t c, int32_t split, char *room)
+{
+    constexpr int kStride = BR * 32 + 4, kThreads = BR * 4, kColumns = 64 / kThreads;       // words; threads per column; columns at a time
+    const int lane = threadIdx.x & 63, part = lane % kThreads, first = lane / kThreads;
+    f32x4 *const to = (f32x4 *)room + ((lane & 31) * kStride + (lane >> 5) * 4) / 4;
+    const f32x4 *const from = (const f32x4 *)room + (first * kStride + part * 8) / 4;
+    const int32_t mine = r + part * 8;
+    Finish8<false, OUT != kParts> finish;
+    finish.init(a, mine);
+    const bool wide = OUT != kParts && (a.ld_out * (OUT == TICTAC_F32 ? 4 : 2)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
+#pragma unroll
+    for (int j = 0; j < BC; ++j) {
+#pragma unroll
+        for (int i = 0; i < BR; ++i)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) to[i * 8 + n * 2] = f32x4{acc[i][j][4 * n], acc[i][j][4 * n + 1], acc[i][j][4 * n + 2], acc[i][j][4 * n + 3]};
+        wave_sync();
+#pragma unroll
+        for (int k = 0; k < 32 / kColumns; ++k) {
+            const f32x4 lo = from[k * kColumns * kStride / 4], hi = from[k * kColumns * kStride / 4 + 1];
+            const int32_t column = c + j * 32 + k * kColumns + first;
+            if (column >= a.C || mine >= a.R) continue;
+            const float sum[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if constexpr (OUT == kParts) {
+                float *const out = (float *)a.parts + ((int64_t)split * a.C + column) * a.R;
+                if (a.R % 8 == 0) store8<TICTAC_F32, true>(out, mine, a.R, sum);
+                else store8<TICTAC_F32, false>(out, mine, a.R, sum);
+            } else {
+                finish.template store<OUT>(a, mine, column, sum, wide);
+            }
+        }
+        wave_sync();
+    }
+}
+
+// A tile of 64 BR x 64 BC outputs by four waves, STAGES buffers in turn, two workgroups per compute unit where they fit.  A step has two halves of 64 bytes of k, a matrix instruction for each
+// block of 32 x 32; under those of each half the operands of the next are read:
+//   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1;
+//   - half 1 of step t reads the first half of step t + 1 and asks for step t + STAGES, into the buffer of step t.
+template <int QF, int OUT, int BR, int BC, int STAGES>
+__global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_f8_kernel(ProductsF8 all)
 {
     using OP = OpF8<QF>;
-    constexpr int TR = FR * 32, TC = FC * 32;
+    constexpr int TR = BR * 64, TC = BC * 64, kMma = BR * BC, kReads = BR + BC;
     typedef TileLoads<TR, TC, 4, 0> Loads;
     typedef ScaleLoads<TR, TC, 4> Scales;
-    constexpr int kBuffer = (TR + TC) * 128 + Scales::kBytes, kLoads = Loads::LP + Loads::LQ + Scales::NS;
+    constexpr int kBuffer = (TR + TC) * 128 + Scales::kBytes, kOperands = Loads::LP + Loads::LQ, kLoads = kOperands + Scales::NS;
     extern __shared__ char lds[];                                       // [STAGES]{[TR + TC][128], scales}
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if ((int32_t)blockIdx.x >= all.first[2]) {
+    if ((int32_t)blockIdx.x >= all.first[2]) {                          // (a workgroup per tile)
         column_sums(all.sums, blockIdx.x - all.first[2], (float *)lds);
         return;
     }
@@ -85,69 +138,85 @@ __global__ __launch_bounds__(256, STAGES * (FR + FC) > 20 ? 1 : 2) void product_
     Scales scales;
     loads.init(a, r0, c0, first, wave);
     scales.init(a, r0, c0, wave);
-    const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
-    const int lo = (fk ^ swizzle) * 16, hi = ((4 + fk) ^ swizzle) * 16, row_p = wr * FR * 16 + frow, row_q = wc * FC * 16 + frow;
-    f32x4 acc[FR][FC];
+    const int wr = wave & 1, wc = wave >> 1, frow = lane & 31, fk = lane >> 5, swizzle = frow & 7;
+    const int row_p = wr * BR * 32 + frow, row_q = TR + wc * BC * 32 + frow;
+    f32x16 acc[BR][BC];
 #pragma unroll
-    for (int i = 0; i < FR; ++i)
+    for (int i = 0; i < BR; ++i)
 #pragma unroll
-        for (int j = 0; j < FC; ++j) acc[i][j] = f32x4{};
-    struct Operands {
-        i32x8 p[FR], q[FC];
-        int ep[FR], eq[FC];
+        for (int j = 0; j < BC; ++j) acc[i][j] = f32x16{};
+    i32x8 fp[2][BR], fq[2][BC];
+    int ep[2][BR], eq[2][BC];
+    // operand n of a half: columns first
+    const auto read_one = [&](int half, int n, int32_t step, int buffer) {
+        const char *const from = lds + buffer * kBuffer;
+        const int lo = ((half * 4 + fk * 2) ^ swizzle) * 16, hi = ((half * 4 + fk * 2 + 1) ^ swizzle) * 16, row = n < BC ? row_q + n * 32 : row_p + (n - BC) * 32;
+        const i32x4 u = *(const i32x4 *)(from + row * 128 + lo), v = *(const i32x4 *)(from + row * 128 + hi);
+        const i32x8 w{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+        const int e = *(const uint8_t *)(from + (TR + TC) * 128 + row * 4 + (step & 3));
+        if (n < BC) { fq[half][n] = w; eq[half][n] = e; }
+        else { fp[half][n - BC] = w; ep[half][n - BC] = e; }
     };
-    const auto request = [&](int32_t step) {
-        char *to = lds + (step - first) % STAGES * kBuffer;
+    const auto request = [&](int32_t step, char *to) {
         loads.request(a, to, wave);
         scales.request(step, to + (TR + TC) * 128, wave);
     };
-    const auto two = [&](const char *row) {
-        const i32x4 u = *(const i32x4 *)(row + lo), v = *(const i32x4 *)(row + hi);
-        return i32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-    };
-    const auto read = [&](int32_t step, Operands &o) {
-        const char *from = lds + (step - first) % STAGES * kBuffer, *e = from + (TR + TC) * 128 + (step & 3);
-#pragma unroll
-        for (int i = 0; i < FR; ++i) { o.p[i] = two(from + (row_p + i * 16) * 128); o.ep[i] = *(const uint8_t *)(e + (row_p + i * 16) * 4); }
-#pragma unroll
-        for (int j = 0; j < FC; ++j) { o.q[j] = two(from + (TR + row_q + j * 16) * 128); o.eq[j] = *(const uint8_t *)(e + (TR + row_q + j * 16) * 4); }
-    };
-    const auto multiply = [&](const Operands &o) {
-#pragma unroll
-        for (int i = 0; i < FR; ++i)
-#pragma unroll
-            for (int j = 0; j < FC; ++j) acc[i][j] = OP::mma(o.p[i], o.q[j], acc[i][j], o.ep[i], o.eq[j]);
-    };
-    // waits until all but the loads of the last `later` steps that were asked for have arrived, and for the wave's reads
+    // the wait for a step's loads, with `later` steps' behind them under way
     const auto arrived = [&](int32_t later) {
-        if (STAGES > 3 && later >= 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * kLoads) : "memory");
-        else if (STAGES > 2 && later >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kLoads) : "memory");
-        else if (later >= 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
+        if (STAGES > 3 && later >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kLoads) : "memory");
+        else if (STAGES > 2 && later >= 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kLoads) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        asm volatile("" ::: "memory");                                  // (nothing is read before the barrier)
     };
-    Operands now, next;
-    if (first < last) {
-        for (int32_t step = first; step < last && step < first + STAGES; ++step) request(step);
-        arrived(min(last - 1 - first, STAGES - 1));                     // the first step
-        read(first, now);
-        arrived(min(max(last - 2 - first, 0), STAGES - 2));             // the second; nobody reads the first any more
-    }
-    for (int32_t step = first; step < last; ++step) {
-        if (step + STAGES < last) request(step + STAGES);
-        if (step + 1 < last) read(step + 1, next);
-        multiply(now);
-        if (step + 1 < last) {
-            // what was asked for behind step + 2: up to step + STAGES, or to the last
-            arrived(min(max(last - 3 - step, 0), STAGES - 2));
-            now = next;
+    const auto run = [&](int half, int32_t step, int buffer, bool ask, char *to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int m = 0; m < kMma; ++m) {
+            OP::mma(fp[half][m / BC], fq[half][m % BC], acc[m / BC][m % BC], ep[half][m / BC], eq[half][m % BC]);
+#pragma unroll
+            for (int n = m * kReads / kMma; n < (m + 1) * kReads / kMma; ++n) read_one(half ^ 1, n, step, buffer);
+            if (ask)
+#pragma unroll
+                for (int n = m * kOperands / kMma; n < (m + 1) * kOperands / kMma; ++n) loads.request_one(a, to, wave, n);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    };
+    if (first < last) {
+        for (int32_t step = first; step < last && step < first + STAGES; ++step) request(step, lds + (step - first) * kBuffer);
+        const int32_t later = min(last - 1 - first, STAGES - 1);
+        if (STAGES > 3 && later >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kLoads) : "memory");
+        else if (STAGES > 2 && later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        else if (later >= 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < kReads; ++n) read_one(0, n, first, 0);
     }
+    int buffer = 0;
+    int32_t step = first;
+    for (; step + STAGES < last; ++step) {
+        const int next = buffer + 1 < STAGES ? buffer + 1 : 0;
+        char *const to = lds + buffer * kBuffer;
+        run(0, step, buffer, false, nullptr);
+        arrived(STAGES - 2);
+        run(1, step + 1, next, true, to);
+        scales.request(step + STAGES, to + (TR + TC) * 128, wave);
+        loads.next(a);
+        buffer = next;
+    }
+    for (; step < last; ++step) {
+        const int next = buffer + 1 < STAGES ? buffer + 1 : 0;
+        run(0, step, buffer, false, nullptr);
+        arrived(min(last - 2 - step, STAGES - 2));
+        run(1, step + 1, next, false, nullptr);                         // (behind the last step what is read is not used)
+        buffer = next;
+    }
+    results_settled(acc);
     __syncthreads();
-    char *room = lds + wave * 16 * (FR * 16 + 4) * 4;
-    if (a.splits > 1) put_blocks<OP, kParts, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
-    else put_blocks<OP, OUT, FR, FC>(a, acc, r0 + wr * FR * 16, c0 + wc * FC * 16, split, room);
+    char *room = lds + wave * 32 * (BR * 32 + 4) * 4;
+    if (a.splits > 1) put_blocks32<OP, kParts, BR, BC>(a, acc, r0 + wr * BR * 32, c0 + wc * BC * 32, split, room);
+    else put_blocks32<OP, OUT, BR, BC>(a, acc, r0 + wr * BR * 32, c0 + wc * BC * 32, split, room);
 }
 
 // Sixteen-byte pieces of outputs, four of a line of 128 bytes of column n in lane n + 32 g, to whole lines: the lanes of columns n, n + 8, n + 16 and n + 24 exchange them (a square of four by
@@ -241,8 +310,7 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         char *const to = lds + (step & 1) * kBuffer;
 #pragma unroll
         for (int n = 0; n < FR * FC; ++n) {
-            asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] blgp:%5"
-                         : "+a"(acc[n / FC][n % FC]) : "v"(fp[half][n / FC]), "v"(fq[half][n % FC]), "v"(ep[half][n / FC]), "v"(eq[half][n % FC]), "n"(QF));
+            OpF8<QF>::mma(fp[half][n / FC], fq[half][n % FC], acc[n / FC][n % FC], ep[half][n / FC], eq[half][n % FC]);
             if (read && n < FR + FC) read_one(half ^ 1, n, step + half);        // (half 1 reads the next step)
             if (ask) loads.request_one(a, to, wave, n);
             if (ask && n % 8 == 7) scales.request_one(step + 2, to + (TR + TC) * 128, wave, n / 8);
@@ -293,9 +361,7 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         tile += workers;
         const bool more = tile < all.first[2];
         if (more) begin(tile);
-        // the compiler does not know that matrix instructions wrote these, and their results take a while
-#pragma unroll
-        for (int i = 0; i < FR; ++i) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]));
+        results_settled(acc);
         typedef typename Elem<OUT>::type T;
         const bool wide = (a.ld_out * sizeof(T)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
         const bool whole = wide && row0 + TR <= a.R && col0 + TC <= a.C;
@@ -338,7 +404,7 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
 }
 
 struct TileF8 { int32_t r, c; };
-constexpr TileF8 kTilesF8[] = {{4, 4}, {4, 2}, {2, 2}, {8, 8}};
+constexpr TileF8 kTilesF8[] = {{2, 2}, {2, 1}, {1, 1}, {4, 4}};
 constexpr int32_t kLargest = 3;
 
 ProductPlan plan_products_f8(const ProductShape *shapes, int n) { return plan_products(shapes, n); }
@@ -347,7 +413,7 @@ template <int QF, int OUT>
 static hipError_t launch_as(const ProductF8Args *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s)
 {
     ProductsF8 all{};
-    const int32_t tr = 32 * kTilesF8[tile].r, tc = 32 * kTilesF8[tile].c;
+    const int32_t tr = 64 * kTilesF8[tile].r, tc = 64 * kTilesF8[tile].c;
     int32_t blocks = 0;
     for (int i = 0; i < 2; ++i) {
         all.first[i] = blocks;
@@ -371,9 +437,9 @@ static hipError_t launch_as(const ProductF8Args *a, int n, int32_t tile, const C
     blocks += all.sum_blocks;
     const bool alone = blocks <= 256;
     const auto kernel = large       ? product_f8_kernel_256<QF, OUT>
-                        : tile == 0 ? (alone ? product_f8_kernel<QF, OUT, 4, 4, 4> : product_f8_kernel<QF, OUT, 4, 4, 2>)
-                        : tile == 1 ? product_f8_kernel<QF, OUT, 4, 2, 3>
-                                    : product_f8_kernel<QF, OUT, 2, 2, 4>;
+                        : tile == 0 ? (alone ? product_f8_kernel<QF, OUT, 2, 2, 4> : product_f8_kernel<QF, OUT, 2, 2, 2>)
+                        : tile == 1 ? product_f8_kernel<QF, OUT, 2, 1, 3>
+                                    : product_f8_kernel<QF, OUT, 1, 1, 4>;
     const int stages = large ? 2 : tile == 0 ? (alone ? 4 : 2) : tile == 1 ? 3 : 4, scales = ((tr + tc) / 64 + 3) / 4 * 1024;
     const int lds = stages * ((tr + tc) * 128 + scales) + (large ? 1024 : 0);
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
