@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_
 {
     using OP = OpF8<QF>;
     constexpr int TR = BR * 64, TC = BC * 64, kMma = BR * BC, kReads = BR + BC;
-    typedef TileLoads<TR, TC, 4, 0> Loads;
+    typedef TileLoads<TR, TC, 4, 2> Loads;
     typedef ScaleLoads<TR, TC, 4> Scales;
     constexpr int kBuffer = (TR + TC) * 128 + Scales::kBytes, kOperands = Loads::LP + Loads::LQ, kLoads = kOperands + Scales::NS;
     extern __shared__ char lds[];                                       // [STAGES]{[TR + TC][128], scales}
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_
     Scales scales;
     loads.init(a, r0, c0, first, wave);
     scales.init(a, r0, c0, wave);
-    const int wr = wave & 1, wc = wave >> 1, frow = lane & 31, fk = lane >> 5, swizzle = frow & 7;
+    const int wr = wave & 1, wc = wave >> 1, frow = lane & 31, fk = lane >> 5, swizzle = frow >> 1 & 7;
     const int row_p = wr * BR * 32 + frow, row_q = TR + wc * BC * 32 + frow;
     f32x16 acc[BR][BC];
 #pragma unroll
@@ -260,7 +260,7 @@ template <int QF, int OUT>
 __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
 {
     constexpr int TR = 256, TC = 256, FR = 4, FC = 4;
-    typedef TileLoads<TR, TC, 4, 2> Loads;
+    typedef TileLoads<TR, TC, 4, 3> Loads;
     typedef ScaleLoads<TR, TC, 4> Scales;
     constexpr int kBuffer = (TR + TC) * 128 + Scales::kBytes;
     extern __shared__ char lds[];                                       // [2]{[TR + TC][128], scales}, bias
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         return;
     }
     const int wr = wave & 1, wc = wave >> 1, frow = lane & 31, fk = lane >> 5;
-    const int row_p = wr * 128 + (frow >> 2 & 1) * 16 + (frow >> 3) * 4 + (frow & 3), row_q = TR + wc * 128 + frow, swizzle = frow & 7;     // (of both)
+    const int row_p = wr * 128 + (frow >> 2 & 1) * 16 + (frow >> 3) * 4 + (frow & 3), row_q = TR + wc * 128 + frow, swizzle = frow >> 1 & 7;     // (of both)
     Loads loads;
     Scales scales;
     f32x16 acc[FR][FC];
