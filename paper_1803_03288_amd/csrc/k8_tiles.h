@@ -208,9 +208,8 @@ __device__ __forceinline__ void put_lines(T *out, int32_t row, int32_t column, i
     i32x4 a, b;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int32_t mine = first ? hi[e] : lo[e], other = __builtin_amdgcn_update_dpp(0, mine, 0x128, 0xf, 0xf, true);     // row_ror:8
-        a[e] = first ? lo[e] : other;
-        b[e] = first ? other : hi[e];
+        a[e] = __builtin_amdgcn_update_dpp(lo[e], hi[e], 0x128, 0xf, 0xc, false);       // row_ror:8, to columns n + 8
+        b[e] = __builtin_amdgcn_update_dpp(hi[e], lo[e], 0x128, 0xf, 0x3, false);       // to columns n
     }
     i32x4 *const to = (i32x4 *)(out + (int64_t)(first ? column : column - 8) * ld + row + (first ? 0 : STEP)), *const next = (i32x4 *)((T *)to + 8 * ld);
     __builtin_nontemporal_store(a, to);

@@ -219,50 +219,22 @@ __global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_
     else put_blocks32<OP, OUT, BR, BC>(a, acc, r0 + wr * BR * 32, c0 + wc * BC * 32, split, room);
 }
 
-// Sixteen-byte pieces of outputs, four of a line of 128 bytes of column n in lane n + 32 g, to whole lines: the lanes of columns n, n + 8, n + 16 and n + 24 exchange them (a square of four by
-// four is turned round), so that each of four stores brings eight lanes' 128 bytes of eight columns.
-template <typename T>
-__device__ __forceinline__ void put_lines32(T *line, int64_t ld, i32x4 (&piece)[4])
-{
-    const int lane = threadIdx.x & 63;
-    const bool first = (lane & 8) == 0;
-    i32x4 out[2][2];                    // [column + 16 ..][+ 8 ..]
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const auto r = __builtin_amdgcn_permlane16_swap((uint32_t)piece[k][e], (uint32_t)piece[k + 2][e], false, false);
-            piece[k][e] = (int32_t)r[0];
-            piece[k + 2][e] = (int32_t)r[1];
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int32_t lo = piece[2 * h][e], hi = piece[2 * h + 1][e], other = __builtin_amdgcn_update_dpp(0, first ? hi : lo, 0x128, 0xf, 0xf, true);       // row_ror:8
-            out[h][0][e] = first ? lo : other;
-            out[h][1][e] = first ? other : hi;
-        }
-    }
-    T *const to = line + (int64_t)(lane & 7) * ld + (lane & 16) * 2 + (lane >> 5) * 16 + (lane & 8);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) __builtin_nontemporal_store(out[h][k], (i32x4 *)(to + (int64_t)(h * 16 + k * 8) * ld));
-}
-
-// Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each: 4 x 4 blocks of 32 x 32, whose matrix instruction takes half a step (64 bytes of k).  A step has two halves of
-// sixteen of them; under each half the operands of the next are read:
-//   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1;
-//   - half 1 of step t reads the first half of step t + 1 and asks for step t + 2, into the buffer of step t.
-// The accumulators fill the 256 accumulation registers, hence the matrix instructions in assembly.  (Blocks of 16 x 16 take a whole step at once: operands of two steps do not
-// fit beside them.)  One workgroup per compute unit goes from tile to tile, and the first two steps of the next tile are asked for before this one's outputs are formed.
-// Row m of a block of rows of p is row 16 (m / 4 % 2) + 4 (m / 8) + m % 4 of 32, so that a lane has sixteen outputs next to each other.
+// Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each: 8 x 8 blocks of 16 x 16, whose matrix instruction takes a whole step.  (Blocks of 32 x 32 take half a step each, and
+// 5 to 7 % more power for the same values, by which large products are bound: 8192 x 4096 -> 16384 492 us.)  The accumulators fill the 256 accumulation registers, the operands of one step
+// half of the others; the next step's go to the same registers, as they become free:
+//   - the first half of step t multiplies rows 0-3 of the blocks by all columns, and reads rows 4-7; then a barrier, before which each wave has waited for its reads and for its loads of
+//     step t + 1: nobody reads the buffer of step t any more;
+//   - the second half multiplies rows 4-7, column by column, and reads rows 0-3 of step t + 1 and, behind each column, that column of step t + 1, while loads of step t + 2 go to the
+//     buffer of step t.
+// One workgroup per compute unit goes from tile to tile, and the first two steps of the next tile are asked for before this one's outputs are formed.  Rows of p lie in the order that gives a
+// lane eight outputs next to each other, as in product_kernel_256.
 template <int QF, int OUT>
 __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
 {
-    constexpr int TR = 256, TC = 256, FR = 4, FC = 4;
-    typedef TileLoads<TR, TC, 4, 3> Loads;
+    constexpr int TR = 256, TC = 256, FR = 8, FC = 8;
+    typedef TileLoads<TR, TC, 4, 1> Loads;
     typedef ScaleLoads<TR, TC, 4> Scales;
-    constexpr int kBuffer = (TR + TC) * 128 + Scales::kBytes;
+    constexpr int kScales = (TR + TC) * 128, kBuffer = kScales + Scales::kBytes;
     extern __shared__ char lds[];                                       // [2]{[TR + TC][128], scales}, bias
     float *const biases = (float *)(lds + 2 * kBuffer);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -271,15 +243,16 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         column_sums(all.sums, blockIdx.x - workers, (float *)lds);
         return;
     }
-    const int wr = wave & 1, wc = wave >> 1, frow = lane & 31, fk = lane >> 5;
-    const int row_p = wr * 128 + (frow >> 2 & 1) * 16 + (frow >> 3) * 4 + (frow & 3), row_q = TR + wc * 128 + frow, swizzle = frow >> 1 & 7;     // (of both)
+    const int wr = wave & 1, wc = wave >> 1, frow = lane & 15, fk = lane >> 4, swizzle = frow & 7;
+    const int row_p = wr * FR * 16 + (frow >> 2) * 8 + (frow & 3), row_q = TR + wc * FC * 16 + frow, lo = (fk ^ swizzle) * 16, hi = ((4 + fk) ^ swizzle) * 16;
     Loads loads;
     Scales scales;
-    f32x16 acc[FR][FC];
-    i32x8 fp[2][FR], fq[2][FC];
-    int ep[2][FR], eq[2][FC];
+    f32x4 acc[FR][FC];
+    i32x8 p[FR], q[FC];
+    int ep[FR], eq[FC];
     int32_t r0, c0, which;
-    const auto begin = [&](int32_t tile) {
+    float bias;                                                         // of row r0 + the thread's number
+    const auto begin = [&](int32_t tile) __attribute__((always_inline)) {
         which = tile >= all.first[1];
         const ProductF8Args &a = all.a[which];
         int32_t split, tr, tc;
@@ -289,117 +262,155 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         loads.init(a, r0, c0, 0, wave);
         scales.init(a, r0, c0, wave);
         loads.request(a, lds, wave);
-        scales.request(0, lds + (TR + TC) * 128, wave);
+        scales.request(0, lds + kScales, wave);
         if (a.steps > 1) {
             loads.request(a, lds + kBuffer, wave);
-            scales.request(1, lds + kBuffer + (TR + TC) * 128, wave);
+            scales.request(1, lds + kBuffer + kScales, wave);
         }
+        bias = a.bias && r0 + (int32_t)threadIdx.x < a.R ? param(a.bias, a.bias_dtype, r0 + (int32_t)threadIdx.x) : 0.0f;
     };
-    // operand n of a half: columns first
-    const auto read_one = [&](int half, int n, int32_t step) {
-        const char *const from = lds + (step & 1) * kBuffer;
-        const int lo = ((half * 4 + fk * 2) ^ swizzle) * 16, hi = ((half * 4 + fk * 2 + 1) ^ swizzle) * 16, row = n < FC ? row_q + n * 32 : row_p + (n - FC) * 32;
-        const i32x4 u = *(const i32x4 *)(from + row * 128 + lo), v = *(const i32x4 *)(from + row * 128 + hi);
-        const i32x8 w{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-        const int e = *(const uint8_t *)(from + (TR + TC) * 128 + row * 4 + (step & 3));
-        if (n < FC) { fq[half][n] = w; eq[half][n] = e; }
-        else { fp[half][n - FC] = w; ep[half][n - FC] = e; }
+    // Where a lane's reads of a step begin, in bytes of LDS: blocks lie at constant distances from there.
+    typedef const __attribute__((address_space(3))) char *At;
+    struct Places {
+        At lo, hi, e;
     };
-    // One half of a step: its sixteen matrix instructions, behind the first eight of them an operand of the next half is read, and in half 1 loads of a later step are asked for
-    const auto run = [&](const ProductF8Args &a, int half, int32_t step, bool read, bool ask) {
-        char *const to = lds + (step & 1) * kBuffer;
-#pragma unroll
-        for (int n = 0; n < FR * FC; ++n) {
-            OpF8<QF>::mma(fp[half][n / FC], fq[half][n % FC], acc[n / FC][n % FC], ep[half][n / FC], eq[half][n % FC]);
-            if (read && n < FR + FC) read_one(half ^ 1, n, step + half);        // (half 1 reads the next step)
-            if (ask) loads.request_one(a, to, wave, n);
-            if (ask && n % 8 == 7) scales.request_one(step + 2, to + (TR + TC) * 128, wave, n / 8);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (ask) loads.next(a);
+    const auto places = [&](int32_t step, int row) __attribute__((always_inline)) {
+        const At from = (At)lds + (step & 1) * kBuffer;
+        Places at{from + (row * 128 + lo), from + (row * 128 + hi), from + (kScales + (step & 3) + row * 4)};
+        asm("" : "+v"(at.lo), "+v"(at.hi), "+v"(at.e));                 // (what is added to them stays an offset of the reads)
+        return at;
+    };
+    const auto operand = [&](const Places &at, int row, i32x8 &to, int &e) __attribute__((always_inline)) {
+        typedef const __attribute__((address_space(3))) i32x4 *Quad;
+        const i32x4 u = *(Quad)(at.lo + row * 128), v = *(Quad)(at.hi + row * 128);
+        to = i32x8{u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+        e = *(const __attribute__((address_space(3))) uint8_t *)(at.e + row * 4);
+    };
+    const auto read_p = [&](const Places &at, int i) __attribute__((always_inline)) { operand(at, (i >> 1) * 32 + (i & 1) * 4, p[i], ep[i]); };
+    const auto read_q = [&](const Places &at, int j) __attribute__((always_inline)) { operand(at, j * 16, q[j], eq[j]); };
+    const auto mma = [&](int i, int j) __attribute__((always_inline)) {
+        asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] blgp:%5" : "+a"(acc[i][j]) : "v"(p[i]), "v"(q[j]), "v"(ep[i]), "v"(eq[j]), "n"(QF));
     };
     const auto barrier = [] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");                                  // (nothing is read before the barrier)
     };
+    // the loads of step + 2, two behind each column from kFirst on of the first half
+    constexpr int kFirst = 5;
+    const auto request_two = [&](const ProductF8Args &a, int32_t step, int k) __attribute__((always_inline)) {
+        char *const to = lds + (step & 1) * kBuffer;
+        if (k < 8) {
+            loads.request_one(a, to, wave, 2 * k);
+            loads.request_one(a, to, wave, 2 * k + 1);
+        } else if (k == 8) {
+            scales.request_one(step + 2, to + kScales, wave, 0);
+            scales.request_one(step + 2, to + kScales, wave, 1);
+            loads.next(a);
+        }
+    };
+    // the halves of a step
+    const auto first_half = [&](const ProductF8Args &a, int32_t step, bool ask) __attribute__((always_inline)) {
+        const Places at_p = places(step, row_p);
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma(i, j);
+            if (j < 4) read_p(at_p, 4 + j);
+            if (j == kFirst - 1 && ask) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                barrier();
+            }
+            if (j >= kFirst && ask) request_two(a, step, j - kFirst);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ask) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (FC - kFirst)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        barrier();
+    };
+    const auto second_half = [&](const ProductF8Args &a, int32_t step, bool read, bool ask) __attribute__((always_inline)) {
+        const Places at_p = places(step + 1, row_p), at_q = places(step + 1, row_q);
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mma(4 + i, j);
+            if (read) read_q(at_q, j);
+            if (read && j < 4) read_p(at_p, j);
+            if (ask) request_two(a, step, j + FC - kFirst);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     int32_t tile = blockIdx.x, after = 0;                               // after: stores that surely were issued behind the loads under way
     begin(tile);
     while (true) {
         const ProductF8Args &a = all.a[which];
-        const int32_t steps = a.steps, row0 = r0, col0 = c0, t = threadIdx.x;
-        float bias = 0.0f;
-        if (a.bias && row0 + t < a.R) bias = param(a.bias, a.bias_dtype, row0 + t);
-#pragma unroll
-        for (int i = 0; i < FR; ++i)
-#pragma unroll
-            for (int j = 0; j < FC; ++j) acc[i][j] = f32x16{};
+        const int32_t steps = a.steps, row0 = r0, col0 = c0, r = wr * FR * 16 + fk * 8, c = wc * FC * 16 + frow;
         // (of what was issued behind the loads, the stores of the tile before may go on)
-        if (after >= 32) asm volatile("s_waitcnt vmcnt(32)" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        biases[threadIdx.x] = bias;
+        if (after >= 32) asm volatile("s_waitcnt vmcnt(32) lgkmcnt(0)" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         barrier();
+        // sums begin with the bias
 #pragma unroll
-        for (int n = 0; n < FR + FC; ++n) read_one(0, n, 0);
-        const auto meet = [&] {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            barrier();
-        };
+        for (int i = 0; i < FR; ++i) {
+            const f32x4 b = *(const f32x4 *)(biases + r + (i >> 1) * 32 + (i & 1) * 4);
+#pragma unroll
+            for (int j = 0; j < FC; ++j) acc[i][j] = b;
+        }
+        {
+            const Places at_p = places(0, row_p), at_q = places(0, row_q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) read_p(at_p, i);
+#pragma unroll
+            for (int j = 0; j < FC; ++j) read_q(at_q, j);
+        }
         int32_t step = 0;
         for (; step + 2 < steps; ++step) {
-            run(a, 0, step, true, false);
-            meet();
-            run(a, 1, step, true, true);
+            first_half(a, step, true);
+            second_half(a, step, true, true);
         }
         for (; step < steps; ++step) {
-            run(a, 0, step, true, false);
-            meet();
-            run(a, 1, step, step + 1 < steps, false);
+            first_half(a, step, false);
+            second_half(a, step, true, false);                          // (behind the last step what is read is not used)
         }
-        // (the last reads of a step lie before its barrier: LDS is free)
-        biases[t] = bias;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        barrier();
+        // (what the last step needed was read before its last barrier: LDS is free)
         tile += workers;
         const bool more = tile < all.first[2];
         if (more) begin(tile);
-        results_settled(acc);
+        // the compiler does not know that matrix instructions wrote these, and their results take a while
+#pragma unroll
+        for (int i = 0; i < FR; ++i)
+            asm volatile("s_nop 15" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]), "+a"(acc[i][4]), "+a"(acc[i][5]), "+a"(acc[i][6]), "+a"(acc[i][7]));
         typedef typename Elem<OUT>::type T;
         const bool wide = (a.ld_out * sizeof(T)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
         const bool whole = wide && row0 + TR <= a.R && col0 + TC <= a.C;
         T *const out = (T *)a.out;
 #pragma unroll
-        for (int line = 0; line < 2; ++line) {
-            float b[2][16];
+        for (int j = 0; j < FC; ++j) {
+            const int32_t column = col0 + c + j * 16;
+            if (whole) {
+                i32x4 piece[FR / 2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const f32x4 v = *(const f32x4 *)(biases + wr * 128 + line * 64 + h * 32 + fk * 16 + k * 4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) b[h][k * 4 + e] = v[e];
-                }
-#pragma unroll
-            for (int j = 0; j < FC; ++j) {
-                i32x4 piece[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int i = 0; i < FR / 2; ++i) {
                     float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = acc[line * 2 + (k >> 1)][j][(k & 1) * 8 + e] + b[k >> 1][(k & 1) * 8 + e];
-                    if (whole) {
-                        piece[k] = __builtin_bit_cast(i32x4, Elem<OUT>::pack(v));
-                        continue;
-                    }
-                    const int32_t row = row0 + wr * 128 + line * 64 + (k >> 1) * 32 + fk * 16 + (k & 1) * 8, column = col0 + wc * 128 + j * 32 + frow;
-                    if (column >= a.C) continue;
-                    if (wide) store8<OUT, true>(out + (int64_t)column * a.ld_out, row, a.R, v);
-                    else store8<OUT, false>(out + (int64_t)column * a.ld_out, row, a.R, v);
+                    for (int e = 0; e < 8; ++e) v[e] = acc[2 * i + (e >> 2)][j][e & 3];
+                    piece[i] = __builtin_bit_cast(i32x4, Elem<OUT>::pack(v));
                 }
-                if (whole) put_lines32(out + (int64_t)(col0 + wc * 128 + j * 32) * a.ld_out + row0 + wr * 128 + line * 64, a.ld_out, piece);
+#pragma unroll
+                for (int i = 0; i < FR / 2; i += 2) put_lines<32>(out, row0 + r + i * 32, column, a.ld_out, piece[i], piece[i + 1]);
+            } else if (column < a.C) {
+#pragma unroll
+                for (int i = 0; i < FR / 2; ++i) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[2 * i + (e >> 2)][j][e & 3];
+                    if (wide) store8<OUT, true>(out + (int64_t)column * a.ld_out, row0 + r + i * 32, a.R, v);
+                    else store8<OUT, false>(out + (int64_t)column * a.ld_out, row0 + r + i * 32, a.R, v);
+                }
             }
         }
         if (!more) return;
         after = whole ? 32 : 0;
-        barrier();                                                      // (the biases are read before the next tile's are written)
     }
 }
 
