@@ -189,7 +189,7 @@ try {
 
 int tictac_adamw_step(int32_t n, const tictac_adamw_tensor *tensors, const tictac_adamw_options *options, tictac_stream stream)
 try {
-    if (n < 0) { set_error("n = %d", n); return TICTAC_ERR_UNSUPPORTED; }
+    if (n < 0 || n >= 1 << 24) { set_error("n = %d", n); return TICTAC_ERR_UNSUPPORTED; }
     if ((n && !tensors) || !options) { set_error("tensors or options is NULL"); return TICTAC_ERR_NULL; }
     const tictac_adamw_options &o = *options;
     const auto number = [](double v) { return fabs(v) < INFINITY; };
