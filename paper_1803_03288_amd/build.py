@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import glob
 import os
+import re
 import subprocess
 import sys
 
@@ -145,17 +146,26 @@ def check_counted_waits(asm: str) -> list:
     return bad
 
 
-# The matrix instructions of the largest tiles are written in asm, in place, so that their 256 accumulators stay where they are; the compiler does not know
-# how long their results take, so it must not move an accumulator beside them.
+# The matrix instructions of these kernels are written in asm, in place, so that their accumulators stay where they are; the compiler does not know
+# how long their results take, so it must not move an accumulator beside them, and that they need what a vector instruction wrote two instructions earlier.
 ACCUMULATORS = "18product_kernel_256"
+ACCUMULATORS_F8 = ("21product_f8_kernel_256", "17product_f8_kernelI")
 
 
-def check_accumulators(asm: str) -> list:
-    """Violations (strings) in the device assembly of k8_product.hip: an accumulator read, written or moved in a stretch of code without labels
+def _registers(operands: str) -> set:
+    """The vector and accumulation registers that a list of operands names."""
+    found = set()
+    for kind, first, last, one in re.findall(r"\b([av])(?:\[(\d+):(\d+)\]|(\d+))", operands):
+        found.update((kind, n) for n in range(int(first or one), int(last or one) + 1))
+    return found
+
+
+def check_accumulators(asm: str, kernel: str = ACCUMULATORS) -> list:
+    """Violations (strings) in the device assembly of a source of products: an accumulator read, written or moved in a stretch of code without labels
     that holds matrix instructions, or read before the wait that follows them, and registers that spill; [] when it is sound."""
     bad, seen = [], 0
     for name, lines in _functions(asm):
-        if ACCUMULATORS not in name:
+        if kernel not in name:
             continue
         seen += 1
         multiplies = moves = waited = spilled = early = mixed = 0
@@ -172,6 +182,9 @@ def check_accumulators(asm: str) -> list:
             elif t.startswith("v_accvgpr"):
                 moves += 1
                 early += t.startswith("v_accvgpr_read") and not waited
+            elif t.startswith(("ds_write", "global_store")) and any(kind == "a" for kind, _ in _registers(t.split(";")[0])):
+                moves += 1
+                early += not waited
             elif t.startswith("scratch_"):
                 spilled += 1
         if mixed:
@@ -181,8 +194,56 @@ def check_accumulators(asm: str) -> list:
         if spilled:
             bad.append(f"{name}: register spills (scratch instructions)")
     if not seen:
-        bad.append(f"no kernel {ACCUMULATORS} found")
+        bad.append(f"no kernel {kernel} found")
     return bad
+
+
+def check_operands(asm: str, kernel: str) -> list:
+    """Violations (strings) in the device assembly of a source of products: a matrix instruction that reads a register which one of the two instructions
+    before it wrote, along the text and along every branch (an "s_nop N" counts N + 1); [] when it is sound."""
+    bad = []
+    for name, lines in _functions(asm):
+        if kernel not in name:
+            continue
+        code, at = [], {}                       # (mnemonic, operands); label: the instruction behind it
+        for line in lines:
+            t = line.split(";")[0].strip()
+            if t.startswith(".") and t.split()[0].endswith(":"):
+                at[t.split()[0][:-1]] = len(code)
+            elif t and not t.startswith("."):
+                op, _, rest = t.partition(" ")
+                code.append((op, rest.strip()))
+
+        def written(i):
+            op, rest = code[i]
+            return _registers(rest.split(",")[0]) if op.startswith("v_") and not op.startswith(("v_mfma", "v_cmp")) else set()
+
+        def short(i, reads, waits, came):
+            """whether, going back from in front of instruction i, one of `reads` was written less than `waits` instructions ago"""
+            while waits > 0:
+                for j in came.get(i, ()):
+                    if short(j + 1, reads, waits, {}):
+                        return True
+                i -= 1
+                if i < 0 or code[i][0] in ("s_branch", "s_endpgm", "s_setpc_b64"):
+                    return False
+                if written(i) & reads:
+                    return True
+                waits -= int(code[i][1]) + 1 if code[i][0] == "s_nop" else 1
+            return False
+
+        came = {}
+        for j, (op, rest) in enumerate(code):
+            if op.startswith(("s_cbranch", "s_branch")) and rest in at:
+                came.setdefault(at[rest], []).append(j)
+        for i, (op, rest) in enumerate(code):
+            if op.startswith("v_mfma") and short(i, _registers(rest.split(",", 1)[1]), 2, came):
+                bad.append(f"{name}: {op} {rest} reads what was written right before it")
+    return bad
+
+
+def check_products_f8(asm: str) -> list:
+    return [x for kernel in ACCUMULATORS_F8 for check in (check_accumulators, check_operands) for x in check(asm, kernel)]
 
 
 def device_assembly(source: str) -> str:
@@ -211,7 +272,8 @@ def build(verbose: bool = False) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    for source, check in (("k1_propagate.hip", check_counted_waits), ("k8_product.hip", check_accumulators)):
+    for source, check in (("k1_propagate.hip", check_counted_waits), ("k8_product.hip", check_accumulators),
+                          ("k9_product.hip", check_products_f8)):
         bad = check(device_assembly(os.path.join(CSRC, source)))
         if bad:
             os.remove(LIB)

@@ -291,6 +291,13 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
     const auto mma = [&](int i, int j) __attribute__((always_inline)) {
         asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0] blgp:%5" : "+a"(acc[i][j]) : "v"(p[i]), "v"(q[j]), "v"(ep[i]), "v"(eq[j]), "n"(QF));
     };
+    // what the matrix instructions wrote can be read, or moved, behind this: the compiler does not know that they wrote it, and that it takes a while
+    const auto settled = [&]() __attribute__((always_inline)) {
+        asm volatile("s_nop 15");
+#pragma unroll
+        for (int i = 0; i < FR; ++i)
+            asm volatile("" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]), "+a"(acc[i][4]), "+a"(acc[i][5]), "+a"(acc[i][6]), "+a"(acc[i][7]));
+    };
     const auto barrier = [] {
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");                                  // (nothing is read before the barrier)
@@ -364,9 +371,12 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
             for (int j = 0; j < FC; ++j) read_q(at_q, j);
         }
         int32_t step = 0;
-        for (; step + 2 < steps; ++step) {
-            first_half(a, step, true);
-            second_half(a, step, true, true);
+        if (steps > 2) {
+            do {
+                first_half(a, step, true);
+                second_half(a, step, true, true);
+            } while (++step + 2 < steps);
+            settled();                                                  // (between the loops some move to other registers)
         }
         for (; step < steps; ++step) {
             first_half(a, step, false);
@@ -376,10 +386,7 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
         tile += workers;
         const bool more = tile < all.first[2];
         if (more) begin(tile);
-        // the compiler does not know that matrix instructions wrote these, and their results take a while
-#pragma unroll
-        for (int i = 0; i < FR; ++i)
-            asm volatile("s_nop 15" : "+a"(acc[i][0]), "+a"(acc[i][1]), "+a"(acc[i][2]), "+a"(acc[i][3]), "+a"(acc[i][4]), "+a"(acc[i][5]), "+a"(acc[i][6]), "+a"(acc[i][7]));
+        settled();
         typedef typename Elem<OUT>::type T;
         const bool wide = (a.ld_out * sizeof(T)) % 16 == 0 && ((uintptr_t)a.out & 15) == 0 && a.R % 8 == 0;
         const bool whole = wide && row0 + TR <= a.R && col0 + TC <= a.C;
