@@ -86,7 +86,7 @@ struct F8Rows {
     int32_t format, shift;
 };
 
-inline int64_t f8_blocks(int64_t n) { return (n + kF8Block - 1) / kF8Block; }
+__host__ __device__ inline int64_t f8_blocks(int64_t n) { return (n + kF8Block - 1) / kF8Block; }
 inline int64_t f8_scale_stride(int64_t cols) { return (f8_blocks(cols) + 3) / 4 * 4; }
 
 // ---- k9_blocks.hip ----
@@ -96,14 +96,15 @@ struct F8QuantizeArgs {
     const void *x;                      // to 8 bits
     void *out;                          // and back
     int64_t ld_x;
-    uint8_t *q;                         // NULL (blocks of one row): the values that 8 bits keep go to `wide`
+    uint8_t *q;
     int64_t ld_q;
     uint8_t *scale;
     int64_t ld_scale;
-    uint16_t *wide;                     // bf16 [rows][ld_q]
 };
 hipError_t launch_quantize_f8(const F8QuantizeArgs &a, hipStream_t s);
 hipError_t launch_dequantize_f8(const F8QuantizeArgs &a, hipStream_t s);
+// x (of float32, or where x.x is NULL of 8-bit floats) and w as bf16, [rows][padded], to `out`: ld_q of an x of float32; else cols is ld_x, the padded width
+hipError_t launch_widen_f8(const F8QuantizeArgs &x, const F8QuantizeArgs &w, hipStream_t s);
 
 // The operands of a backward pass: k contiguous and padded with zeros to whole blocks of 128; 8-bit floats with their scales, or where the gradients are float32 the values
 // as bf16.  `dy` in blocks of its columns and (turned round) of its rows, x and w turned round.

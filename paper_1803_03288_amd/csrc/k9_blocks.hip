@@ -1,4 +1,6 @@
 // Rounding to 8-bit floats in blocks (f8.h), back, and the operands of a backward pass.
+#include <algorithm>
+
 #include "device_utils.h"
 #include "f8.h"
 
@@ -14,12 +16,13 @@ __device__ __forceinline__ void put_scale(uint8_t *row, int64_t at, int64_t bloc
     if (lane == 0 || (lane < 4 && at == blocks - 1 && at + lane < (blocks + 3) / 4 * 4)) row[at + lane] = lane ? (uint8_t)0 : (uint8_t)scale;
 }
 
-template <int DT, bool WIDE, int FORMAT>
-__global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int64_t blocks, int64_t total)
+// The blocks of one row that workgroup `group` of `groups` has.  BF16: the values that 8 bits keep, as bf16.
+template <int DT, bool WIDE, int FORMAT, bool BF16>
+__device__ __forceinline__ void quantize_blocks(const F8QuantizeArgs &p, int64_t blocks, int64_t total, uint32_t group, uint32_t groups)
 {
     using E = Elem<DT>;
     const int lane = threadIdx.x & 15;
-    const int64_t first = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 16, step = (int64_t)gridDim.x * 16;
+    const int64_t first = ((int64_t)group * 256 + threadIdx.x) / 16, step = (int64_t)groups * 16;
     for (int64_t at = first; at < total; at += kTurns * step) {
         typename E::raw raw[kTurns];
         int64_t row[kTurns], col[kTurns];
@@ -41,15 +44,21 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int6
             for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[i]));
             const uint32_t scale = f8_scale(row16_max(m), FORMAT);
             const uint2 q = f8_quantized8<FORMAT>(v, scale, f8_nans(p.cols - col[k]));      // (also the zeros behind the end)
-            if (p.wide) {
+            if constexpr (BF16) {
                 f8_values8(q, scale, FORMAT, v);
-                *(i32x4 *)(p.wide + row[k] * p.ld_q + col[k]) = f8_bf16(v);
-                continue;
+                *(i32x4 *)((uint16_t *)p.out + row[k] * p.ld_q + col[k]) = f8_bf16(v);
+            } else {
+                *(uint2 *)(p.q + row[k] * p.ld_q + col[k]) = q;
+                put_scale(p.scale + row[k] * p.ld_scale, col[k] >> 7, blocks, lane, scale);
             }
-            *(uint2 *)(p.q + row[k] * p.ld_q + col[k]) = q;
-            put_scale(p.scale + row[k] * p.ld_scale, col[k] >> 7, blocks, lane, scale);
         }
     }
+}
+
+template <int DT, bool WIDE, int FORMAT>
+__global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int64_t blocks, int64_t total)
+{
+    quantize_blocks<DT, WIDE, FORMAT, false>(p, blocks, total, blockIdx.x, gridDim.x);
 }
 
 // The tile that a workgroup of 256 has: thread t has rows 8 (t / 16) .. + 7 and columns 8 (t % 16) .. + 7 of 128 x 128.
@@ -116,9 +125,9 @@ __global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p
 
 // Back: eight values a thread.
 template <int DT, bool WIDE>
-__global__ __launch_bounds__(256) void dequantize_f8_kernel(F8QuantizeArgs p, int64_t chunks, int64_t total)
+__device__ __forceinline__ void dequantize_chunks(const F8QuantizeArgs &p, int64_t chunks, int64_t total, uint32_t group, uint32_t groups)
 {
-    const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+    const int64_t first = (int64_t)group * 256 + threadIdx.x, step = (int64_t)groups * 256;
     const int shift = p.block == 1 ? 0 : 7;
     for (int64_t at = first; at < total; at += kTurns * step) {
         uint2 q[kTurns];
@@ -143,7 +152,35 @@ __global__ __launch_bounds__(256) void dequantize_f8_kernel(F8QuantizeArgs p, in
     }
 }
 
-static unsigned blocks_of(int64_t n) { return (unsigned)(n < 1 ? 1 : n > 256 * 16 ? 256 * 16 : n); }
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(256) void dequantize_f8_kernel(F8QuantizeArgs p, int64_t chunks, int64_t total)
+{
+    dequantize_chunks<DT, WIDE>(p, chunks, total, blockIdx.x, gridDim.x);
+}
+
+// The operands of a product in float32 as bf16, in one launch: x of floats (rounded to e4m3) or of 8-bit floats, and w.  (333 x 1001 -> 777: 13.7 us; in two launches with a quarter
+// of the workgroups 17.9, in one with so few 16.6.)
+template <bool FLOATS, bool WIDE>
+__global__ __launch_bounds__(256) void widen_f8_kernel(F8QuantizeArgs x, F8QuantizeArgs w, uint32_t x_groups)
+{
+    if (blockIdx.x >= x_groups) {
+        const int64_t chunks = w.cols / 8;
+        dequantize_chunks<TICTAC_BF16, true>(w, chunks, chunks * w.rows, blockIdx.x - x_groups, gridDim.x - x_groups);
+    } else if constexpr (FLOATS) {
+        const int64_t blocks = f8_blocks(x.cols);
+        quantize_blocks<TICTAC_F32, WIDE, TICTAC_E4M3, true>(x, blocks, blocks * x.rows, blockIdx.x, x_groups);
+    } else {
+        const int64_t chunks = x.cols / 8;
+        dequantize_chunks<TICTAC_BF16, true>(x, chunks, chunks * x.rows, blockIdx.x, x_groups);
+    }
+}
+
+// Workgroups for `n` times what one has at once: a turn each while few of them run, then kTurns, then more turns for all.  (333 x 1001: a turn each 4.4 us, four 7.6.)
+static unsigned groups_of(int64_t n)
+{
+    constexpr int64_t kFew = 1024, kMost = 256 * 16;
+    return (unsigned)std::min(kMost, std::max<int64_t>({1, (n + kTurns - 1) / kTurns, std::min(n, kFew)}));
+}
 
 template <int DT, bool WIDE>
 static hipError_t quantize(const F8QuantizeArgs &p, hipStream_t s)
@@ -153,7 +190,7 @@ static hipError_t quantize(const F8QuantizeArgs &p, hipStream_t s)
     if (p.block == 1) {
         const int64_t total = blocks * p.rows;
         const auto kernel = e5 ? quantize_f8_kernel<DT, WIDE, TICTAC_E5M2> : quantize_f8_kernel<DT, WIDE, TICTAC_E4M3>;
-        hipLaunchKernelGGL(kernel, dim3(blocks_of((total + 16 * kTurns - 1) / (16 * kTurns))), dim3(256), 0, s, p, blocks, total);
+        hipLaunchKernelGGL(kernel, dim3(groups_of((total + 15) / 16)), dim3(256), 0, s, p, blocks, total);
     } else {
         const auto kernel = e5 ? quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E5M2> : quantize_f8_tiles_kernel<DT, WIDE, TICTAC_E4M3>;
         hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks * f8_blocks(p.rows))), dim3(256), 0, s, p, (uint32_t)blocks);
@@ -165,7 +202,7 @@ template <int DT, bool WIDE>
 static hipError_t dequantize(const F8QuantizeArgs &p, hipStream_t s)
 {
     const int64_t chunks = (p.cols + 7) / 8, total = chunks * p.rows;
-    hipLaunchKernelGGL((dequantize_f8_kernel<DT, WIDE>), dim3(blocks_of((total + 256 * kTurns - 1) / (256 * kTurns))), dim3(256), 0, s, p, chunks, total);
+    hipLaunchKernelGGL((dequantize_f8_kernel<DT, WIDE>), dim3(groups_of((total + 255) / 256)), dim3(256), 0, s, p, chunks, total);
     return hipGetLastError();
 }
 
@@ -174,6 +211,14 @@ hipError_t launch_quantize_f8(const F8QuantizeArgs &p, hipStream_t s)
     return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), quantize, p, s);
 }
 hipError_t launch_dequantize_f8(const F8QuantizeArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.out, p.dtype, p.ld_x, p.cols), dequantize, p, s); }
+
+hipError_t launch_widen_f8(const F8QuantizeArgs &x, const F8QuantizeArgs &w, hipStream_t s)
+{
+    const unsigned x_groups = groups_of(x.x ? (f8_blocks(x.cols) * x.rows + 15) / 16 : (x.cols / 8 * x.rows + 255) / 256), w_groups = groups_of((w.cols / 8 * w.rows + 255) / 256);
+    const auto kernel = !x.x ? widen_f8_kernel<false, true> : wide_rows(x.x, TICTAC_F32, x.ld_x, x.cols) ? widen_f8_kernel<true, true> : widen_f8_kernel<true, false>;
+    hipLaunchKernelGGL(kernel, dim3(x_groups + w_groups), dim3(256), 0, s, x, w, x_groups);
+    return hipGetLastError();
+}
 
 // ---- the operands of a backward pass ----
 // A workgroup has a tile of 128 x 128 of dy, of x or of w as floats in registers; blocks of its rows are maxima over 16 lanes, those of its columns meet in LDS, through which they are

@@ -278,13 +278,13 @@ static ForwardRoom forward_room(int32_t dtype, int32_t from_floats, int64_t rows
 }
 size_t linear_f8_workspace(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs) { return forward_room(dtype, from_floats, rows, cols, outs).bytes; }
 
-// the values of 8-bit floats as bf16, [rows][padded]
-static hipError_t launch_widen(const F8Rows &r, int64_t rows, int64_t padded, uint16_t *to, hipStream_t s)
+// 8-bit floats whose values go to `to` as bf16, [rows][padded]
+static F8QuantizeArgs widened(const F8Rows &r, int64_t rows, int64_t padded, void *to)
 {
     F8QuantizeArgs a{};
     a.dtype = TICTAC_BF16; a.format = r.format; a.block = 1 << r.shift; a.rows = rows; a.cols = padded; a.out = to; a.ld_x = padded;
     a.q = const_cast<uint8_t *>(r.q); a.ld_q = r.ld; a.scale = const_cast<uint8_t *>(r.scale); a.ld_scale = r.ld_scale;
-    return launch_dequantize_f8(a, s);
+    return a;
 }
 
 template <bool EXACT, int QF>
@@ -303,20 +303,20 @@ hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
     const bool exact = p.dtype == TICTAC_F32, few = p.rows <= kFewRows, wide = exact && !few;
     char *at = (char *)p.workspace;
     F8Rows x = p.x8;
+    F8QuantizeArgs q{};
     if (p.x) {
-        F8QuantizeArgs q{};
         q.dtype = p.dtype; q.format = TICTAC_E4M3; q.block = 1; q.rows = p.rows; q.cols = p.cols; q.x = p.x; q.ld_x = p.ld_x; q.ld_q = ld;
         if (wide) {
-            q.wide = (uint16_t *)(at + room.x);
+            q.out = at + room.x;
         } else {
             q.q = (uint8_t *)at + room.x;
             q.scale = (uint8_t *)at + room.xe;
             q.ld_scale = f8_scale_stride(p.cols);
+            if (const hipError_t e = launch_quantize_f8(q, s); e != hipSuccess) return e;
+            x = F8Rows{q.q, ld, q.scale, q.ld_scale, TICTAC_E4M3, 0};
         }
-        if (const hipError_t e = launch_quantize_f8(q, s); e != hipSuccess) return e;
-        x = F8Rows{q.q, ld, q.scale, q.ld_scale, TICTAC_E4M3, 0};
     } else if (wide) {
-        if (const hipError_t e = launch_widen(p.x8, p.rows, ld, (uint16_t *)(at + room.x), s); e != hipSuccess) return e;
+        q = widened(p.x8, p.rows, ld, at + room.x);
     }
     const int32_t splits = room.plan.splits[0];
     ProductF8Args a{};
@@ -330,7 +330,7 @@ hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
         return splits > 1 ? launch_product_join_biased(a, s) : hipGetLastError();
     }
     if (wide) {
-        if (const hipError_t e = launch_widen(p.w, p.outs, ld, (uint16_t *)(at + room.w), s); e != hipSuccess) return e;
+        if (const hipError_t e = launch_widen_f8(q, widened(p.w, p.outs, ld, at + room.w), s); e != hipSuccess) return e;
         a.p = at + room.w; a.ld_p = ld * 2;
         a.q = at + room.x; a.ld_q = ld * 2;
         a.steps = a.p_steps = (int32_t)(ld / 64);

@@ -17,7 +17,7 @@ from test_gpu_layer_paths import JOIN, kernels, ran
 
 ONCE16, ONCE8, DX, DW = "linear_f8_once_kernel<{dt}, {wide}, 16>", "linear_f8_once_kernel<{dt}, {wide}, 8>", "linear_f8_dx_few_kernel", "linear_f8_dw_few_kernel"
 S64, S128X64, S128, S128DEEP, S256 = "product_f8_kernel<{f}, {dt}, 1, 1, 4>", "product_f8_kernel<{f}, {dt}, 2, 1, 3>", "product_f8_kernel<{f}, {dt}, 2, 2, 2>", "product_f8_kernel<{f}, {dt}, 2, 2, 4>", "product_f8_kernel_256<{f}, {dt}>"
-WIDEN, EXACT64, EXACT128X64, EXACT256 = "dequantize_f8_kernel<2, true>", "product_kernel<OpBf16Biased, 0, 2, 2, 4>", "product_kernel<OpBf16Biased, 0, 4, 2, 3>", "product_kernel_256<OpBf16Biased, 0>"
+WIDEN, EXACT64, EXACT128X64, EXACT256 = "widen_f8_kernel", "product_kernel<OpBf16Biased, 0, 2, 2, 4>", "product_kernel<OpBf16Biased, 0, 4, 2, 3>", "product_kernel_256<OpBf16Biased, 0>"
 BACK64, BACK128X64, BACK128, BACK256 = "product_kernel<OpBf16, 0, 2, 2, 4>", "product_kernel<OpBf16, 0, 4, 2, 3>", "product_kernel<OpBf16, 0, 4, 4, 2>", "product_kernel_256<OpBf16, 0>"
 DT = {F32: 0, F16: 1, BF16: 2}
 
