@@ -19,7 +19,9 @@ __device__ __forceinline__ f32x4 mma_bf16(i32x4 a, i32x4 b, f32x4 c)
 // ---- few rows: bound by the bytes of the weights ----
 // A workgroup has 16 FB outputs and a part of k, its eight waves blocks of 128 of that in turn: weights go from memory to the matrix instruction without LDS, 32 bytes per lane, the next
 // block under way while one is computed.  TB blocks of 16 rows of x come from the caches.  The sums of the waves meet in LDS, those of several workgroups along k in the
-// workspace.  EXACT: bf16 instructions.
+// workspace.  EXACT: bf16 instructions.  A lane's 32 bytes of a block lie next to each other: the order of k is free, where both operands have it.
+// x is asked for together with the weights (float32 outputs, 16 x 16384 -> 16384: 64.5 us, 4.2 TB/s; without that 68.8), but where its bf16 values leave no registers for that
+// (64 x 25088 -> 4096: 43 us, with it 70).
 constexpr int kFewWaves = 8;
 
 // sixteen 8-bit floats times a power of two as operands of two bf16 instructions
@@ -39,8 +41,9 @@ __device__ __forceinline__ void widen(i32x4 q, float s, int format, i32x4 (&to)[
 template <bool EXACT, int QF, int TB, int FB>
 __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8Args p, F8Rows xq, int32_t splits, float *parts)
 {
+    constexpr bool kAhead = !(EXACT && TB == 4);
     __shared__ f32x4 sums[kFewWaves][TB][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row = lane & 15, fk = (lane >> 4) * 32;
     const int64_t blocks = gridDim.x / splits, o0 = blockIdx.x % blocks * (16 * FB);
     const int32_t split = (int32_t)(blockIdx.x / blocks), all = (int32_t)((p.cols + 127) / 128);
     const int32_t first = (int32_t)((int64_t)all * split / splits), units = (int32_t)((int64_t)all * (split + 1) / splits);
@@ -57,29 +60,31 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8A
         x[b] = xq.q + t * xq.ld + fk;
         xe[b] = xq.scale + (t >> xq.shift) * xq.ld_scale;
     }
-    struct Weights {
-        i32x4 q[FB][2];
-        int e[FB];
+    struct Operands {
+        i32x4 q[FB][2], x[TB][2];
+        int e[FB], ex[TB];
     } now, next;
     f32x4 acc[FB][TB] = {};
+    const auto request_x = [&](int32_t u) {
+#pragma unroll
+        for (int b = 0; b < TB; ++b) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) next.x[b][k] = *(const i32x4 *)(x[b] + (int64_t)u * 128 + k * 16);
+            next.ex[b] = xe[b][u];
+        }
+    };
     const auto request = [&](int32_t u) {
 #pragma unroll
         for (int f = 0; f < FB; ++f) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) next.q[f][k] = *(const i32x4 *)(w[f] + (int64_t)u * 128 + k * 64);
+            for (int k = 0; k < 2; ++k) next.q[f][k] = *(const i32x4 *)(w[f] + (int64_t)u * 128 + k * 16);
             next.e[f] = we[f][u];
         }
+        if (kAhead) request_x(u);
     };
     if (first + wave < units) request(first + wave);
     for (int32_t u = first + wave; u < units; u += kFewWaves) {
-        i32x4 fx[TB][2];
-        int ex[TB];
-#pragma unroll
-        for (int b = 0; b < TB; ++b) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) fx[b][k] = *(const i32x4 *)(x[b] + (int64_t)u * 128 + k * 64);
-            ex[b] = xe[b][u];
-        }
+        if (!kAhead) request_x(u);
         now = next;
         if (u + kFewWaves < units) request(u + kFewWaves);
         if constexpr (EXACT) {
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8A
 #pragma unroll
             for (int b = 0; b < TB; ++b)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) widen(fx[b][k], f8_factor(ex[b]), QF, wide_x[b][k]);
+                for (int k = 0; k < 2; ++k) widen(now.x[b][k], f8_factor(now.ex[b]), QF, wide_x[b][k]);
 #pragma unroll
             for (int f = 0; f < FB; ++f)
 #pragma unroll
@@ -105,7 +110,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8A
             for (int f = 0; f < FB; ++f)
 #pragma unroll
                 for (int b = 0; b < TB; ++b)
-                    acc[f][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(now.q[f]), whole(fx[b]), acc[f][b], TICTAC_E4M3, QF, 0, now.e[f], 0, ex[b]);
+                    acc[f][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(now.q[f]), whole(now.x[b]), acc[f][b], TICTAC_E4M3, QF, 0, now.e[f], 0, now.ex[b]);
         }
     }
 #pragma unroll
