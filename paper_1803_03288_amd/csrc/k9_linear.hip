@@ -138,13 +138,12 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_f8_few_kernel(LinearF8A
 }
 
 // Up to sixteen rows of floats, rounded to 8 bits here: every workgroup does that again, into LDS, under its first loads of the weights, which costs less than a launch before it while there
-// are few elements for each thread (kOnceElements).  A workgroup has 16 outputs, its waves blocks of 128 of k in turn, kUnits of them under way.  The 8-bit values are those
-// of quantize_f8_kernel.
-constexpr int kOnceRows = 16, kOnceUnits = 4;
-constexpr int64_t kOnceElements = 32768;
+// are few elements to round, of a workgroup and of all (once).  A workgroup has 16 outputs, its eight waves blocks of 128 of k in turn, kOnceUnits of them under way.  The 8-bit values are
+// those of quantize_f8_kernel.  1 x 4096 -> 16384 bfloat16: 13.6 us, 4.9 TB/s.
+constexpr int kOnceRows = 16, kOnceUnits = 4, kOnceWaves = 8;
 
-template <int DT, bool WIDE, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void linear_f8_once_kernel(LinearF8Args p)
+template <int DT, bool WIDE>
+__global__ __launch_bounds__(kOnceWaves * 64) void linear_f8_once_kernel(LinearF8Args p)
 {
     using E = Elem<DT>;
     constexpr bool EXACT = DT == TICTAC_F32;
@@ -165,8 +164,8 @@ __global__ __launch_bounds__(WAVES * 64) void linear_f8_once_kernel(LinearF8Args
         unit[n].e = we[u];
     };
 #pragma unroll
-    for (int n = 0; n < kOnceUnits; ++n) request(n, wave + n * WAVES);
-    for (int32_t at = (int32_t)threadIdx.x >> 4; at < rows * units; at += WAVES * 4) {
+    for (int n = 0; n < kOnceUnits; ++n) request(n, wave + n * kOnceWaves);
+    for (int32_t at = (int32_t)threadIdx.x >> 4; at < rows * units; at += kOnceWaves * 4) {
         const int32_t t = at / units, b = at - t * units, part = (int32_t)threadIdx.x & 15, col = b * 128 + part * 8;
         float v[8];
         E::floats(load8<DT, WIDE>((const typename E::type *)p.x + t * p.ld_x, col, p.cols), v);
@@ -181,13 +180,13 @@ __global__ __launch_bounds__(WAVES * 64) void linear_f8_once_kernel(LinearF8Args
     const int mine = min(row, rows - 1);
     const uint8_t *const x = held + mine * stride + fk, *const xe = scales + mine * units;
     f32x4 acc{};
-    for (int32_t u0 = wave; u0 < units; u0 += kOnceUnits * WAVES) {
+    for (int32_t u0 = wave; u0 < units; u0 += kOnceUnits * kOnceWaves) {
 #pragma unroll
         for (int n = 0; n < kOnceUnits; ++n) {
-            const int32_t u = u0 + n * WAVES;
+            const int32_t u = u0 + n * kOnceWaves;
             if (u >= units) break;
             const Unit now = unit[n];
-            if (u + kOnceUnits * WAVES < units) request(n, u + kOnceUnits * WAVES);
+            if (u + kOnceUnits * kOnceWaves < units) request(n, u + kOnceUnits * kOnceWaves);
             const i32x4 lo = *(const i32x4 *)(x + u * 128), hi = *(const i32x4 *)(x + u * 128 + 64);
             const int e = xe[u];
             if constexpr (EXACT) {
@@ -214,23 +213,25 @@ __global__ __launch_bounds__(WAVES * 64) void linear_f8_once_kernel(LinearF8Args
     if (t >= rows || o0 + out >= p.outs) return;
     float sum = 0.0f;
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) sum += sums[k * 64 + (out >> 2) * 16 + t][out & 3];
+    for (int k = 0; k < kOnceWaves; ++k) sum += sums[k * 64 + (out >> 2) * 16 + t][out & 3];
     if (p.bias) sum += param(p.bias, p.bias_dtype, o0 + out);
     put_param(p.y, p.dtype, t * p.ld_y + o0 + out, sum);
 }
 
-static bool once(int64_t rows, int64_t cols) { return rows <= kOnceRows && rows * rows8_stride(cols) <= kOnceElements; }
+// (microseconds, here and by a launch for the rounding and the better of the others, outputs of 16 bits: 1 x 4096 -> 4096 5.6 and 9.1, 8 rows 9.5 and 9.8, 12 rows 11.9 and 10.1;
+// 2 x 4096 -> 16384 14.1 and 16.5, 4 rows 17.4 and 16.6; float32, whose operands are widened in every workgroup too: 2 x 4096 -> 4096 8.1 and 9.5, 8 rows 11.6 and 10.2)
+static bool once(bool exact, int64_t rows, int64_t cols, int64_t outs)
+{
+    const int64_t elements = rows * rows8_stride(cols);
+    return rows <= kOnceRows && elements <= 1 << 15 && elements * ((outs + 15) / 16) <= (exact ? 1 << 22 : 1 << 23);
+}
 
 template <int DT, bool WIDE>
 static hipError_t launch_once(const LinearF8Args &p, hipStream_t s)
 {
-    // (few workgroups: more waves in each)
-    const int64_t blocks = (p.outs + 15) / 16;
-    const int waves = blocks <= 512 ? 16 : 8;
-    const auto kernel = waves == 16 ? linear_f8_once_kernel<DT, WIDE, 16> : linear_f8_once_kernel<DT, WIDE, 8>;
     const int64_t units = f8_blocks(p.cols);
-    const size_t lds = std::max<size_t>((size_t)(p.rows * (units * 128 + 16 + units)), (size_t)waves * 1024);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(waves * 64), (lds + 15) / 16 * 16, s, p);
+    const size_t lds = std::max<size_t>((size_t)(p.rows * (units * 128 + 16 + units)), kOnceWaves * 1024);
+    hipLaunchKernelGGL((linear_f8_once_kernel<DT, WIDE>), dim3((unsigned)((p.outs + 15) / 16)), dim3(kOnceWaves * 64), (lds + 15) / 16 * 16, s, p);
     return hipGetLastError();
 }
 
@@ -247,11 +248,20 @@ static int32_t parts_along_k(int64_t blocks, int64_t most, int64_t room)
     return best;
 }
 
-constexpr int64_t kFewRows = 64;
-static int32_t few_blocks_of(int64_t rows, int64_t outs) { return rows <= 8 || outs <= 2048 ? 1 : rows <= 16 ? 2 : 4; }
+// Few rows, by linear_f8_few_kernel: float32 outputs up to 64, where tiles want all weights as bf16 first (64 x 4096 -> 4096: 19 us, 25 in tiles; 17 rows 11.6 and 25).  In 16 bits tiles read the
+// weights as fast and x less often, and what is left are small products and, up to 16 rows, medium ones (microseconds, here and in tiles: 16 x 4096 -> 4096 10.7 and 12.4, 16 x 4096 ->
+// 16384 19.2 and 17.0; 32 x 1024 -> 4096 8.2 and 9.7, 32 x 4096 -> 4096 13.0 and 12.7, 32 x 25088 -> 4096 31.9 and 28.4).
+static bool few_rows(bool exact, int64_t rows, int64_t cols, int64_t outs)
+{
+    const int64_t weights = cols * outs;
+    return exact ? rows <= 64 : rows <= 16 ? weights < 1 << 26 : rows <= 64 && weights <= 1 << 22;
+}
+// Blocks of 16 outputs of a workgroup: more of them read x less often, but leave fewer workgroups.  (16 x 2048 -> 16384: one 14.0 us, two 12.3; 16 x 4096 -> 4096 10.7 and 12.2; float32, 64 x 2048 ->
+// 16384: one 34, four 21; 32 x 4096 -> 4096 13.3 and 14.2.)
+static int32_t few_blocks_of(int64_t rows, int64_t cols, int64_t outs) { return cols * outs < 1 << 25 ? 1 : rows <= 16 ? 2 : 4; }
 static int32_t few_splits(int64_t rows, int64_t cols, int64_t outs)
 {
-    const int64_t each = 16 * few_blocks_of(rows, outs), blocks = (outs + each - 1) / each, units = (cols + 127) / 128;
+    const int64_t each = 16 * few_blocks_of(rows, cols, outs), blocks = (outs + each - 1) / each, units = (cols + 127) / 128;
     return parts_along_k(blocks, units / kFewWaves, 256);
 }
 
@@ -265,9 +275,9 @@ struct ForwardRoom {
 static ForwardRoom forward_room(int32_t dtype, int32_t from_floats, int64_t rows, int64_t cols, int64_t outs)
 {
     ForwardRoom r{};
-    if (from_floats && once(rows, cols)) return r;
     const int64_t ld = rows8_stride(cols);
-    const bool exact = dtype == TICTAC_F32, few = rows <= kFewRows;
+    const bool exact = dtype == TICTAC_F32, few = few_rows(exact, rows, cols, outs);
+    if (from_floats && once(exact, rows, cols, outs)) return r;
     if (few) {
         r.plan = {0, {few_splits(rows, cols, outs), 1}};
     } else {
@@ -295,17 +305,18 @@ static F8QuantizeArgs widened(const F8Rows &r, int64_t rows, int64_t padded, voi
 template <bool EXACT, int QF>
 static auto few_kernel(int64_t rows, int32_t fb)
 {
-    return rows <= 16   ? (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 1, 1> : linear_f8_few_kernel<EXACT, QF, 1, 2>)
-           : rows <= 32 ? (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 2, 1> : linear_f8_few_kernel<EXACT, QF, 2, 4>)
-                        : (fb == 1 ? linear_f8_few_kernel<EXACT, QF, 4, 1> : linear_f8_few_kernel<EXACT, QF, 4, 4>);
+    if (rows <= 16) return fb == 1 ? linear_f8_few_kernel<EXACT, QF, 1, 1> : linear_f8_few_kernel<EXACT, QF, 1, 2>;
+    if constexpr (EXACT)
+        if (fb != 1) return rows <= 32 ? linear_f8_few_kernel<EXACT, QF, 2, 4> : linear_f8_few_kernel<EXACT, QF, 4, 4>;
+    return rows <= 32 ? linear_f8_few_kernel<EXACT, QF, 2, 1> : linear_f8_few_kernel<EXACT, QF, 4, 1>;
 }
 
 hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
 {
-    if (p.x && once(p.rows, p.cols)) return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), launch_once, p, s);
+    const bool exact = p.dtype == TICTAC_F32, few = few_rows(exact, p.rows, p.cols, p.outs), wide = exact && !few;
+    if (p.x && once(exact, p.rows, p.cols, p.outs)) return BY_TYPE(p.dtype, wide_rows(p.x, p.dtype, p.ld_x, p.cols), launch_once, p, s);
     const ForwardRoom room = forward_room(p.dtype, p.x != nullptr, p.rows, p.cols, p.outs);
     const int64_t ld = rows8_stride(p.cols);
-    const bool exact = p.dtype == TICTAC_F32, few = p.rows <= kFewRows, wide = exact && !few;
     char *at = (char *)p.workspace;
     F8Rows x = p.x8;
     F8QuantizeArgs q{};
@@ -328,7 +339,7 @@ hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
     a.R = (int32_t)p.outs; a.C = (int32_t)p.rows; a.splits = splits;
     a.out = p.y; a.ld_out = p.ld_y; a.dtype = p.dtype; a.bias = p.bias; a.bias_dtype = p.bias_dtype; a.parts = at + room.parts;
     if (few) {
-        const int32_t fb = few_blocks_of(p.rows, p.outs), outs = 16 * fb;
+        const int32_t fb = few_blocks_of(p.rows, p.cols, p.outs), outs = 16 * fb;
         const auto kernel = exact ? (x.format == TICTAC_E5M2 ? few_kernel<true, TICTAC_E5M2>(p.rows, fb) : few_kernel<true, TICTAC_E4M3>(p.rows, fb))
                                   : (x.format == TICTAC_E5M2 ? few_kernel<false, TICTAC_E5M2>(p.rows, fb) : few_kernel<false, TICTAC_E4M3>(p.rows, fb));
         hipLaunchKernelGGL(kernel, dim3((unsigned)((p.outs + outs - 1) / outs * splits)), dim3(kFewWaves * 64), 0, s, p, x, splits, (float *)a.parts);
@@ -518,7 +529,7 @@ template <int QF>
 static hipError_t launch_dx_few(const LinearF8Args &p, const F8Operand &dy, void *parts, hipStream_t s)
 {
     const int32_t splits = dx_few_splits(p.cols, p.outs);
-    const auto kernel = p.rows <= 16 ? linear_f8_dx_few_kernel<QF, 1> : p.rows <= 32 ? linear_f8_dx_few_kernel<QF, 2> : linear_f8_dx_few_kernel<QF, 4>;
+    const auto kernel = p.rows <= 16 ? linear_f8_dx_few_kernel<QF, 1> : linear_f8_dx_few_kernel<QF, 2>;
     const size_t lds = (size_t)kBackWaves * 8 * 64 * 16;
     if (const hipError_t e = ensure_dynamic_lds((const void *)kernel, lds); e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(f8_blocks(p.cols) * splits)), dim3(kBackWaves * 64), lds, s, p, dy, splits, (float *)parts);
@@ -529,6 +540,11 @@ static hipError_t launch_dx_few(const LinearF8Args &p, const F8Operand &dy, void
 }
 
 // ---- backward ----
+// Both products in tiles are one launch; by themselves those of few rows leave the weights as they lie and write dw past the caches, which pays where there are many weights (microseconds,
+// outputs of 16 bits, dx and dw by themselves, dw alone, none: 32 x 1024 -> 4096 25, 24, 20; 32 x 4096 -> 4096 29, 35, 36; 64 x 4096 -> 4096 42, 35, 36; 32 x 25088 -> 4096 83, 109, 127;
+// 64 x 25088 -> 4096 120, 113, 129; 128 x 4096 -> 4096 41 and 35, 128 x 4096 -> 16384 94 and 103 for the last two).
+constexpr int64_t kDxFewRows = 32;
+static bool dw_by_itself(bool exact, int64_t rows, int64_t cols, int64_t outs) { return !exact && rows <= kF8Block && cols * outs >= (rows <= kDxFewRows ? 1 << 23 : 1 << 25); }
 struct BackwardRoom {
     int64_t padded_o, padded_t;
     ProductPlan plan;                       // dx, dw
@@ -543,9 +559,9 @@ static BackwardRoom backward_room(int32_t dtype, int64_t rows, int64_t cols, int
     r.padded_t = rows8_stride(rows);
     const int64_t step = exact ? 64 : 128;
     const ProductShape shapes[2] = {{(int32_t)cols, (int32_t)rows, (int32_t)(r.padded_o / step)}, {(int32_t)cols, (int32_t)outs, (int32_t)(r.padded_t / step)}};
-    const bool few = rows <= kFewRows && !exact;            // (dx then may come from the weights as they lie)
-    // up to a block of rows dw is by itself, and the tiles are dx's alone
-    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes, rows <= kF8Block ? 1 : 2);
+    const bool alone = dw_by_itself(exact, rows, cols, outs), few = alone && rows <= kDxFewRows;       // (few: dx may come from the weights as they lie)
+    // where dw is by itself, the tiles are dx's alone
+    r.plan = exact ? plan_products(shapes, 2) : plan_products_f8(shapes, alone ? 1 : 2);
     const size_t e = exact ? 0 : 1;         // (values as bf16 have no scales)
     r.w = r.sums + up((size_t)f8_blocks(rows) * outs * 4);
     r.we = r.w + up((size_t)cols * r.padded_o * size);
@@ -580,12 +596,12 @@ hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
 {
     if (p.rows == 0 || p.outs == 0) return backward_nothing(p, s);
     const BackwardRoom room = backward_room(p.dtype, p.rows, p.cols, p.outs);
-    const bool exact = p.dtype == TICTAC_F32;
+    const bool exact = p.dtype == TICTAC_F32, alone = dw_by_itself(exact, p.rows, p.cols, p.outs);
     const int64_t size = exact ? 2 : 1, step = exact ? 64 : 128;
     char *at = (char *)p.workspace;
     F8TurnArgs t{};
     t.dtype = p.dtype; t.format = p.format; t.rows = p.rows; t.cols = p.cols; t.outs = p.outs; t.dy = p.dy; t.ld_dy = p.ld_dy; t.x = p.x8; t.w = p.w;
-    const bool dx_few = p.dx && p.rows <= kFewRows && !exact && p.w.shift;
+    const bool dx_few = p.dx && alone && p.rows <= kDxFewRows && p.w.shift;
     if (p.dx) {
         if (!dx_few) t.w_cols = {at + room.w, room.padded_o, (uint8_t *)at + room.we, f8_scale_stride(p.outs)};
         t.dy_rows = {at + room.dy_rows, room.padded_o, (uint8_t *)at + room.dy_rows_e, f8_scale_stride(p.outs)};
@@ -610,7 +626,7 @@ hipError_t launch_linear_f8_backward(const LinearF8Args &p, hipStream_t s)
     }
     if (p.dx && !dx_few) add(t.w_cols, t.dy_rows, room.padded_o, p.rows, p.dx, p.ld_dx, room.plan.splits[0], room.parts_x);
     const ColumnSums c{t.sums, f8_blocks(p.rows), p.outs, p.db, p.dtype};
-    if (p.dw && !exact && p.rows <= kF8Block) {
+    if (p.dw && alone) {
         const bool wide = wide_rows(p.dw, p.dtype, p.ld_dw, p.cols);
         const hipError_t e = p.dtype == TICTAC_F16 ? (wide ? launch_dw_few<TICTAC_F16, true>(p, t.x_cols, t.dy_cols, c, s) : launch_dw_few<TICTAC_F16, false>(p, t.x_cols, t.dy_cols, c, s))
                                                    : (wide ? launch_dw_few<TICTAC_BF16, true>(p, t.x_cols, t.dy_cols, c, s) : launch_dw_few<TICTAC_BF16, false>(p, t.x_cols, t.dy_cols, c, s));
