@@ -43,9 +43,21 @@ struct ColumnSums {
 // How the products of one launch are dealt to workgroups: the tile, and into how many parts each product's steps are cut.
 struct ProductShape { int32_t R, C, steps; };
 struct ProductPlan {
-    int32_t tile;               // one of kTiles, or kTile256
+    int32_t tile;               // one of kCosts.tiles, or kTile256
     int32_t splits[2];
 };
+constexpr int32_t kTile256 = 3;
+
+// What tiles take: see kCosts.
+struct ProductTile { int32_t r, c; float fixed, step, step2; };
+struct ProductCosts {
+    ProductTile tiles[3];
+    int32_t longest;            // steps of a part, at most
+    bool beside;                // the longest workgroups go on beside the starts and ends of others, and up to two per compute unit the time rises with their number
+    float joined;               // bytes of parts that are written and read again in a us
+    float first256, tile256, next256, step256, half256;         // tiles of 256 x 256: what a launch, a tile and each turn but the first take beside the steps, a step, the least of a step
+};
+ProductPlan plan_products(const ProductShape *shapes, int n, const ProductCosts &costs);
 ProductPlan plan_products(const ProductShape *shapes, int n);
 inline size_t product_parts_bytes(int32_t splits, int32_t R, int32_t C) { return splits > 1 ? (size_t)splits * R * C * 4 : 0; }
 hipError_t launch_product_i8(const ProductArgs &a, int32_t tile, hipStream_t s);

@@ -283,11 +283,14 @@ __global__ __launch_bounds__(256, 1) void product_kernel_256(Products all)
 // together) with two.  Measured with int8 on 256, 512 and 1024 workgroups of 2 to 64 steps: 128 x 128 on 256 workgroups 8.7 us for two steps and 39.5 for 64,
 // 128 x 64 6.8 and 26.6, 64 x 64 5.6 and 21.6; on 512 11.1 and 63.6, 8.7 and 43.1, 6.2 and 29.2.  Full, all of them come to what the L2 gives LDS (18 to
 // 21 TB/s).
-struct Tile { int32_t r, c; float fixed, step, step2; };
-constexpr Tile kTiles[] = {{4, 4, 7.6f, 0.5f, 0.85f}, {4, 2, 6.0f, 0.33f, 0.56f}, {2, 2, 5.1f, 0.26f, 0.37f}};
-constexpr int32_t kTile256 = 3;
+// Tiles of 256 x 256, one workgroup per compute unit from tile to tile: 1.45 us a step with all compute units busy, 1.0 with half of them, 6 us for a first tile besides and 11 for each
+// behind it.
+constexpr ProductCosts kCosts{{{4, 4, 7.6f, 0.5f, 0.85f}, {4, 2, 6.0f, 0.33f, 0.56f}, {2, 2, 5.1f, 0.26f, 0.37f}}, 64, false, 4.5e6f, 4.0f, 6.0f, 5.0f, 1.45f, 1.0f};
+constexpr const ProductTile (&kTiles)[3] = kCosts.tiles;
 
-ProductPlan plan_products(const ProductShape *shapes, int n)
+ProductPlan plan_products(const ProductShape *shapes, int n) { return plan_products(shapes, n, kCosts); }
+
+ProductPlan plan_products(const ProductShape *shapes, int n, const ProductCosts &costs)
 {
     ProductPlan best{0, {1, 1}};
     float least = 1e30f;
@@ -299,10 +302,10 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
         best.splits[1] = splits[1];
     };
     for (int32_t tile = 0; tile < kTile256; ++tile) {
-        const Tile &t = kTiles[tile];
+        const ProductTile &t = costs.tiles[tile];
         int64_t tiles[2] = {0, 0};
         for (int i = 0; i < n; ++i) tiles[i] = (int64_t)((shapes[i].R + 32 * t.r - 1) / (32 * t.r)) * ((shapes[i].C + 32 * t.c - 1) / (32 * t.c));
-        for (int32_t most = 1 << 30; most >= 2; most = most > 64 ? 64 : most / 2) {         // steps of a workgroup
+        for (int32_t most = 1 << 30; most >= 2; most = most > costs.longest ? costs.longest : most / 2) {         // steps of a workgroup
             int32_t splits[2] = {1, 1};
             int64_t blocks = 0;
             float steps = 0.0f, all_steps = 0.0f, us = 0.0f;
@@ -311,31 +314,35 @@ ProductPlan plan_products(const ProductShape *shapes, int n)
                 blocks += tiles[i] * splits[i];
                 steps = std::max(steps, (float)shapes[i].steps / (float)splits[i]);
                 all_steps += (float)tiles[i] * (float)shapes[i].steps;
-                if (splits[i] > 1) us += 1.0f + (float)splits[i] * (float)shapes[i].R * (float)shapes[i].C * (8.0f / 4.5e6f);       // written and read again
+                if (splits[i] > 1) us += 1.0f + (float)splits[i] * (float)shapes[i].R * (float)shapes[i].C * (8.0f / costs.joined);       // written and read again
             }
             for (int i = 0; i < n; ++i)
                 if (splits[i] > 1) { us += 2.0f; break; }                                   // the launch that adds them up
-            const float per_cu = (float)((blocks + 255) / 256);
+            const float per_cu = (float)((blocks + 255) / 256), some = costs.beside && blocks < 512 ? (float)blocks / 256.0f - 1.0f : 1.0f;    // (some: compute units with two)
+            const float single = t.fixed + t.step * steps;
             if (per_cu <= 1.0f) {
-                us += t.fixed + t.step * steps;
+                us += single;
             } else {                                            // the longest of them begin at once where they are the first product's, and else may come last
-                const float mean = std::min(all_steps / (float)blocks, steps), work = t.step2 * 0.5f * mean * per_cu, one = t.step2 * steps;
-                us += t.fixed * (0.5f + 0.35f * per_cu) + (shapes[0].steps * splits[n - 1] >= shapes[n - 1].steps * splits[0] ? std::max(work, one) : work + t.step2 * (steps - mean));
+                const float mean = std::min(all_steps / (float)blocks, steps), work = t.step2 * 0.5f * mean * per_cu, starts = t.fixed * (0.5f + 0.35f * per_cu);
+                const bool first = shapes[0].steps * splits[n - 1] >= shapes[n - 1].steps * splits[0];
+                const float all = !first         ? starts + work + t.step2 * (steps - mean)
+                                  : costs.beside ? std::max(starts + work, t.fixed + 0.5f * (t.step + t.step2) * steps)
+                                                 : starts + std::max(work, t.step2 * steps);
+                us += some < 1.0f ? single + some * (all - single) : all;
             }
             take(tile, splits, us);
         }
     }
-    // tiles of 256 x 256, one workgroup per compute unit from tile to tile, those of the first product first: 1.45 us a step with all compute units busy, 1.0 with
-    // half of them, 6 us for a first tile besides and 11 for each behind it; the longest of the workgroups that begin with the second product's tiles one turn earlier or later
+    // tiles of 256 x 256, those of the first product first; the longest of the workgroups that begin with the second product's tiles one turn earlier or later
     float each[2] = {0.0f, 0.0f};
     int64_t tiles[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
         tiles[i] = (int64_t)((shapes[i].R + 255) / 256) * ((shapes[i].C + 255) / 256);
     }
-    const float step = std::min(1.45f, std::max(1.0f, (float)(tiles[0] + tiles[1]) * (1.45f / 256.0f)));
-    for (int i = 0; i < n; ++i) each[i] = 6.0f + step * (float)shapes[i].steps;
+    const float step = std::min(costs.step256, std::max(costs.half256, (float)(tiles[0] + tiles[1]) * (costs.step256 / 256.0f)));
+    for (int i = 0; i < n; ++i) each[i] = costs.tile256 + step * (float)shapes[i].steps;
     const int64_t turns = (tiles[0] + tiles[1] + 255) / 256, early = tiles[0] / 256, late = (tiles[0] + 255) / 256;
-    const float us = 4.0f + 5.0f * (float)(turns - 1) + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
+    const float us = costs.first256 + costs.next256 * (float)(turns - 1) + std::max((float)early * each[0] + (float)(turns - early) * each[1], (float)late * each[0] + (float)(turns - late) * each[1]);
     take(kTile256, {1, 1}, us);
     return best;
 }

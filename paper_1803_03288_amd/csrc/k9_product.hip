@@ -421,17 +421,19 @@ __global__ __launch_bounds__(256, 1) void product_f8_kernel_256(ProductsF8 all)
     }
 }
 
-struct TileF8 { int32_t r, c; };
-constexpr TileF8 kTilesF8[] = {{2, 2}, {2, 1}, {1, 1}, {4, 4}};
-constexpr int32_t kLargest = 3;
+// Measured on 128 to 1024 workgroups of 1 to 196 steps: 128 x 128 on 256 workgroups 7.8 us for two steps and 41.3 for 64, 128 x 64 5.8 and 28.2, 64 x 64 5.0 and 24.7; on 512 10.6 and 68.5,
+// 7.5 and 46.2, 5.6 and 34.9; 256 x 256 12.0 and 98.9, on 512 24.5 and 196.  Over 61 forward and backward calls the choice takes up to 1.06 of the best one's time, and 1.12
+// in two of them; by the costs of int8 up to 1.24 (512 x 25088 -> 4096: 82 us, now 66).
+constexpr ProductCosts kCostsF8{{{4, 4, 6.6f, 0.56f, 0.98f}, {4, 2, 4.9f, 0.36f, 0.66f}, {2, 2, 4.6f, 0.31f, 0.47f}}, 128, true, 4e6f, 4.6f, 4.5f, 3.0f, 1.4f, 1.12f};
 
-ProductPlan plan_products_f8(const ProductShape *shapes, int n) { return plan_products(shapes, n); }
+ProductPlan plan_products_f8(const ProductShape *shapes, int n) { return plan_products(shapes, n, kCostsF8); }
 
 template <int QF, int OUT>
 static hipError_t launch_as(const ProductF8Args *a, int n, int32_t tile, const ColumnSums &c, hipStream_t s)
 {
     ProductsF8 all{};
-    const int32_t tr = 64 * kTilesF8[tile].r, tc = 64 * kTilesF8[tile].c;
+    const bool large = tile == kTile256;
+    const int32_t tr = large ? 256 : 32 * kCostsF8.tiles[tile].r, tc = large ? 256 : 32 * kCostsF8.tiles[tile].c;
     int32_t blocks = 0;
     for (int i = 0; i < 2; ++i) {
         all.first[i] = blocks;
@@ -446,14 +448,13 @@ static hipError_t launch_as(const ProductF8Args *a, int n, int32_t tile, const C
     all.sum_blocks = c.out ? (int32_t)((c.n + 63) / 64) : 0;
     if (n == 1) all.first[1] = all.first[2];
     if (blocks + all.sum_blocks == 0) return hipSuccess;
-    const bool large = tile == kLargest;
     if (large) {
         int device = 0;
         if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
         blocks = std::min(blocks, (int32_t)device_cu_count(device));
     }
     blocks += all.sum_blocks;
-    const bool alone = blocks <= 256;
+    const bool alone = blocks <= 256;                                   // (1024 x 4096 -> 4096, 256 workgroups: four buffers 29.9 us, two 35.8; 2048 x 2048 -> 4096, 512: 35.4 and 29.4)
     const auto kernel = large       ? product_f8_kernel_256<QF, OUT>
                         : tile == 0 ? (alone ? product_f8_kernel<QF, OUT, 2, 2, 4> : product_f8_kernel<QF, OUT, 2, 2, 2>)
                         : tile == 1 ? product_f8_kernel<QF, OUT, 2, 1, 3>
