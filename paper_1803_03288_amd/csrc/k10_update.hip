@@ -5,7 +5,7 @@
 // all in float32, each product and sum rounded by itself, so that moments in 8 bits do not depend on what a compiler contracts.  Moments in 8 bits are rows of e4m3 (f8.h) of m and
 // of r = sqrt(v), which the update needs anyway: the range of r is half of v's in powers of two.  They are rounded at random, up with a probability of the part that is cut off: with
 // b2 = 0.999 v decays by 0.1 % a step, and to nearest would never leave a value whose neighbours are 6 to 12 % away.
-// Bound by memory: an element is read and written once.
+// Bound by memory: an element is read and written once.  67 million parameters with moments in 8 bits: 194 to 227 us, 4.8 to 5.6 TB/s.
 #include <math.h>
 
 #include <algorithm>
@@ -85,7 +85,8 @@ __device__ __forceinline__ void add_squares(const void *g, int64_t at, double &s
     }
 }
 
-// A workgroup has a run of chunks, which a walk through the table finds the tensors of.  67 million bfloat16 values: 27 us, 5 TB/s.
+// A workgroup has a run of chunks, which a walk through the table finds the tensors of.  67 million bfloat16 values: 26 us, 5 TB/s; 33 to 48 behind a
+// step, whose writes are still on their way.
 __global__ __launch_bounds__(256) void gradient_norm_kernel(NormTable table, double *parts)
 {
     __shared__ double part[4];

@@ -362,7 +362,7 @@ hipError_t launch_linear_f8(const LinearF8Args &p, hipStream_t s)
 // The weights, in blocks of 128 x 128, have k (the outputs o) as rows, and the matrix instruction wants 32 of k per lane.  A lane reads eight bytes of each of 32 rows, a wave 128 rows of
 // 128 columns, one block; squares of 4 x 4 bytes are turned round in registers, and byte j of the eight is an operand whose row r is column 8 r + j, so that a lane's results are columns
 // next to each other.  A workgroup has 128 columns and a part of k, its eight waves blocks of that in turn; their sums meet in LDS, in fixed order.  The 16 KB that each wave
-// has under way are more than memory's latency asks for.
+// has under way are more than memory's latency asks for.  32 x 4096 -> 25088 float16: 27 us, 3.9 TB/s.
 constexpr int kBackWaves = 8;
 
 // four rows of four bytes to four columns
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(kBackWaves * 64) void linear_f8_dx_few_kernel(Linea
 
 // dw where the rows are one block: a matrix instruction is all that an output takes, and dw's bytes are what bounds it.  A wave has 64 columns, whose operands (turned round before, 128
 // bytes of k each, of which those behind the last row are not read) stay in registers, and 128 outputs, a workgroup 512 columns.  Row r of operand j is the column at(r) + j: a lane's results (rows 4 g + e) then are eight next to each other at
-// 8 g, and eight at 32 + 8 g, and four lanes store 64 bytes in a row.
+// 8 g, and eight at 32 + 8 g, and four lanes store 64 bytes in a row.  25088 x 4096 float16: 51 us, 4.7 TB/s; workgroups of 256 outputs take 3 us more.
 constexpr int kDwOuts = 128;
 
 template <int QF, int DT, bool WIDE>

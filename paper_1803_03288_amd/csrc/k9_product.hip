@@ -114,6 +114,7 @@ __device__ __forceinline__ void put_blocks32(const ProductArgs &a, const f32x16 
 // block of 32 x 32; under those of each half the operands of the next are read:
 //   - half 0 of step t reads the rest of step t; then a barrier, before which each wave has waited for its reads and for its loads of step t + 1;
 //   - half 1 of step t reads the first half of step t + 1 and asks for step t + STAGES, into the buffer of step t.
+// 1024 x 4096 -> 4096: 23.5 us, 1.46 PFLOP/s; bound by what the L2 gives LDS, and small ones by their start.
 template <int QF, int OUT, int BR, int BC, int STAGES>
 __global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_f8_kernel(ProductsF8 all)
 {
@@ -220,7 +221,8 @@ __global__ __launch_bounds__(256, STAGES * (BR + BC) > 10 ? 1 : 2) void product_
 }
 
 // Tiles of 256 x 256 outputs by four waves, one per SIMD, of 128 x 128 each: 8 x 8 blocks of 16 x 16, whose matrix instruction takes a whole step.  (Blocks of 32 x 32 take half a step each, and
-// 5 to 7 % more power for the same values, by which large products are bound: 8192 x 4096 -> 16384 492 us.)  The accumulators fill the 256 accumulation registers, the operands of one step
+// 5 to 7 % more power for the same values, by which large products are bound: 8192 x 4096 -> 16384 492 us, now 460 to 470, 2.35 PFLOP/s, where a library product of 8-bit floats without
+// such scales takes 446 to 466.)  The accumulators fill the 256 accumulation registers, the operands of one step
 // half of the others; the next step's go to the same registers, as they become free:
 //   - the first half of step t multiplies rows 0-3 of the blocks by all columns, and reads rows 4-7; then a barrier, before which each wave has waited for its reads and for its loads of
 //     step t + 1: nobody reads the buffer of step t any more;
