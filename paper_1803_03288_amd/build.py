@@ -8,6 +8,8 @@ import os
 import re
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -267,17 +269,26 @@ def build_layers(verbose: bool = False) -> str:
     return LAYERS
 
 
+CHECKS = {"k1_propagate.hip": check_counted_waits, "k8_product.hip": check_accumulators, "k9_product.hip": check_products_f8}
+
+
 def build(verbose: bool = False) -> str:
-    cmd = [HIPCC] + FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB] + sources()
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    for source, check in (("k1_propagate.hip", check_counted_waits), ("k8_product.hip", check_accumulators),
-                          ("k9_product.hip", check_products_f8)):
-        bad = check(device_assembly(os.path.join(CSRC, source)))
-        if bad:
-            os.remove(LIB)
-            raise RuntimeError(f"{source}: what is written by hand no longer matches the generated code:\n  " + "\n  ".join(bad))
+    compile_flags = [f for f in FLAGS if f != "-shared"] + ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as jobs:
+        def compiled(source):
+            to = os.path.join(objects, os.path.basename(source) + ".o")
+            cmd = [HIPCC] + compile_flags + ["-c", "-o", to, source]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.check_call(cmd)
+            return to
+
+        checks = {name: jobs.submit(lambda name, check: check(device_assembly(os.path.join(CSRC, name))), name, check) for name, check in CHECKS.items()}
+        found = list(jobs.map(compiled, sorted(sources(), key=os.path.getsize, reverse=True)))
+        for source, check in checks.items():
+            if check.result():
+                raise RuntimeError(f"{source}: what is written by hand no longer matches the generated code:\n  " + "\n  ".join(check.result()))
+        subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + sorted(found))
     build_layers(verbose)
     return LIB
 
