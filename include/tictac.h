@@ -436,7 +436,8 @@ int tictac_linear_f8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t
                               const tictac_float8 *w, void *dx, int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,
                               tictac_stream stream);
 
-/* norm = scale * sqrt(sum of the squares of all elements of n tensors), squares and sums in float64 in a fixed order; norm: one float on the device.  n >= 0. */
+/* norm = scale * sqrt(sum of the squares of all elements of n tensors), squares and sums in float64 in a fixed order; norm: one float on the device.  Fewer than 2^24 tensors of at most 2^37
+ * elements each. */
 typedef struct tictac_gradient {
     const void *g;                 /* device, contiguous */
     int64_t numel;

@@ -56,6 +56,12 @@ F8QuantizeArgs quantize_args(int32_t dtype, int64_t rows, int64_t cols, const ti
     a.q = (uint8_t *)f->q; a.ld_q = f->ld; a.scale = f->scale; a.ld_scale = f->ld_scale;
     return a;
 }
+int check_count(int32_t n)
+{
+    if (n >= 0 && n < 1 << 24) return TICTAC_OK;
+    set_error("n = %d tensors, expected fewer than 2^24", n);
+    return TICTAC_ERR_UNSUPPORTED;
+}
 int check_backward(int64_t rows, int64_t cols, int64_t outs)
 {
     TT_CHECK(check_product(rows, cols, outs));
@@ -165,7 +171,7 @@ try {
 
 int tictac_gradient_norm_workspace(int32_t n, size_t *bytes)
 try {
-    if (n < 0) { set_error("n = %d", n); return TICTAC_ERR_UNSUPPORTED; }
+    TT_CHECK(check_count(n));
     if (!bytes) { set_error("bytes is NULL"); return TICTAC_ERR_NULL; }
     *bytes = gradient_norm_workspace(n);
     return TICTAC_OK;
@@ -173,13 +179,13 @@ try {
 
 int tictac_gradient_norm(int32_t n, const tictac_gradient *gradients, float scale, float *norm, void *workspace, size_t workspace_bytes, tictac_stream stream)
 try {
-    if (n < 0) { set_error("n = %d", n); return TICTAC_ERR_UNSUPPORTED; }
+    TT_CHECK(check_count(n));
     if (n && !gradients) { set_error("gradients is NULL"); return TICTAC_ERR_NULL; }
     TT_CHECK(check_floats("norm", norm, TICTAC_F32, true));
     if (!(fabsf(scale) < INFINITY)) { set_error("scale = %g", (double)scale); return TICTAC_ERR_UNSUPPORTED; }
     for (int32_t i = 0; i < n; ++i) {
         TT_CHECK(check_dtype("dtype of a gradient", gradients[i].dtype));
-        if (gradients[i].numel < 0 || gradients[i].numel > INT64_C(1) << 40) { set_error("gradient %d of %lld elements", i, (long long)gradients[i].numel); return TICTAC_ERR_UNSUPPORTED; }
+        if (gradients[i].numel < 0 || gradients[i].numel > INT64_C(1) << 37) { set_error("gradient %d of %lld elements", i, (long long)gradients[i].numel); return TICTAC_ERR_UNSUPPORTED; }
         TT_CHECK(check_floats("a gradient", gradients[i].g, gradients[i].dtype, gradients[i].numel > 0));
     }
     TT_CHECK(check_workspace(workspace, workspace_bytes, gradient_norm_workspace(n)));
@@ -189,7 +195,7 @@ try {
 
 int tictac_adamw_step(int32_t n, const tictac_adamw_tensor *tensors, const tictac_adamw_options *options, tictac_stream stream)
 try {
-    if (n < 0 || n >= 1 << 24) { set_error("n = %d", n); return TICTAC_ERR_UNSUPPORTED; }
+    TT_CHECK(check_count(n));
     if ((n && !tensors) || !options) { set_error("tensors or options is NULL"); return TICTAC_ERR_NULL; }
     const tictac_adamw_options &o = *options;
     const auto number = [](double v) { return fabs(v) < INFINITY; };

@@ -136,10 +136,10 @@ def test_more_refusals_and_nothing_to_do():
     assert code("tictac_linear_f8_backward_workspace", 1, 0, 10, 10, at) == 0 and n.value == 0
     assert code("tictac_linear_f8_backward_workspace", 1, 100, 10, 10, None) == -1
     assert code("tictac_gradient_norm_workspace", 3, at) == 0 and n.value >= 8
-    assert code("tictac_gradient_norm_workspace", -1, at) == -9 and code("tictac_gradient_norm_workspace", 1, None) == -1
+    assert code("tictac_gradient_norm_workspace", -1, at) == code("tictac_gradient_norm_workspace", 1 << 24, at) == -9 and code("tictac_gradient_norm_workspace", 1, None) == -1
 
 
-@pytest.mark.parametrize("changed,want", [({"n": -1}, -9), ({"list": None}, -1), ({"norm": None}, -1), ({"norm": P + 2}, -9), ({"scale": float("nan")}, -9), ({"scale": float("inf")}, -9), ({"g": None}, -1),
+@pytest.mark.parametrize("changed,want", [({"n": -1}, -9), ({"n": 1 << 24}, -9), ({"numel": (1 << 37) + 1}, -9), ({"list": None}, -1), ({"norm": None}, -1), ({"norm": P + 2}, -9), ({"scale": float("nan")}, -9), ({"scale": float("inf")}, -9), ({"g": None}, -1),
                                           ({"g": P + 2}, -9), ({"numel": -1}, -9), ({"dtype": 4}, -9), ({"workspace": None}, -1), ({"bytes": 7}, -8)])
 def test_norms_that_are_refused(changed, want):
     a = dict(n=1, list=P, scale=1.0, norm=P, workspace=P, bytes=1 << 20, g=P, numel=100, dtype=0)
