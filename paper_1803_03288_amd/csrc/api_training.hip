@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <utility>
 #include <vector>
 
 #include "api_checks.h"
@@ -209,11 +210,8 @@ try {
     TT_CHECK(check_floats("norm", o.norm, TICTAC_F32, false));
     TT_CHECK(check_floats("lr_at", o.lr_at, TICTAC_F32, false));
     if ((uintptr_t)o.step_at & 7) { set_error("step_at does not lie on a boundary of its elements"); return TICTAC_ERR_UNSUPPORTED; }
-    struct Range {
-        uintptr_t at, end;
-        bool written;
-    };
-    std::vector<Range> ranges;
+    // what is read and written: begins, and ends of which the lowest bit says whether it is written
+    std::vector<std::pair<uint64_t, uint64_t>> ranges;
     ranges.reserve((size_t)n * 7);
     for (int32_t i = 0; i < n; ++i) {
         const tictac_adamw_tensor &t = tensors[i];
@@ -225,7 +223,7 @@ try {
         TT_CHECK(check_floats("p", t.p, t.dtype, true));
         TT_CHECK(check_floats("g", t.g, t.grad_dtype, true));
         if (t.copy) TT_CHECK(check_floats("copy", t.copy, t.copy_dtype, true));
-        const auto add = [&](const void *p, int64_t bytes, bool written) { ranges.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, written}); };
+        const auto add = [&](const void *p, int64_t bytes, bool written) { ranges.emplace_back((uint64_t)(uintptr_t)p, ((uint64_t)(uintptr_t)p + (uint64_t)bytes) << 1 | written); };
         const auto size = [](int32_t dtype) { return (int64_t)elem_size(dtype); };
         if (!t.m_scale != !t.v_scale) { set_error("tensor %d: one moment in 8 bits, one in 32", i); return TICTAC_ERR_UNSUPPORTED; }
         if (t.m_scale) {
@@ -246,12 +244,13 @@ try {
         add(t.g, t.numel * size(t.grad_dtype), false);
         if (t.copy) add(t.copy, t.numel * size(t.copy_dtype), true);
     }
-    std::sort(ranges.begin(), ranges.end(), [](const Range &a, const Range &b) { return a.at < b.at; });
-    uintptr_t end = 0, written_end = 0;
-    for (const Range &r : ranges) {
-        if (r.at < written_end || (r.written && r.at < end)) { set_error("tensors overlap: what one element writes is another's"); return TICTAC_ERR_UNSUPPORTED; }
-        end = std::max(end, r.end);
-        if (r.written) written_end = std::max(written_end, r.end);
+    std::sort(ranges.begin(), ranges.end());
+    uint64_t end = 0, written_end = 0;
+    for (const auto &[at, last] : ranges) {
+        const bool written = last & 1;
+        if (at < written_end || (written && at < end)) { set_error("tensors overlap: what one element writes is another's"); return TICTAC_ERR_UNSUPPORTED; }
+        end = std::max(end, last >> 1);
+        if (written) written_end = std::max(written_end, last >> 1);
     }
     HIP_TRY(launch_adamw_step(n, tensors, o, (hipStream_t)stream));
     return TICTAC_OK;

@@ -494,11 +494,22 @@ const void *one(PyObject *o, const char *name, at::ScalarType type)
     if (t.scalar_type() != type || t.numel() != 1 || t.is_neg()) value_error(std::string(name) + ": expected one " + toString(type) + " value");
     return t.data_ptr();
 }
-int float_code(const Tensor &t, const std::string &name)
+int float_code(const Tensor &t, const char *name, Py_ssize_t i)
 {
     const int dt = dtype_code(t.scalar_type());
-    if (dt < 0) type_error(name + " is " + toString(t.scalar_type()) + ": expected float32, float16 or bfloat16");
+    if (dt < 0) type_error(nth(name, i) + " is " + toString(t.scalar_type()) + ": expected float32, float16 or bfloat16");
     return dt;
+}
+// tensor i of many on the current device, which `here` (-1 at first) remembers
+const Tensor &one_of(PyObject *from, const char *name, Py_ssize_t i, c10::DeviceIndex &here)
+{
+    if (!THPVariable_Check(from)) type_error(nth(name, i) + " is no tensor");
+    const Tensor &t = THPVariable_Unpack(from);
+    if (!t.is_cuda() || t.get_device() != here) {
+        check_device(t, nth(name, i).c_str());
+        here = (c10::DeviceIndex)t.get_device();
+    }
+    return t;
 }
 
 // (gradients, scale) -> norm
@@ -511,10 +522,10 @@ PyObject *gradient_norm(PyObject *const *arg, Py_ssize_t n)
     std::vector<Tensor> kept;
     std::vector<tictac_gradient> all;
     all.reserve(grads.size());
+    c10::DeviceIndex here = -1;
     for (Py_ssize_t i = 0; i < grads.size(); ++i) {
-        const Tensor &t = tensor(grads[i], "a gradient");
-        check_device(t, "a gradient");
-        const int dt = float_code(t, "a gradient");
+        const Tensor &t = one_of(grads[i], "grads", i, here);
+        const int dt = float_code(t, "grads", i);
         const Tensor *at = &t;                                          // (signs turned lazily, and the order of elements, do not matter)
         if (!t.is_non_overlapping_and_dense()) {
             kept.push_back(t.contiguous());
@@ -532,9 +543,9 @@ PyObject *gradient_norm(PyObject *const *arg, Py_ssize_t n)
 }
 
 // what is written in place: the version that autograd sees goes up
-void written(const Tensor &t)
+void written(c10::TensorImpl *t)
 {
-    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    if (!t->is_inference()) t->bump_version();
 }
 
 // (params, grads, moments, step, lr, (beta1, beta2), eps, weight_decay, grad_scale, norm, max_norm, copies, seed)
@@ -578,25 +589,22 @@ PyObject *adamw_step(PyObject *const *arg, Py_ssize_t n)
     o.seed = PyLong_AsUnsignedLongLongMask(arg[12]);
     if (PyErr_Occurred()) { PyErr_Clear(); type_error("seed is no whole number"); }
     std::vector<tictac_adamw_tensor> all;
-    std::vector<Tensor> kept, outputs;
+    std::vector<Tensor> kept;
+    std::vector<c10::TensorImpl *> outputs;                              // (which the arguments keep alive)
     all.reserve(count);
     outputs.reserve(count * 4);
+    c10::DeviceIndex here = -1;
     for (Py_ssize_t i = 0; i < count; ++i) {
-        const auto a_tensor = [&](PyObject *from, const char *name) -> const Tensor & {
-            if (!THPVariable_Check(from)) type_error(nth(name, i) + " is no tensor");
-            const Tensor &t = THPVariable_Unpack(from);
-            check_device(t, name);
-            return t;
-        };
+        const auto a_tensor = [&](PyObject *from, const char *name) -> const Tensor & { return one_of(from, name, i, here); };
         tictac_adamw_tensor u{};
         const Tensor &p = a_tensor(params[i], "params");
-        u.dtype = float_code(p, nth("params", i));
+        u.dtype = float_code(p, "params", i);
         if (!p.is_non_overlapping_and_dense() || p.is_neg()) value_error(nth("params", i) + " has gaps or overlaps, or its signs turned lazily: it is changed in place");
         u.p = p.data_ptr();
         u.numel = p.numel();
-        outputs.push_back(p);
+        outputs.push_back(p.unsafeGetTensorImpl());
         const Tensor &g = a_tensor(grads[i], "grads");
-        u.grad_dtype = float_code(g, nth("grads", i));
+        u.grad_dtype = float_code(g, "grads", i);
         if (g.sizes() != p.sizes()) value_error(nth("grads", i) + " has another shape than its parameter");
         if (g.strides() == p.strides() && !g.is_neg()) {
             u.g = g.data_ptr();
@@ -606,10 +614,10 @@ PyObject *adamw_step(PyObject *const *arg, Py_ssize_t n)
         }
         if (copies && (*copies)[i] != Py_None) {
             const Tensor &c = a_tensor((*copies)[i], "copies");
-            u.copy_dtype = float_code(c, nth("copies", i));
+            u.copy_dtype = float_code(c, "copies", i);
             if (c.sizes() != p.sizes() || c.strides() != p.strides() || c.is_neg()) value_error(nth("copies", i) + " has another shape or other strides than its parameter");
             u.copy = c.data_ptr();
-            outputs.push_back(c);
+            outputs.push_back(c.unsafeGetTensorImpl());
         }
         if (!PyTuple_Check(moments[i]) || PyTuple_GET_SIZE(moments[i]) != 2) type_error(nth("moments", i) + ": expected Moments");
         for (int k = 0; k < 2; ++k) {
@@ -620,22 +628,22 @@ PyObject *adamw_step(PyObject *const *arg, Py_ssize_t n)
                 if (f.rows != 1 || f.cols != u.numel || f.c.block != 1 || f.c.format != TICTAC_E4M3) value_error(nth("moments", i) + ": expected one row of " + str(u.numel) + " columns of float8_e4m3fn in blocks of one row");
                 to = f.c.q;
                 (k ? u.v_scale : u.m_scale) = f.c.scale;
-                outputs.push_back(f.q);
-                outputs.push_back(f.scale);
+                outputs.push_back(f.q.unsafeGetTensorImpl());
+                outputs.push_back(f.scale.unsafeGetTensorImpl());
             } else {
                 const Tensor &t = a_tensor(from, "moments");
                 if (t.scalar_type() != at::kFloat) type_error(nth("moments", i) + ": expected float32 or Float8");
                 if (t.numel() != u.numel || t.is_neg() || !(t.dim() == 1 ? t.is_contiguous() : t.sizes() == p.sizes() && t.strides() == p.strides()))
                     value_error(nth("moments", i) + ": expected " + str(u.numel) + " elements, in one row or with the strides of its parameter");
                 to = t.data_ptr();
-                outputs.push_back(t);
+                outputs.push_back(t.unsafeGetTensorImpl());
             }
         }
         if (!u.m_scale != !u.v_scale) value_error(nth("moments", i) + ": one in 8 bits, one in 32");
         all.push_back(u);
     }
     check(g_adamw_step((int32_t)all.size(), all.data(), &o, stream()));
-    for (const Tensor &t : outputs) written(t);
+    for (c10::TensorImpl *const t : outputs) written(t);
     Py_RETURN_NONE;
 }
 
