@@ -18,8 +18,9 @@
 namespace tictac {
 
 // ---- the norm ----
-// Squares and sums in float64: squares of float32 leave its range.  (176 tensors of 2^37 elements at most have fewer than 2^32 chunks.)  A workgroup's sum goes to the workspace, one workgroup adds those up: a fixed order, the same bits at every run.
-constexpr int kNormTensors = 176, kNormBlocks = 2048, kNormChunk = 8192;
+// Squares and sums in float64: squares of float32 leave its range.  (176 tensors of 2^37 elements at most have fewer than 2^32 chunks.)  A workgroup's sum goes to the workspace, one workgroup adds those up: a fixed order, the same bits at every run.  Up to
+// kNormOnce chunks one workgroup is all there is, and one launch (16 384 elements: 3.1 us, in two 4.4; 24 571 in three tensors 5.9 and 5.1).
+constexpr int kNormTensors = 176, kNormBlocks = 2048, kNormOnce = 2, kNormChunk = 8192;
 
 struct NormTable {
     const void *g[kNormTensors];
@@ -97,7 +98,7 @@ __device__ __forceinline__ void add_squares(const void *g, int64_t at, double &s
 
 // A workgroup has a run of chunks, which a walk through the table finds the tensors of.  67 million bfloat16 values: 26 us, 5 TB/s; 33 to 48 behind a
 // step, whose writes are still on their way.
-__global__ __launch_bounds__(256) void gradient_norm_kernel(NormTable table, double *parts)
+__global__ __launch_bounds__(256) void gradient_norm_kernel(NormTable table, double *parts, float scale, float *norm)
 {
     __shared__ double part[4];
     const uint32_t chunks = table.first[table.n];
@@ -126,7 +127,10 @@ __global__ __launch_bounds__(256) void gradient_norm_kernel(NormTable table, dou
     sum = wave_sum_f64(sum);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) parts[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
+    if (threadIdx.x != 0) return;
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
+    if (norm) *norm = (float)(sqrt(sum) * (double)scale);               // (the only workgroup)
+    else parts[blockIdx.x] = sum;
 }
 
 __global__ __launch_bounds__(256) void gradient_norm_join_kernel(const double *parts, int32_t n, float scale, float *norm)
@@ -158,8 +162,9 @@ hipError_t launch_gradient_norm(int32_t n, const tictac_gradient *g, float scale
         }
         if (table.n == 0) break;
         const uint32_t blocks = std::min<uint32_t>(table.first[table.n], kNormBlocks);
-        hipLaunchKernelGGL(gradient_norm_kernel, dim3(blocks), dim3(256), 0, s, table, workspace + parts);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        const bool once = blocks <= kNormOnce && parts == 0 && i == n;
+        hipLaunchKernelGGL(gradient_norm_kernel, dim3(once ? 1 : blocks), dim3(256), 0, s, table, workspace + parts, scale, once ? norm : nullptr);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess || once) return e;
         parts += (int32_t)blocks;
     }
     hipLaunchKernelGGL(gradient_norm_join_kernel, dim3(1), dim3(256), 0, s, workspace, parts, scale, norm);

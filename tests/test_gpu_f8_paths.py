@@ -130,17 +130,17 @@ def test_gradients(L, rows, cols, outs, dtype, block, f8, want):  # noqa: F811
         assert all(torch.equal(a, b) for a, b in zip(L.linear_f8_backward(dy, x, w, f8), got))
 
 
-@pytest.mark.parametrize("tensors", [1, 58, 59, 76, 77, 176, 177])
+@pytest.mark.parametrize("tensors", [1, 2, 3, 58, 59, 76, 77, 176, 177])
 @pytest.mark.parametrize("bits", [8, 32])
 def test_updates(L, tensors, bits):  # noqa: F811
-    """Launches by the number of tensors that one describes: the norm's 176, the step's 58 with moments in 8 bits and 76 with moments in 32; the values are those of each tensor by itself."""
+    """Launches by the number of tensors that one describes: the norm's 176, and another for their sums from three chunks on, the step's 58 with moments in 8 bits and 76 with moments in 32; the values are those of each tensor by itself."""
     g = torch.Generator(device="cuda").manual_seed(tensors)
     d = [torch.randn(1 + 300 * i % 977, generator=g, device="cuda") for i in range(tensors)]
     p, q = ([torch.ones_like(t) for t in d] for _ in range(2))
     moments, others = L.adamw_moments(p, bits), L.adamw_moments(q, bits)
     names, norm = kernels(lambda: L.gradient_norm(d))
     most = 176
-    assert sum("gradient_norm_kernel" in n for n in names) == -(-tensors // most) and sum("gradient_norm_join_kernel" in n for n in names) == 1
+    assert sum("gradient_norm_kernel" in n for n in names) == -(-tensors // most) and sum("gradient_norm_join_kernel" in n for n in names) == (tensors > 2)
     want = math.sqrt(sum(float(t.double().square().sum()) for t in d))
     assert abs(float(norm) - want) <= 2 * ref.U * want
     names, _ = kernels(lambda: L.adamw_step(p, d, moments, 3))
