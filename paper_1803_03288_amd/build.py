@@ -287,6 +287,8 @@ def build(verbose: bool = False) -> str:
         found = list(jobs.map(compiled, sorted(sources(), key=os.path.getsize, reverse=True)))
         for source, check in checks.items():
             if check.result():
+                if os.path.exists(LIB):
+                    os.remove(LIB)
                 raise RuntimeError(f"{source}: what is written by hand no longer matches the generated code:\n  " + "\n  ".join(check.result()))
         subprocess.check_call([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + sorted(found))
     build_layers(verbose)
