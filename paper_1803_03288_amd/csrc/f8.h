@@ -47,17 +47,22 @@ __device__ __forceinline__ uint2 f8_nans(int64_t left)
     const uint64_t all = left <= 0 ? 0 : 0x7f7f7f7f7f7f7f7full >> (8 * (8 - (left < 8 ? left : 8)));
     return uint2{(uint32_t)all, (uint32_t)(all >> 32)};
 }
-// Eight values of a block in 8 bits, without a branch: the kernels that turn operands round hold dozens of these, and what they wait for is their code.
+// Values of a block in 8 bits, without a branch: the kernels that turn operands round hold dozens of these, and what they wait for is their code.
 template <int FORMAT>
-__device__ __forceinline__ uint2 f8_quantized8(const float *v, uint32_t scale, uint2 nans)
+__device__ __forceinline__ uint32_t f8_quantized4(const float *v, uint32_t scale, uint32_t nans)
 {
     constexpr uint32_t kTop = FORMAT == TICTAC_E5M2 ? 16 : 9;
     const float inv = f8_inverse(scale), most = scale >= 256 - kTop ? (FORMAT == TICTAC_E5M2 ? 28672.0f : 240.0f) : (FORMAT == TICTAC_E5M2 ? 57344.0f : 448.0f);
-    float u[8];
+    float u[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -most, most);        // (2^128 is out of float32's range)
-    const uint2 q{f8_pack4<FORMAT>(u[0], u[1], u[2], u[3]), f8_pack4<FORMAT>(u[4], u[5], u[6], u[7])};
+    for (int i = 0; i < 4; ++i) u[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -most, most);        // (2^128 is out of float32's range)
+    const uint32_t q = f8_pack4<FORMAT>(u[0], u[1], u[2], u[3]);
     return scale == 255 ? nans : q;
+}
+template <int FORMAT>
+__device__ __forceinline__ uint2 f8_quantized8(const float *v, uint32_t scale, uint2 nans)
+{
+    return uint2{f8_quantized4<FORMAT>(v, scale, nans.x), f8_quantized4<FORMAT>(v + 4, scale, nans.y)};
 }
 __device__ __forceinline__ void f8_values8(uint2 q, uint32_t scale, int format, float *v)
 {
@@ -69,12 +74,15 @@ __device__ __forceinline__ void f8_values8(uint2 q, uint32_t scale, int format, 
 }
 
 // Values of an 8-bit type times a power of two as bf16: exact (what falls below bf16's range becomes zero).
+__device__ __forceinline__ uint2 f8_bf16_4(const float *v)
+{
+    const auto two = [](float a, float b) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302); };
+    return uint2{two(v[0], v[1]), two(v[2], v[3])};
+}
 __device__ __forceinline__ i32x4 f8_bf16(const float *v)
 {
-    i32x4 r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (int32_t)__builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, v[2 * e + 1]), __builtin_bit_cast(uint32_t, v[2 * e]), 0x07060302);
-    return r;
+    const uint2 lo = f8_bf16_4(v), hi = f8_bf16_4(v + 4);
+    return i32x4{(int32_t)lo.x, (int32_t)lo.y, (int32_t)hi.x, (int32_t)hi.y};
 }
 
 // An operand: blocks of `1 << shift` rows.

@@ -61,32 +61,34 @@ __global__ __launch_bounds__(256) void quantize_f8_kernel(F8QuantizeArgs p, int6
     quantize_blocks<DT, WIDE, FORMAT, false>(p, blocks, total, blockIdx.x, gridDim.x);
 }
 
-// The tile that a workgroup of 256 has: thread t has rows 8 (t / 16) .. + 7 and columns 8 (t % 16) .. + 7 of 128 x 128.
+// The tile of 128 x 128 that a workgroup has: thread t has rows N (t / 16) .. + N - 1 and columns 8 (t % 16) .. + 7 of it.
+template <int N>
 struct Tile128 {
+    static constexpr int kThreads = 128 / N * 16;
     int lane, group;
     int64_t r, c;               // of the thread's first element
-    __device__ __forceinline__ Tile128(int64_t tile_r, int64_t tile_c) : lane(threadIdx.x & 15), group(threadIdx.x >> 4), r(tile_r * 128 + group * 8), c(tile_c * 128 + lane * 8) {}
+    __device__ __forceinline__ Tile128(int64_t tile_r, int64_t tile_c) : lane(threadIdx.x & 15), group(threadIdx.x >> 4), r(tile_r * 128 + group * N), c(tile_c * 128 + lane * 8) {}
 };
 
 // (rows and, with WIDE, columns behind the end: the last again, made zeros, so that all loads are under way at once)
-template <int DT, bool WIDE>
-__device__ __forceinline__ void load_tile(const void *x, int64_t ld, int64_t rows, int64_t cols, const Tile128 &t, typename Elem<DT>::raw (&raw)[8])
+template <int DT, bool WIDE, int N>
+__device__ __forceinline__ void load_tile(const void *x, int64_t ld, int64_t rows, int64_t cols, const Tile128<N> &t, typename Elem<DT>::raw (&raw)[N])
 {
     using E = Elem<DT>;
     const typename E::type *const from = (const typename E::type *)x;
     if (WIDE || t.c + 8 <= cols) {
         const int64_t c = WIDE ? min(t.c, cols - 8) : t.c;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             const typename E::type *const at = from + min(t.r + e, rows - 1) * ld + c;
             raw[e] = WIDE ? E::load(at) : load_anywhere<DT>(at);
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) raw[e] = load8<DT, false>(from + min(t.r + e, rows - 1) * ld, t.c, cols);
+        for (int e = 0; e < N; ++e) raw[e] = load8<DT, false>(from + min(t.r + e, rows - 1) * ld, t.c, cols);
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < N; ++e)
         if (t.r + e >= rows || (WIDE && t.c >= cols)) raw[e] = typename E::raw{};
 }
 
@@ -97,9 +99,9 @@ __global__ __launch_bounds__(256) void quantize_f8_tiles_kernel(F8QuantizeArgs p
     using E = Elem<DT>;
     __shared__ uint32_t part[4];
     const uint32_t tile_r = blockIdx.x / across, tile_c = blockIdx.x % across;
-    const Tile128 t(tile_r, tile_c);
+    const Tile128<8> t(tile_r, tile_c);
     typename E::raw raw[8];
-    load_tile<DT, WIDE>(p.x, p.ld_x, p.rows, p.cols, t, raw);
+    load_tile<DT, WIDE, 8>(p.x, p.ld_x, p.rows, p.cols, t, raw);
     uint32_t m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -223,29 +225,30 @@ hipError_t launch_widen_f8(const F8QuantizeArgs &x, const F8QuantizeArgs &w, hip
 // ---- the operands of a backward pass ----
 // A workgroup has a tile of 128 x 128 of dy, of x or of w as floats in registers; blocks of its rows are maxima over 16 lanes, those of its columns meet in LDS, through which they are
 // turned round too, so that reads and writes are whole lines.  BF16: the values that 8 bits keep, as bf16.  Bound by memory where there is much: the operands of 8192 x 4096 -> 16384
-// bfloat16 take 139 us, 5.4 TB/s; small ones by one trip there and three barriers, 7.4 us.
+// bfloat16 take 139 us, 5.4 TB/s; small ones by one trip there and three barriers, 7 us.
+template <int N>
 struct TurnRoom {
-    uint32_t part[16][128];             // maxima, sums
+    uint32_t part[128 / N][128];        // maxima, sums
     uint8_t scale[128];
 };
 
-// v: 8 x 8 of a tile; the blocks of its columns go to `to`, [columns][ld], in the format
-template <bool BF16, int FORMAT>
-__device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8][8], int64_t rows, int64_t cols, int64_t tile_r, int64_t tile_c, const F8Operand &to,
-                                            TurnRoom &room, char *turned)
+// v: N x 8 of a tile; the blocks of its columns go to `to`, [columns][ld], in the format
+template <bool BF16, int FORMAT, int N>
+__device__ __forceinline__ void put_columns(const Tile128<N> &t, const float (&v)[N][8], int64_t rows, int64_t cols, int64_t tile_r, int64_t tile_c, const F8Operand &to,
+                                            TurnRoom<N> &room, char *turned)
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         uint32_t m = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = max(m, magnitude(v[e][i]));
+        for (int e = 0; e < N; ++e) m = max(m, magnitude(v[e][i]));
         room.part[t.group][t.lane * 8 + i] = m;
     }
     __syncthreads();
     if (threadIdx.x < 128) {
         uint32_t m = 0;
 #pragma unroll
-        for (int g = 0; g < 16; ++g) m = max(m, room.part[g][threadIdx.x]);
+        for (int g = 0; g < 128 / N; ++g) m = max(m, room.part[g][threadIdx.x]);
         const uint32_t scale = f8_scale(m, FORMAT);
         room.scale[threadIdx.x] = (uint8_t)scale;
         const int64_t c = tile_c * 128 + threadIdx.x;
@@ -256,23 +259,36 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
     // Eight rows of a column are one piece; piece g of column c lies at place g ^ c / 8 of its 16: a wave's stores and loads then meet all banks alike.
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float u[8];
+        float u[N];
         const uint32_t scale = room.scale[t.lane * 8 + i];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = v[e][i];
-        const uint2 q = f8_quantized8<FORMAT>(u, scale, nans);
-        const int at = (t.lane * 8 + i) * 16 + (t.group ^ t.lane);
-        if (BF16) {
-            f8_values8(q, scale, FORMAT, u);
-            *(i32x4 *)(turned + at * 16) = f8_bf16(u);
-        } else {
-            *(uint2 *)(turned + at * 8) = q;
+        for (int e = 0; e < N; ++e) u[e] = v[e][i];
+        const int at = (t.lane * 8 + i) * 16 + ((t.group * N / 8) ^ t.lane);
+        if constexpr (N == 8) {
+            const uint2 q = f8_quantized8<FORMAT>(u, scale, nans);
+            if (BF16) {
+                f8_values8(q, scale, FORMAT, u);
+                *(i32x4 *)(turned + at * 16) = f8_bf16(u);
+            } else {
+                *(uint2 *)(turned + at * 8) = q;
+            }
+        } else {                                                        // (half a piece)
+            const uint32_t q = f8_quantized4<FORMAT>(u, scale, nans.x);
+            if (BF16) {
+                f8_values4(q, FORMAT, u);
+                const float s = f8_factor(scale);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] *= s;
+                *(uint2 *)(turned + at * 16 + (t.group & 1) * 8) = f8_bf16_4(u);
+            } else {
+                *(uint32_t *)(turned + at * 8 + (t.group & 1) * 4) = q;
+            }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < (BF16 ? 8 : 4); ++k) {
-        const int n = k * 256 + threadIdx.x, c = n / (BF16 ? 16 : 8), piece = n % (BF16 ? 16 : 8), lane = c >> 3;
+    for (int k = 0; k < (BF16 ? N : N / 2); ++k) {
+        const int n = k * Tile128<N>::kThreads + threadIdx.x, c = n / (BF16 ? 16 : 8), piece = n % (BF16 ? 16 : 8), lane = c >> 3;
         if (tile_c * 128 + c >= cols) continue;
         if (BF16) {
             *(i32x4 *)((uint16_t *)to.q + (tile_c * 128 + c) * to.ld + tile_r * 128 + piece * 8) = *(const i32x4 *)(turned + (c * 16 + (piece ^ lane)) * 16);
@@ -283,28 +299,28 @@ __device__ __forceinline__ void put_columns(const Tile128 &t, const float (&v)[8
     }
 }
 
-template <int DT, bool WIDE, int FORMAT>
-__global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_tiles, uint32_t x_tiles)
+template <int DT, bool WIDE, int FORMAT, int N>
+__global__ __launch_bounds__(Tile128<N>::kThreads) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_tiles, uint32_t x_tiles)
 {
     using E = Elem<DT>;
     constexpr bool BF16 = DT == TICTAC_F32;
-    __shared__ TurnRoom room;
+    __shared__ TurnRoom<N> room;
     __shared__ __align__(16) char turned[128 * 16 * (BF16 ? 16 : 8)];
     uint32_t unit = blockIdx.x;
-    float v[8][8];
+    float v[N][8];
     if (unit < dy_tiles) {
         const uint32_t across = (uint32_t)((p.outs + 127) / 128), tile_r = unit / across, tile_c = unit % across;
-        const Tile128 t(tile_r, tile_c);
+        const Tile128<N> t(tile_r, tile_c);
         {
-            typename E::raw raw[8];
-            load_tile<DT, WIDE>(p.dy, p.ld_dy, p.rows, p.outs, t, raw);
+            typename E::raw raw[N];
+            load_tile<DT, WIDE, N>(p.dy, p.ld_dy, p.rows, p.outs, t, raw);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) E::floats(raw[e], v[e]);
+            for (int e = 0; e < N; ++e) E::floats(raw[e], v[e]);
         }
         if (p.dy_rows.q) {
             const uint2 nans = f8_nans(p.outs - t.c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < N; ++e) {
                 uint32_t m = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) m = max(m, magnitude(v[e][i]));
@@ -327,7 +343,7 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_
             for (int i = 0; i < 8; ++i) {
                 float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum += v[e][i];
+                for (int e = 0; e < N; ++e) sum += v[e][i];
                 room.part[t.group][t.lane * 8 + i] = __builtin_bit_cast(uint32_t, sum);
             }
             __syncthreads();
@@ -335,12 +351,12 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_
             if (threadIdx.x < 128 && c < p.outs) {
                 float sum = 0.0f;
 #pragma unroll
-                for (int g = 0; g < 16; ++g) sum += __builtin_bit_cast(float, room.part[g][threadIdx.x]);
+                for (int g = 0; g < 128 / N; ++g) sum += __builtin_bit_cast(float, room.part[g][threadIdx.x]);
                 p.sums[tile_r * p.outs + c] = sum;
             }
             __syncthreads();
         }
-        if (p.dy_cols.q) put_columns<BF16, FORMAT>(t, v, p.rows, p.outs, tile_r, tile_c, p.dy_cols, room, turned);
+        if (p.dy_cols.q) put_columns<BF16, FORMAT, N>(t, v, p.rows, p.outs, tile_r, tile_c, p.dy_cols, room, turned);
         return;
     }
     unit -= dy_tiles;
@@ -349,22 +365,26 @@ __global__ __launch_bounds__(256) void turn_f8_kernel(F8TurnArgs p, uint32_t dy_
     const F8Rows &from = is_x ? p.x : p.w;
     const int64_t rows = is_x ? p.rows : p.outs;
     const uint32_t across = (uint32_t)((p.cols + 127) / 128), tile_r = unit / across, tile_c = unit % across;
-    const Tile128 t(tile_r, tile_c);
-    uint2 q[8];
-    uint32_t scale[8];
+    const Tile128<N> t(tile_r, tile_c);
+    uint2 q[N];
+    uint32_t scale[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < N; ++e) {
         const int64_t row = min(t.r + e, rows - 1);
         q[e] = *(const uint2 *)(from.q + row * from.ld + t.c);
         scale[e] = from.scale[(row >> from.shift) * from.ld_scale + tile_c];
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < N; ++e) {
         const bool in = t.r + e < rows;
         f8_values8(uint2{in ? q[e].x : 0, in ? q[e].y : 0}, in ? scale[e] : 127, from.format, v[e]);
     }
-    put_columns<BF16, TICTAC_E4M3>(t, v, rows, p.cols, tile_r, tile_c, is_x ? p.x_cols : p.w_cols, room, turned);
+    put_columns<BF16, TICTAC_E4M3, N>(t, v, rows, p.cols, tile_r, tile_c, is_x ? p.x_cols : p.w_cols, room, turned);
 }
+
+// Up to a tile per compute unit by workgroups of 512: what bounds them is each wave's own code.  (us of a gradient by 512 and by 256: 30 x 300 -> 200 bfloat16 9.7 and 10.5, 64 x 1024 -> 1000 11.9 and
+// 12.5, 8192 x 4096 -> 4096 247 and 243.)
+constexpr int64_t kFewTurns = 256;
 
 template <int DT, bool WIDE>
 static hipError_t turn(const F8TurnArgs &p, hipStream_t s)
@@ -372,8 +392,10 @@ static hipError_t turn(const F8TurnArgs &p, hipStream_t s)
     const int64_t dy = p.dy_rows.q || p.dy_cols.q || p.sums ? f8_blocks(p.rows) * f8_blocks(p.outs) : 0, x = p.x_cols.q ? f8_blocks(p.rows) * f8_blocks(p.cols) : 0,
                   w = p.w_cols.q ? f8_blocks(p.outs) * f8_blocks(p.cols) : 0;
     if (dy + x + w == 0) return hipSuccess;
-    const auto kernel = p.format == TICTAC_E5M2 ? turn_f8_kernel<DT, WIDE, TICTAC_E5M2> : turn_f8_kernel<DT, WIDE, TICTAC_E4M3>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(dy + x + w)), dim3(256), 0, s, p, (uint32_t)dy, (uint32_t)x);
+    const bool few = dy + x + w <= kFewTurns;
+    const auto kernel = p.format == TICTAC_E5M2 ? (few ? turn_f8_kernel<DT, WIDE, TICTAC_E5M2, 4> : turn_f8_kernel<DT, WIDE, TICTAC_E5M2, 8>)
+                                                : (few ? turn_f8_kernel<DT, WIDE, TICTAC_E4M3, 4> : turn_f8_kernel<DT, WIDE, TICTAC_E4M3, 8>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(dy + x + w)), dim3(few ? 512 : 256), 0, s, p, (uint32_t)dy, (uint32_t)x);
     return hipGetLastError();
 }
 hipError_t launch_turn_f8(const F8TurnArgs &p, hipStream_t s) { return BY_TYPE(p.dtype, wide_rows(p.dy, p.dtype, p.ld_dy, p.outs), turn, p, s); }

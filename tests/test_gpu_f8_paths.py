@@ -120,6 +120,10 @@ def test_gradients(L, rows, cols, outs, dtype, block, f8, want):  # noqa: F811
     dy = random(g, rows, outs, dtype, 0.01)
     print(rows, cols, outs, dtype, flush=True)
     names, got = kernels(lambda: L.linear_f8_backward(dy, x, w, f8))
+    up = lambda n: -(-n // 128)  # noqa: E731
+    tiles = up(rows) * (up(outs) + up(cols)) + (0 if any(DX in w for w in want) else up(outs) * up(cols))
+    turns = next(n for n in names if "turn_f8_kernel" in n)
+    assert turns.endswith(", 4>" if tiles <= 256 else ", 8>"), (turns, tiles)
     ran(names, ["turn_f8_kernel"] + named(want, dtype, f8))
     close(got[0], *ref.product(operand(L.quantize_f8(dy, 1, f8)), turned(L, w), dtype != F32), dtype)
     close(got[1], *ref.product(operand(L.quantize_f8(dy.t().contiguous(), 1, f8)), turned(L, x), dtype != F32), dtype)
