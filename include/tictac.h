@@ -451,7 +451,8 @@ int tictac_gradient_norm(int32_t n, const tictac_gradient *gradients, float scal
  *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g g
  *     p = p (1 - lr weight_decay) - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * in float32, p and copy rounded to their types.  Moments in 32 bits: float32 m and v, m_scale and v_scale NULL.  In 8 bits: m and sqrt(v) as one row each of numel columns of e4m3 in
- * blocks (above), rounded at random: with 16 bits u of a hash, steps = floor(|x| / step + u / 2^16).  The hash of element i of the tensor with index j of the call is
+ * blocks (above), rounded at random: with 16 bits u of a hash, steps = floor(|x| / step + u / 2^16), for a positive sqrt(v) one at least.  (Steps are 2^-9 of the scale at the lower end:
+ * elements whose sqrt(v) is below 2^-17 of the largest of its block of 128 count as of such a size, and move less than with moments in 32 bits.)  The hash of element i of the tensor with index j of the call is
  *     mix(mix(mix(mix(mix(seed low) + seed high) + step) + j) + i),   mix(x): x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0x6A09E667, x ^= x >> 16
  * in 32 bits, its low half for m, its high half for sqrt(v): the same call has the same result.
  * norm may be NULL (max_norm is not used then); where *norm is not finite nothing is changed.  lr_at and step_at, device, may be NULL; they stand for lr and step, for

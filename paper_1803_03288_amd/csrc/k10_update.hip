@@ -4,7 +4,8 @@
 //   p' = p (1 - lr decay) - lr / (1 - b1^t) m' / (sqrt(v') / sqrt(1 - b2^t) + eps)
 // all in float32, each product and sum rounded by itself, so that moments in 8 bits do not depend on what a compiler contracts.  Moments in 8 bits are rows of e4m3 (f8.h) of m and
 // of r = sqrt(v), which the update needs anyway: the range of r is half of v's in powers of two.  They are rounded at random, up with a probability of the part that is cut off: with
-// b2 = 0.999 v decays by 0.1 % a step, and to nearest would never leave a value whose neighbours are 6 to 12 % away.
+// b2 = 0.999 v decays by 0.1 % a step, and to nearest would never leave a value whose neighbours are 6 to 12 % away.  A positive r is a step of the type at least: it divides, and where it became zero
+// the next step would have only 1 - b2 of a gradient's square under an m of up to a whole step (elements 2^-17 of their block's largest moved by up to 500 lr in a step; now by up to 4).
 // Bound by memory: an element is read and written once.  67 million parameters with moments in 8 bits: 194 to 227 us, 4.8 to 5.6 TB/s.
 #include <math.h>
 
@@ -216,14 +217,14 @@ struct UpdateFactors {
     uint32_t key;
 };
 
-// `x` (a moment) in e4m3 under the scale of its block, up or down by 16 random bits: how many steps it is from zero, plus a part of a step, cut off.
-__device__ __forceinline__ float f8_at_random(float x, float inv, uint32_t bits)
+// `x` (a moment) in e4m3 under the scale of its block, up or down by 16 random bits: how many steps it is from zero, plus a part of a step, cut off; no fewer than `least`.
+__device__ __forceinline__ float f8_at_random(float x, float inv, uint32_t bits, float least)
 {
 #pragma clang fp contract(off)
     const float y = x * inv, a = fabsf(y);
     // the exponent of the step: that of a, from -6 on, less 3
     const int32_t e = max((int32_t)(__builtin_bit_cast(uint32_t, a) >> 23) - 127, -6) - 3;
-    const float k = floorf(a * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23) + (float)bits * 0x1p-16f);
+    const float k = fmaxf(floorf(a * __builtin_bit_cast(float, (uint32_t)(127 - e) << 23) + (float)bits * 0x1p-16f), least);
     return copysignf(k * __builtin_bit_cast(float, (uint32_t)(127 + e) << 23), y);
 }
 
@@ -300,8 +301,8 @@ __device__ __forceinline__ void update8(const UpdateRates &table, const UpdateTe
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t bits = mixed(f.key + (uint32_t)(at + i));
-            m[i] = f8_at_random(m[i], im, bits & 0xffff);
-            r[i] = f8_at_random(r[i], ir, bits >> 16);
+            m[i] = f8_at_random(m[i], im, bits & 0xffff, 0.0f);
+            r[i] = f8_at_random(r[i], ir, bits >> 16, r[i] > 0.0f ? 1.0f : 0.0f);
         }
         const auto put8 = [&](void *to, uint8_t *scales, uint32_t scale, const float *y) {
             uint2 q{f8_pack4<TICTAC_E4M3>(y[0], y[1], y[2], y[3]), f8_pack4<TICTAC_E4M3>(y[4], y[5], y[6], y[7])};

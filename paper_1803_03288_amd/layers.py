@@ -164,7 +164,8 @@ def linear_f8_backward(dy: torch.Tensor, x: Float8, w: Float8, grad_dtype: torch
 
 class Moments(NamedTuple):
     """Moments of one parameter, in the order in which its elements lie in memory: float32 ``m`` and ``v`` of its number of elements; or in 8 bits ``m`` and the root of
-    ``v``, each a ``Float8`` of one row, blocks of one row, float8_e4m3fn."""
+    ``v``, each a ``Float8`` of one row, blocks of one row, float8_e4m3fn.  The root of an element whose gradients are not zero is a step of the type at least: elements whose root is below 2^-17 of the
+    largest among their 128 neighbours count as of that size, and move less than with moments in 32 bits."""
     m: Union[torch.Tensor, Float8]
     v: Union[torch.Tensor, Float8]
 

@@ -119,6 +119,12 @@ def at_random(x, bits):
     return torch.copysign(torch.floor(t).double() * step, y)[:n], byte[0]
 
 
+def root_at_random(x, bits):
+    """The same for the root of the second moment: a positive one is a step of the type at least (the last, 2^-9 of the scale; larger values have eight steps and more)."""
+    q, byte = at_random(x, bits)
+    return torch.where((q == 0) & (x > 0), torch.full_like(q, 2.0 ** -9), q), byte
+
+
 def adamw(p, g, m, v, step, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2):
     """New (p, m, v) in float64."""
     b1, b2 = betas
