@@ -456,7 +456,7 @@ int tictac_gradient_norm(int32_t n, const tictac_gradient *gradients, float scal
  *     mix(mix(mix(mix(mix(seed low) + seed high) + step) + j) + i),   mix(x): x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0x6A09E667, x ^= x >> 16
  * in 32 bits, its low half for m, its high half for sqrt(v): the same call has the same result.
  * norm may be NULL (max_norm is not used then); where *norm is not finite nothing is changed.  lr_at and step_at, device, may be NULL; they stand for lr and step, for
- * calls that are captured.  step counts from 1.  Tensors may not overlap (TICTAC_ERR_UNSUPPORTED); fewer than 2^24 of at most 2^32 elements each. */
+ * calls that are captured.  step counts from 1.  Tensors may not overlap, nor norm, lr_at and step_at what is written (TICTAC_ERR_UNSUPPORTED); fewer than 2^24 of at most 2^32 elements each. */
 typedef struct tictac_adamw_tensor {
     void *p;                       /* device, contiguous, of dtype, as all of these */
     const void *g;                 /* of grad_dtype */

@@ -212,7 +212,12 @@ try {
     if ((uintptr_t)o.step_at & 7) { set_error("step_at does not lie on a boundary of its elements"); return TICTAC_ERR_UNSUPPORTED; }
     // what is read and written: begins, and ends of which the lowest bit says whether it is written
     std::vector<std::pair<uint64_t, uint64_t>> ranges;
-    ranges.reserve((size_t)n * 7);
+    ranges.reserve((size_t)n * 7 + 3);
+    const auto add = [&](const void *p, int64_t bytes, bool written) { ranges.emplace_back((uint64_t)(uintptr_t)p, ((uint64_t)(uintptr_t)p + (uint64_t)bytes) << 1 | written); };
+    // (every workgroup reads these when it starts, behind others' ends)
+    if (o.norm) add(o.norm, sizeof(*o.norm), false);
+    if (o.lr_at) add(o.lr_at, sizeof(*o.lr_at), false);
+    if (o.step_at) add(o.step_at, sizeof(*o.step_at), false);
     for (int32_t i = 0; i < n; ++i) {
         const tictac_adamw_tensor &t = tensors[i];
         TT_CHECK(check_dtype("dtype", t.dtype));
@@ -223,7 +228,6 @@ try {
         TT_CHECK(check_floats("p", t.p, t.dtype, true));
         TT_CHECK(check_floats("g", t.g, t.grad_dtype, true));
         if (t.copy) TT_CHECK(check_floats("copy", t.copy, t.copy_dtype, true));
-        const auto add = [&](const void *p, int64_t bytes, bool written) { ranges.emplace_back((uint64_t)(uintptr_t)p, ((uint64_t)(uintptr_t)p + (uint64_t)bytes) << 1 | written); };
         const auto size = [](int32_t dtype) { return (int64_t)elem_size(dtype); };
         if (!t.m_scale != !t.v_scale) { set_error("tensor %d: one moment in 8 bits, one in 32", i); return TICTAC_ERR_UNSUPPORTED; }
         if (t.m_scale) {

@@ -200,6 +200,6 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], mo
     ``grad_scale``; where it is not finite, nothing is changed.  Parameters and gradients may each be float32, float16 or bfloat16; arithmetic is float32.  ``copies`` receive
     the new parameters in their own types, for parameters in float32 with layers that take 16 bits.  ``step`` counts from 1; it and ``lr`` may be tensors of one element
     on the device (int64, float32), which are read when the step runs, so that a captured one goes on.  Moments in 8 bits are rounded at random by a hash of ``seed``,
-    ``step``, the index in ``params`` and the element's: the same call has the same result.  Tensors may not overlap.  Parameters may have any strides without gaps; gradients
+    ``step``, the index in ``params`` and the element's: the same call has the same result.  Tensors may not overlap, and ``norm``, ``lr`` and ``step`` may not lie in what is written.  Parameters may have any strides without gaps; gradients
     in another order are copied first."""
     (_module or _native()).adamw_step(params, grads, moments, step, lr, betas, eps, weight_decay, grad_scale, norm, max_norm, copies, seed)
