@@ -187,10 +187,10 @@ class Update:
         self.lr = torch.full((1,), lr, device=it.x.device)
 
     def run(self, grads: List[Layer], op: Callable = lambda name, call: call()):
-        """Takes one step; the norm that the gradients had."""
+        """Takes one step, where the gradients' norm is finite; that norm."""
         ly, flat = self.it.layers, [t for d in grads for t in d]
         norm = op("update.norm", lambda: ly.gradient_norm(flat))
-        self.step.add_(1)
+        self.step.add_(norm < math.inf)                     # (a step that changes nothing is not counted)
         op("update.step", lambda: ly.adamw_step(self.params, flat, self.moments, self.step, lr=self.lr, norm=norm, max_norm=self.max_norm))
         op("update.weights", self.it.refresh)
         return norm
