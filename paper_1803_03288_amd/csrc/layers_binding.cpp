@@ -353,7 +353,7 @@ struct Float8 {
     int64_t rows, cols;
     tictac_float8 c;
 };
-// scales whose rows do not start on 4-byte boundaries, or end before the next, are copied, but where they will be written
+// scales whose rows do not start on 4-byte boundaries, end before the next or lie on each other (one row for all) are copied, but where they will be written
 Float8 float8(PyObject *o, const char *name, const at::Device *device, bool written = false)
 {
     if (!is_rows8(o)) type_error(std::string(name) + ": expected Float8");
@@ -373,7 +373,7 @@ Float8 float8(PyObject *o, const char *name, const at::Device *device, bool writ
     const int64_t up = (r.rows + block - 1) / block, along = padded(r.cols) / kGroup;
     if (r.scale.size(0) != up || r.scale.size(1) < along)
         value_error(std::string(name) + ": scales of " + str(r.scale.size(0)) + " x " + str(r.scale.size(1)) + " blocks, expected " + str(up) + " x " + str(along));
-    const bool as_is = r.scale.stride(1) == 1 && r.scale.size(1) >= scales_of(r.cols) && (up <= 1 || r.scale.stride(0) % 4 == 0) && ((uintptr_t)r.scale.data_ptr() & 3) == 0;
+    const bool as_is = r.scale.stride(1) == 1 && r.scale.size(1) >= scales_of(r.cols) && (up <= 1 || (r.scale.stride(0) % 4 == 0 && r.scale.stride(0) >= scales_of(r.cols))) && ((uintptr_t)r.scale.data_ptr() & 3) == 0;
     if (!as_is) {
         if (written) value_error(std::string(name) + ": scales lie on 4-byte boundaries, " + str(scales_of(r.cols)) + " of them");
         Tensor to = at::zeros({up, scales_of(r.cols)}, r.scale.options().dtype(at::kByte));

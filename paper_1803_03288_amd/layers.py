@@ -122,7 +122,7 @@ def linear_q8_backward(dy: torch.Tensor, x: Rows8, w: Rows8):
 class Float8(NamedTuple):
     """8-bit floats in blocks: the values ``q * scale`` of ``[rows][cols]``.  ``q`` is float8_e4m3fn or float8_e5m2 ``[rows][ld]``, ``ld`` a multiple of 128, zeros behind
     column ``cols``; a block is 128 columns of ``block`` rows, 1 or 128; ``scale`` is float8_e8m0fnu (powers of two) ``[ceil(rows / block)][ceil(cols / 128)]``,
-    rounded up to a multiple of four in the last dimension (scales that are not, or whose rows do not start on 4-byte boundaries, are copied in each call)."""
+    rounded up to a multiple of four in the last dimension (scales that are not, or whose rows do not start on 4-byte boundaries or lie on each other, are copied in each call)."""
     q: torch.Tensor
     scale: torch.Tensor
     cols: int
