@@ -430,7 +430,7 @@ int tictac_linear_f8(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, co
  *   dw[o][i] = sum_t B[t][o] X[t][i]    B: dy in `format`, blocks of 128 rows of a column; X: x8, in blocks of 128 rows of a column
  *   db[o] = sum_t dy[t][o]
  * W and X are rounded again, to e4m3: W is w itself where its blocks are of 128 rows, and else, as X, what scales of powers of two let differ (values that
- * get 2^-15 of a block's largest or less).  Sums as in tictac_linear_f8.  x8 is read for dw alone, w for dx alone. */
+ * get 2^-14 of a block's largest or less).  Sums as in tictac_linear_f8.  x8 is read for dw alone, w for dx alone. */
 int tictac_linear_f8_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, size_t *bytes);
 int tictac_linear_f8_backward(int32_t dtype, int64_t rows, int64_t cols, int64_t outs, const void *dy, int64_t ld_dy, int32_t format, const tictac_float8 *x8,
                               const tictac_float8 *w, void *dx, int64_t ld_dx, void *dw, int64_t ld_dw, void *db, void *workspace, size_t workspace_bytes,

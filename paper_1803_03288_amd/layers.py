@@ -155,7 +155,7 @@ def linear_f8(x: Union[torch.Tensor, Float8], w: Float8, bias: Optional[torch.Te
 def linear_f8_backward(dy: torch.Tensor, x: Float8, w: Float8, grad_dtype: torch.dtype = torch.float8_e4m3fn):
     """``(dx, dw, db)`` of ``linear_f8`` from the 8-bit operands that the forward pass took, all of the type of ``dy``; the rounding of the input counts as the
     identity.  ``dy`` is rounded to ``grad_dtype`` (float8_e4m3fn, or float8_e5m2 for a wider range) in blocks of 128 along what is summed over: its outputs for dx, its
-    rows for dw; ``x``, and ``w`` where its blocks are of one row, are rounded again to float8_e4m3fn in such blocks, which changes only values of 2^-15 of a block's
+    rows for dw; ``x``, and ``w`` where its blocks are of one row, are rounded again to float8_e4m3fn in such blocks, which changes only values of 2^-14 of a block's
     largest and less.  ``db`` is of ``dy`` itself.  Sums as in ``linear_f8``.  A NaN or an infinity in ``dy`` makes its row of dx and the rows of dw that its block reaches NaN."""
     return (_module or _native()).linear_f8_backward(dy, x, w, grad_dtype)
 
