@@ -79,3 +79,15 @@ def test_the_least_root(L, betas):  # noqa: F811
             assert torch.equal(of.q.cpu()[0, :n].double(), q) and not of.q.cpu().view(torch.uint8)[0, n:].any()
         assert torch.equal(moments[0].v.q.cpu()[0, :n].double() == 0, r == 0)
     assert below > 1000                                     # (there were such roots)
+
+
+@pytest.mark.parametrize("tensors", [58, 59])
+def test_every_tensor_of_full_launches(L, tensors):  # noqa: F811
+    """Moments of zeros: a step's new parameters do not depend on random bits, so each tensor's are what it gets by itself."""
+    g = torch.Generator(device="cuda").manual_seed(tensors)
+    d = [torch.randn(1 + 300 * i % 977, generator=g, device="cuda") for i in range(tensors)]
+    p, q = ([torch.ones_like(t) for t in d] for _ in range(2))
+    L.adamw_step(p, d, L.adamw_moments(p, 8), 3)
+    for a, b, t in zip(p, q, d):
+        L.adamw_step([b], [t], L.adamw_moments([b], 8), 3)
+        assert torch.equal(a, b) and not torch.equal(a, torch.ones_like(a))
