@@ -141,10 +141,9 @@ __device__ __forceinline__ void tile_of(int32_t block, int32_t tiles_r, int32_t 
 // The loads of a tile.  A load brings 8 rows of 128 bytes to LDS, lane l the sixteen bytes that belong at place l % 8 of row l / 8.  Place j of row i
 // holds the bytes 16 (j ^ i % 8) ..: eight rows of one k then lie in all banks.  Rows behind the end are the last row again; nobody
 // stores what comes of them.
-// ORDER 1: rows of p go to the places that suit the reads of product_kernel_256, j ^ (i % 4 + 4 (i / 8 % 2)).  LDS serves sixteen-byte reads sixteen lanes at a time, from 64 banks: lanes 0-3,
-// 12-15, 20-23 and 24-27, then 4-7, 8-11, 16-19 and 28-31.  Where the first 32 lanes read 32 rows (the blocks of 32 x 32 of 8-bit floats, ORDER 2), places j ^ (i / 2 % 8) have
-// all of them apart, and j ^ i % 8 half (8192 x 4096 -> 16384: 33.6 million cycles of conflicts); with the rows of p in the order of product_f8_kernel_256 (3) those are
-// j ^ (i / 2 % 2 + 2 (i / 16 % 2) + 4 (i / 4 % 2)).
+// ORDER 1: rows of p go to the places that suit the reads of the tiles of 256 x 256 (both types'), j ^ (i % 4 + 4 (i / 8 % 2)).  LDS serves sixteen-byte reads sixteen lanes at a time, from 64
+// banks: lanes 0-3, 12-15, 20-23 and 24-27, then 4-7, 8-11, 16-19 and 28-31.  Where the first 32 lanes read 32 rows (the blocks of 32 x 32 of product_f8_kernel, ORDER 2), places
+// j ^ (i / 2 % 8) have all of them apart, and j ^ i % 8 half.
 template <int TR, int TC, int WAVES, int ORDER>
 struct TileLoads {
     static constexpr int LP = TR / 8 / WAVES, LQ = TC / 8 / WAVES;      // per wave and step
@@ -155,7 +154,7 @@ struct TileLoads {
     {
         static_assert(WAVES % 4 == 0, "rows 8 (i WAVES + wave) .. + 7: bits 3 and 4 are those of the wave");
         const int lane = threadIdx.x & 63, row = lane >> 3, key = ORDER < 2 ? row : (row >> 1) | (wave & 1) << 2;
-        const int key_p = ORDER == 1 ? (row & 3) | (wave & 1) << 2 : ORDER == 3 ? (row >> 1 & 1) | (wave >> 1 & 1) << 1 | (row & 4) : key;
+        const int key_p = ORDER == 1 ? (row & 3) | (wave & 1) << 2 : key;
         const int col = ((lane & 7) ^ key) * 16, col_p = ((lane & 7) ^ key_p) * 16;
 #pragma unroll
         for (int i = 0; i < LP; ++i) off_p[i] = (uint32_t)min(a.R - 1 - r0, (i * WAVES + wave) * 8 + row) * (uint32_t)a.ld_p + col_p;
