@@ -455,7 +455,8 @@ int tictac_gradient_norm(int32_t n, const tictac_gradient *gradients, float scal
  * elements whose sqrt(v) is below 2^-17 of the largest of its block of 128 count as of such a size, and move less than with moments in 32 bits.)  The hash of element i of the tensor with index j of the call is
  *     mix(mix(mix(mix(mix(seed low) + seed high) + step) + j) + i),   mix(x): x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0x6A09E667, x ^= x >> 16
  * in 32 bits, its low half for m, its high half for sqrt(v): the same call has the same result.
- * norm may be NULL (max_norm is not used then); where *norm is not finite nothing is changed.  lr_at and step_at, device, may be NULL; they stand for lr and step, for
+ * norm may be NULL (max_norm is not used then); where *norm is not finite nothing is changed.  Without a norm a NaN or an infinity in a gradient spoils its element, and with moments in 8 bits
+ * its block of 128, whose parameters are NaN from the next step on.  lr_at and step_at, device, may be NULL; they stand for lr and step, for
  * calls that are captured.  step counts from 1.  Tensors may not overlap, nor norm, lr_at and step_at what is written (TICTAC_ERR_UNSUPPORTED); fewer than 2^24 of at most 2^32 elements each. */
 typedef struct tictac_adamw_tensor {
     void *p;                       /* device, contiguous, of dtype, as all of these */

@@ -6,7 +6,7 @@
 // of r = sqrt(v), which the update needs anyway: the range of r is half of v's in powers of two.  They are rounded at random, up with a probability of the part that is cut off: with
 // b2 = 0.999 v decays by 0.1 % a step, and to nearest would never leave a value whose neighbours are 6 to 12 % away.  A positive r is a step of the type at least: it divides, and where it became zero
 // the next step would have only 1 - b2 of a gradient's square under an m of up to a whole step (elements 2^-17 of their block's largest moved by up to 500 lr in a step; now by up to 4).
-// Bound by memory: an element is read and written once.  67 million parameters with moments in 8 bits: 194 to 227 us, 4.8 to 5.6 TB/s.
+// Bound by memory: an element is read and written once.  67 million parameters with moments in 8 bits: 196 to 227 us, 4.8 to 5.5 TB/s (0.7 % of it for the least root, both in turn).
 #include <math.h>
 
 #include <algorithm>

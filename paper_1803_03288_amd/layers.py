@@ -197,7 +197,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], mo
     """One step of AdamW over all ``params``, in place, in few launches.
 
     ``grads`` are multiplied by ``grad_scale``, and where ``max_norm`` is given by ``min(1, max_norm / norm)`` too.  ``norm`` is what ``gradient_norm`` gives for the same
-    ``grad_scale``; where it is not finite, nothing is changed.  Parameters and gradients may each be float32, float16 or bfloat16; arithmetic is float32.  ``copies`` receive
+    ``grad_scale``; where it is not finite, nothing is changed.  Without ``norm`` the step is always taken: a NaN or an infinity in a gradient then spoils its element, and with moments in 8 bits the
+    moments of its block of 128 neighbours, whose parameters are NaN from the next step on.  Parameters and gradients may each be float32, float16 or bfloat16; arithmetic is float32.  ``copies`` receive
     the new parameters in their own types, for parameters in float32 with layers that take 16 bits.  ``step`` counts from 1; it and ``lr`` may be tensors of one element
     on the device (int64, float32), which are read when the step runs, so that a captured one goes on.  Moments in 8 bits are rounded at random by a hash of ``seed``,
     ``step``, the index in ``params`` and the element's: the same call has the same result.  Tensors may not overlap, and ``norm``, ``lr`` and ``step`` may not lie in what is written.  Parameters may have any strides without gaps; gradients
